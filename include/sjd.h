@@ -91,6 +91,10 @@ typedef enum {
  * changed, if one is found. sjd_verify: in sjd_verify_params.flags;
  * decoder contexts: in sjd_config.flags. */
 #define SJD_CHECK_FINITE 32u
+/* sjd_verify_given only: the row behind a window's last draft holds the
+ * target's probabilities too, and a window whose drafts are all accepted
+ * commits one more token, drawn from it */
+#define SJD_BONUS 512u
 /* sjd_verify only, the reference mode of the top-k selection: every row
  * selects its kept set by histograms over the whole row instead of by the
  * candidates at or above a threshold estimated from a sample of the row. The
@@ -196,6 +200,184 @@ SJD_API int sjd_verify(const sjd_verify_params* params, const sjd_verify_io* io,
  * the caller; a call leaves its records behind, and none of the next call's
  * results depend on them. */
 SJD_API int sjd_verify_noalloc(const sjd_verify_params* params, const sjd_verify_io* io, void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* Verification of drafted tokens against given probabilities, with the
+ * caller's own random numbers: for programs that have their own sampler (any
+ * truncation or shaping of the distributions, any generator), where
+ * sjd_verify starts from logits and draws from Philox.
+ *
+ * Window b has n drafts (0 <= n <= L, d_n[b]). Row j < n verifies draft x_j: it
+ * is accepted iff u_j * q_j(x_j) < p_j(x_j) (Sec. 3.2's min(1, p/q) with u in
+ * [0, 1); the products are exact). Rejected, the row's token is drawn from
+ * norm(max(0, p_j - q_j)), or from p_j where that has no mass. Without draft
+ * probabilities (d_q NULL) the drafts are certain (a lookup, a greedy drafter):
+ * q_j is 1 at x_j, so acceptance is u_j < p_j(x_j) and the residual is p_j without
+ * x_j. A draft outside [vis_lo, vis_lo + V) is rejected and its row drawn from
+ * p_j. With SJD_BONUS row n is drawn from p_n.
+ * A draw takes the least x with cum(x) > r * total, weights being summed in 64
+ * bits; weights that are negative or NaN count as zero, and a row without any
+ * mass draws -1.
+ *  committed: the drafts before the first rejection and that row's draw; all
+ *    accepted: the n drafts, and with SJD_BONUS the draw of row n.
+ *  SJD_AC: the rows behind the first rejection are verified too (Sec. 4.2),
+ *    and their tokens (with SJD_BONUS row n's draw last) are the next drafts. */
+typedef struct {
+  int32_t B;       /* windows, 1..65535                                            */
+  int32_t L;       /* most drafts of a window, 1..64                               */
+  int32_t V;       /* probabilities per row, 1..2^24                               */
+  uint32_t flags;  /* SJD_AC | SJD_BONUS                                           */
+  int32_t vis_lo;  /* token id of entry 0                                          */
+  int64_t p_row, p_win, q_row, q_win; /* elements between rows and windows of d_p and d_q;
+                      rows >= V apart (q_*: not looked at when d_q is NULL)         */
+} sjd_given_params;
+
+typedef struct {
+  const float* d_p;       /* target probabilities of rows 0 .. L-1 (SJD_BONUS: .. L)  */
+  const float* d_q;       /* draft probabilities of rows 0 .. L-1, or NULL           */
+  const int32_t* d_draft; /* [B][L] drafts                                           */
+  const int32_t* d_n;     /* [B] drafts of each window, or NULL: L                   */
+  const float* d_u;       /* [B][L] accept uniforms in [0, 1)                        */
+  const float* d_r;       /* [B][L+1] draw uniforms in [0, 1); row j uses entry j    */
+  int32_t* d_meta;        /* [B][4] { n_c committed, first rejected row or -1, accepted
+                             drafts before it, next drafts }, 16-byte aligned          */
+  int32_t* d_tok;         /* [B][L+1] committed tokens (n_c valid, rest -1)          */
+  int32_t* d_next;        /* [B][L] next drafts (rest -1); may be NULL without SJD_AC */
+} sjd_given_io;
+
+/* Outputs must not overlap inputs. A window whose n lies outside [0, L] is not
+ * verified: its meta becomes {-1, -1, 0, 0} and its other outputs are left as
+ * they were. Nothing is allocated; rows of 16-byte aligned buffers whose
+ * strides are multiples of 4 are read fastest. */
+SJD_API int sjd_verify_given(const sjd_given_params* params, const sjd_given_io* io, void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* Operators on a cache in pages, for programs that run their own projections
+ * around this library's step: rows of q and k are placed (sjd_rope_axes), key
+ * and value rows go into the pages (sjd_kv_append), and the new rows attend
+ * over them (sjd_paged_attention). They allocate nothing and keep nothing from
+ * one call to the next, so calls on different streams and captured calls are
+ * independent as long as their buffers are. */
+typedef enum { SJD_F32 = 0, SJD_BF16 = 1, SJD_E4M3 = 2 } sjd_dtype;
+
+/* Rotary positions with several axes (an image token's time, row and column).
+ * Pair i of a head (dims i and pairs + i) turns by
+ *   phi = pos[t][axis[i]] * freq[i]   (formed in 64 bits)
+ * so (a, b) becomes (a cos - b sin, b cos + a sin); dims from 2 * pairs on pass
+ * through. `inverse` turns back. Sections of pairs per axis, interleaved axes, and
+ * frequencies that start anew on each axis are all choices of axis and freq. */
+typedef struct {
+  int32_t T;        /* rows, 0 .. 2^24                                              */
+  int32_t H, Hkv;   /* heads of q and of k, >= 0; 0: that tensor is not there        */
+  int32_t head_dim; /* 2..256, even                                                 */
+  int32_t pairs;    /* 1 .. head_dim / 2                                            */
+  int32_t axes;     /* 1..4                                                         */
+  int32_t dtype;    /* SJD_F32 or SJD_BF16                                          */
+  int32_t inverse;  /* 0 or 1                                                       */
+  int64_t q_row, k_row, out_q_row, out_k_row; /* elements between rows (heads lie one
+                       behind the other), >= heads * head_dim                        */
+  double freq[128];
+  uint8_t axis[128]; /* < axes                                                       */
+} sjd_rope_params;
+
+typedef struct {
+  const void* d_q;      /* [T][H][head_dim]                                          */
+  const void* d_k;      /* [T][Hkv][head_dim]                                        */
+  const int32_t* d_pos; /* [T][axes]                                                 */
+  void* d_out_q;        /* may be d_q itself (same row stride), else must not overlap */
+  void* d_out_k;
+} sjd_rope_io;
+
+SJD_API int sjd_rope_axes(const sjd_rope_params* params, const sjd_rope_io* io, void* stream);
+
+/* A pool of pages. A page holds page_len positions of every key / value head:
+ * [Hkv][K, V] parts of page_len * head_dim elements, then (e4m3) [Hkv][K, V] parts
+ * of page_len exponent bytes, padded to a multiple of 256 bytes.
+ * An e4m3 row of a head carries one exponent byte E (1..254): the values are code *
+ * 2^(E - 127). Rows that sjd_kv_append writes have the smallest E with max |x| <= 448 *
+ * 2^(E - 127), kept within [27, 246] (E = 127 for a row of zeros); the maximum is taken
+ * over finite values, larger ones and infinities become +-448, NaN stays. Powers of
+ * two lose nothing in a floating type, make the quotient exact and are a shift to
+ * undo.
+ * Within a part, positions come in tiles of 32 (32 * head_dim elements), in the
+ * order of the attention's matrix operands, so that a wave reads a tile in
+ * contiguous 1 KB loads. Element of position i (of the tile) and dim j, with
+ * swap(i) = i with its bits 2 and 3 exchanged and h2 = head_dim / 2:
+ *   K: lane = swap(i) + 32 (j / h2), t = j % h2 / 8
+ *      bf16 (64 t + lane) 8 + j % 8;  e4m3 (64 (t / 2) + lane) 16 + 8 (t % 2) + j % 8
+ *   V: lane = j % 32 + 32 (i / 8 % 2)
+ *      bf16 ((j / 32 * 2 + i / 16) 64 + lane) 8 + i % 8
+ *      e4m3 (64 (j / 32) + lane) 16 + 8 (i / 16) + i % 8                              */
+typedef struct {
+  void* d_pool;       /* n_pages * sjd_page_bytes() bytes, 256-byte aligned             */
+  int32_t n_pages;    /* >= 1                                                         */
+  int32_t page_len;   /* positions per page: 32, 64, 128, 256, 512 or 1024             */
+  int32_t n_kv_heads; /* 1..1024                                                      */
+  int32_t head_dim;   /* 64 or 128 (SJD_ENOTSUP otherwise)                            */
+  int32_t dtype;      /* SJD_BF16 or SJD_E4M3                                         */
+} sjd_pages;
+
+/* Bytes of one page (0 for fields out of range). */
+SJD_API int64_t sjd_page_bytes(const sjd_pages* pages);
+
+/* Windows of new rows behind what is cached of B sequences. Sequence z's rows
+ * lie at [row0, row0 + rows) of the row tensors and take positions cached ..
+ * cached + rows - 1; position p is in page table[z][p / page_len]. Row tensors hold T
+ * rows; rows that no sequence names are left as they were.
+ * max_rows and max_cached bound what d_seq holds (they set the launch). Device
+ * data cannot be reported as a status: a sequence whose numbers are negative,
+ * exceed these bounds, its table or T is left out (nothing of it is read or written),
+ * and so are positions whose page id lies outside [0, n_pages). Windows must not
+ * share rows, nor (sjd_kv_append) positions of a page. */
+typedef struct {
+  int32_t B;          /* sequences, 0..65535                                          */
+  int32_t T;          /* rows of the row tensors                                      */
+  int32_t max_rows;   /* rows of the longest window                                   */
+  int32_t max_cached; /* cached positions of the longest sequence                     */
+  int32_t table_len;  /* page ids per sequence                                        */
+  const int32_t* d_seq;   /* [B][4] { row0, rows, cached, 0 }, 16-byte aligned           */
+  const int32_t* d_table; /* [B][table_len]                                           */
+} sjd_windows;
+
+/* Key and value rows [T][n_kv_heads][head_dim], heads one behind the other. */
+typedef struct {
+  void* d_k;
+  void* d_v;
+  int64_t k_row, v_row; /* elements between rows, multiples of 8; pointers 16-byte aligned */
+  int32_t dtype;        /* SJD_F32 or SJD_BF16                                         */
+} sjd_kv_rows;
+
+/* Writes the windows' rows into their pages (rounded to the pages' type); other
+ * positions of a page keep their bytes. */
+SJD_API int sjd_kv_append(const sjd_pages* pages, const sjd_windows* win, const sjd_kv_rows* rows, void* stream);
+
+/* Reads positions cached .. cached + rows - 1 of every sequence back into the rows
+ * (rounded to their type). Positions outside the pool read as zeros. */
+SJD_API int sjd_kv_read(const sjd_pages* pages, const sjd_windows* win, const sjd_kv_rows* rows, void* stream);
+
+/* Attention of the windows' rows over their sequences' pages, which hold the
+ * rows' own keys and values already (sjd_kv_append): out = softmax(scale * q . k) v
+ * over every cached position and, of the window, over the rows up to itself or
+ * (d_anc) the rows i whose bit i is set in the row's ancestor mask (tree windows;
+ * max_rows <= 64). A row that attends to nothing gives zeros. Query head h uses
+ * key / value head h / (H / n_kv_heads). Scores, statistics and sums are held in 32
+ * bits; probabilities enter the value product as bf16, relative to the row's
+ * running maximum. Non-finite keys and values reach only rows that attend to them.
+ * d_ws: sjd_paged_attention_workspace() bytes of scratch, 256-byte aligned (NULL
+ * when that is 0); it holds nothing between calls, and calls that overlap in time
+ * need one each. */
+typedef struct {
+  int32_t H;             /* query heads, a multiple of n_kv_heads                      */
+  float scale;           /* finite                                                    */
+  const void* d_q;       /* [T][H][head_dim] bf16, 16-byte aligned                      */
+  void* d_out;           /* [T][H][head_dim] bf16, 16-byte aligned; must not overlap q   */
+  int64_t q_row, out_row; /* elements between rows, multiples of 8                       */
+  const uint64_t* d_anc; /* [T] ancestor masks, or NULL: causal                         */
+} sjd_attention_io;
+
+SJD_API int64_t sjd_paged_attention_workspace(const sjd_pages* pages, const sjd_windows* win, int32_t H);
+SJD_API int sjd_paged_attention(const sjd_pages* pages, const sjd_windows* win, const sjd_attention_io* io, void* d_ws,
+                                int64_t ws_bytes, void* stream);
 
 /* ------------------------------------------------------------------------ */
 /* Decoder context: weights, KV cache and window state of one generation.

@@ -1,0 +1,83 @@
+// Internal interface of the standalone operators (not part of the C ABI):
+// rotary axes, caches in pages, their attention, given verification.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "sjd.h"
+
+namespace sjd {
+
+// ---- pages (layout: sjd.h). page_len is a power of two of at least a tile.
+constexpr int kTile = 32;          // positions per tile, the attention's MFMA key rows
+constexpr int kMinExp = 27, kMaxExp = 246;  // exponent bytes that the quantiser writes
+
+struct PoolView {
+  char* pool;
+  int n_pages, Hkv;
+  int plen_log2;
+  int64_t page_bytes;
+};
+
+inline int64_t page_data_bytes(const sjd_pages& p) {
+  return 2LL * p.n_kv_heads * p.page_len * p.head_dim * (p.dtype == SJD_E4M3 ? 1 : 2);
+}
+inline int64_t page_bytes(const sjd_pages& p) {
+  const int64_t b = page_data_bytes(p) + (p.dtype == SJD_E4M3 ? 2LL * p.n_kv_heads * p.page_len : 0);
+  return (b + 255) / 256 * 256;
+}
+inline PoolView pool_view(const sjd_pages& p) {
+  int lg = 0;
+  while ((1 << lg) < p.page_len) ++lg;
+  return PoolView{(char*)p.d_pool, p.n_pages, p.n_kv_heads, lg, page_bytes(p)};
+}
+
+#ifdef __HIPCC__
+// A sequence of a call, or rows = 0 where its numbers break the call's bounds
+// (sjd.h: it is left out).
+struct Seq {
+  int row0, rows, cached;
+};
+__device__ __forceinline__ Seq load_seq(const sjd_windows& w, const PoolView& pv, int z) {
+  const int4 v = ((const int4*)w.d_seq)[z];
+  Seq s{v.x, v.y, v.z};
+  // (unsigned: negative numbers are large)
+  const bool ok = (uint32_t)s.rows <= (uint32_t)w.max_rows && (uint32_t)s.cached <= (uint32_t)w.max_cached && s.row0 >= 0 &&
+                  s.row0 <= w.T - s.rows && (int64_t)s.cached + s.rows <= ((int64_t)w.table_len << pv.plen_log2);
+  if (!ok) s.rows = 0;
+  return s;
+}
+// Start of the page that holds position p of sequence z, or NULL
+__device__ __forceinline__ char* page_of(const sjd_windows& w, const PoolView& pv, int z, int p) {
+  const int id = w.d_table[(int64_t)z * w.table_len + (p >> pv.plen_log2)];
+  return (uint32_t)id < (uint32_t)pv.n_pages ? pv.pool + (int64_t)id * pv.page_bytes : nullptr;
+}
+// Byte offsets inside a page, head h: the tile of position `in` (of the page), and
+// the exponent bytes of the page's positions 0 ..
+template <int HD, int ES>
+__device__ __forceinline__ int64_t tile_off(const PoolView& pv, int h, int in, int kv) {
+  return (((int64_t)(2 * h + kv) << pv.plen_log2) + (in & ~(kTile - 1))) * (HD * ES);
+}
+template <int HD>
+__device__ __forceinline__ int64_t exp_off(const PoolView& pv, int h, int kv) {
+  return ((int64_t)2 * pv.Hkv * HD + 2 * h + kv) << pv.plen_log2;
+}
+#endif
+
+hipError_t launch_kv_append(const sjd_pages& p, const sjd_windows& w, const sjd_kv_rows& r, hipStream_t s);
+hipError_t launch_kv_read(const sjd_pages& p, const sjd_windows& w, const sjd_kv_rows& r, hipStream_t s);
+
+// ---- attention over pages
+struct AttnPlan {
+  int chunk;   // keys per split, a multiple of the workgroup's keys per round
+  int splits;  // most splits of a sequence
+};
+AttnPlan paged_attention_plan(const sjd_pages& p, const sjd_windows& w, int H);
+int64_t paged_attention_ws(const sjd_pages& p, const sjd_windows& w, int H);
+hipError_t launch_paged_attention(const sjd_pages& p, const sjd_windows& w, const sjd_attention_io& io, void* ws,
+                                  hipStream_t s);
+
+hipError_t launch_rope_axes(const sjd_rope_params& p, const sjd_rope_io& io, hipStream_t s);
+hipError_t launch_verify_given(const sjd_given_params& p, const sjd_given_io& io, hipStream_t s);
+
+}  // namespace sjd

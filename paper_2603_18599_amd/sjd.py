@@ -18,6 +18,7 @@ SJD_NO_TUNE = 8
 SJD_TUNE = 16
 SJD_CHECK_FINITE = 32
 SJD_FULL_SELECT = 64
+SJD_BONUS = 512
 SJD_VERIFY_NOALLOC_MAX_ROWS = 131072
 
 _STATUS = {0: "SJD_OK", -1: "SJD_EINVAL", -2: "SJD_ENOMEM", -3: "SJD_EHIP", -4: "SJD_ESTATE", -5: "SJD_ENOTSUP",
@@ -58,9 +59,53 @@ class Weights(C.Structure):
                 ("d_lm_head", C.c_void_p)]
 
 
+class GivenParams(C.Structure):
+    _fields_ = [("B", C.c_int32), ("L", C.c_int32), ("V", C.c_int32), ("flags", C.c_uint32), ("vis_lo", C.c_int32),
+                ("p_row", C.c_int64), ("p_win", C.c_int64), ("q_row", C.c_int64), ("q_win", C.c_int64)]
+
+
+class GivenIO(C.Structure):
+    _fields_ = [("d_p", C.c_void_p), ("d_q", C.c_void_p), ("d_draft", C.c_void_p), ("d_n", C.c_void_p),
+                ("d_u", C.c_void_p), ("d_r", C.c_void_p), ("d_meta", C.c_void_p), ("d_tok", C.c_void_p),
+                ("d_next", C.c_void_p)]
+
+
+class RopeParams(C.Structure):
+    _fields_ = [("T", C.c_int32), ("H", C.c_int32), ("Hkv", C.c_int32), ("head_dim", C.c_int32),
+                ("pairs", C.c_int32), ("axes", C.c_int32), ("dtype", C.c_int32), ("inverse", C.c_int32),
+                ("q_row", C.c_int64), ("k_row", C.c_int64), ("out_q_row", C.c_int64), ("out_k_row", C.c_int64),
+                ("freq", C.c_double * 128), ("axis", C.c_uint8 * 128)]
+
+
+class RopeIO(C.Structure):
+    _fields_ = [("d_q", C.c_void_p), ("d_k", C.c_void_p), ("d_pos", C.c_void_p), ("d_out_q", C.c_void_p),
+                ("d_out_k", C.c_void_p)]
+
+
+class PagesDesc(C.Structure):
+    _fields_ = [("d_pool", C.c_void_p), ("n_pages", C.c_int32), ("page_len", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("dtype", C.c_int32)]
+
+
+class WindowsDesc(C.Structure):
+    _fields_ = [("B", C.c_int32), ("T", C.c_int32), ("max_rows", C.c_int32), ("max_cached", C.c_int32),
+                ("table_len", C.c_int32), ("d_seq", C.c_void_p), ("d_table", C.c_void_p)]
+
+
+class KvRows(C.Structure):
+    _fields_ = [("d_k", C.c_void_p), ("d_v", C.c_void_p), ("k_row", C.c_int64), ("v_row", C.c_int64),
+                ("dtype", C.c_int32)]
+
+
+class AttentionIO(C.Structure):
+    _fields_ = [("H", C.c_int32), ("scale", C.c_float), ("d_q", C.c_void_p), ("d_out", C.c_void_p),
+                ("q_row", C.c_int64), ("out_row", C.c_int64), ("d_anc", C.c_void_p)]
+
+
 EXPORTS = ["sjd_status_str", "sjd_verify", "sjd_verify_noalloc", "sjd_init", "sjd_prefill", "sjd_prefill_image",
            "sjd_prefill_cfg", "sjd_prefill_image_cfg", "sjd_set_drafts", "sjd_step", "sjd_forward_window",
-           "sjd_get_plan", "sjd_destroy"]
+           "sjd_get_plan", "sjd_destroy", "sjd_verify_given", "sjd_rope_axes", "sjd_page_bytes", "sjd_kv_append",
+           "sjd_kv_read", "sjd_paged_attention_workspace", "sjd_paged_attention"]
 
 _lib = None
 
@@ -111,6 +156,20 @@ def load_library():
     lib.sjd_forward_window.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p]
     lib.sjd_destroy.restype = None
     lib.sjd_destroy.argtypes = [C.c_void_p]
+    lib.sjd_verify_given.restype = C.c_int
+    lib.sjd_verify_given.argtypes = [C.POINTER(GivenParams), C.POINTER(GivenIO), C.c_void_p]
+    lib.sjd_rope_axes.restype = C.c_int
+    lib.sjd_rope_axes.argtypes = [C.POINTER(RopeParams), C.POINTER(RopeIO), C.c_void_p]
+    lib.sjd_page_bytes.restype = C.c_int64
+    lib.sjd_page_bytes.argtypes = [C.POINTER(PagesDesc)]
+    for name in ("sjd_kv_append", "sjd_kv_read"):
+        getattr(lib, name).restype = C.c_int
+        getattr(lib, name).argtypes = [C.POINTER(PagesDesc), C.POINTER(WindowsDesc), C.POINTER(KvRows), C.c_void_p]
+    lib.sjd_paged_attention_workspace.restype = C.c_int64
+    lib.sjd_paged_attention_workspace.argtypes = [C.POINTER(PagesDesc), C.POINTER(WindowsDesc), C.c_int32]
+    lib.sjd_paged_attention.restype = C.c_int
+    lib.sjd_paged_attention.argtypes = [C.POINTER(PagesDesc), C.POINTER(WindowsDesc), C.POINTER(AttentionIO),
+                                        C.c_void_p, C.c_int64, C.c_void_p]
     _lib = lib
     return lib
 
@@ -159,6 +218,164 @@ def verify_outputs(B, L, K, D, device="cuda"):
             "tok": torch.zeros(B, L, dtype=torch.int32, device=device),
             "next": torch.zeros(B, L, dtype=torch.int32, device=device),
             "sib": torch.zeros(B, max(D, 0), max(K - 1, 0), dtype=torch.int32, device=device)}
+
+
+def _expect(fn, ok):
+    """The library reads device memory by the sizes that it is told: a tensor of
+    another type, shape or layout is refused like any other bad argument."""
+    if not ok:
+        raise SjdError(fn, -1)
+
+
+def _rows_of(fn, t, T, heads, hd, dtypes):
+    """Row stride of [T, heads, hd] rows whose heads lie one behind the other."""
+    _expect(fn, t.dim() == 3 and tuple(t.shape) == (T, heads, hd) and str(t.dtype)[6:] in dtypes)
+    _expect(fn, T == 0 or heads == 0 or (t.stride(2) == 1 and (heads == 1 or t.stride(1) == hd)))
+    return t.stride(0) if T > 1 else max(t.stride(0), heads * hd)
+
+
+def _one_device(fn, *tensors):
+    """Every tensor on the current GPU (the library launches there)."""
+    import torch
+    for t in tensors:
+        if t is not None:
+            _expect(fn, t.device.type == "cuda" and t.device.index == torch.cuda.current_device())
+
+
+def _dense(fn, t, shape, dtype):
+    _expect(fn, t is None or (tuple(t.shape) == tuple(shape) and t.is_contiguous() and str(t.dtype)[6:] == dtype))
+
+
+def sjd_verify_given(p, q, draft, n, u, r, meta, tok, next=None, *, flags=0, vis_lo=0, stream=None):
+    """Verification against given probabilities with given uniforms
+    (sjd_verify_given in include/sjd.h). p: float32 [B, L (SJD_BONUS: L + 1),
+    V], q: float32 [B, L, V] or None (certain drafts), entries one behind the
+    other; draft int32 [B, L]; n int32 [B] or None; u float32 [B, L]; r
+    float32 [B, L + 1]; outputs int32 meta [B, 4], tok [B, L + 1], next [B, L]
+    (None without SJD_AC)."""
+    fn = "sjd_verify_given"
+    _expect(fn, draft.dim() == 2 and p.dim() == 3)
+    (B, L), V = draft.shape, p.shape[2]
+    _dense(fn, draft, (B, L), "int32")
+    _dense(fn, n, (B,), "int32")
+    _dense(fn, u, (B, L), "float32")
+    _dense(fn, r, (B, L + 1), "float32")
+    _dense(fn, meta, (B, 4), "int32")
+    _dense(fn, tok, (B, L + 1), "int32")
+    _dense(fn, next, (B, L), "int32")
+    for t, rows in ((p, L + (1 if flags & SJD_BONUS else 0)), (q, L)):
+        _expect(fn, t is None or (tuple(t.shape) == (B, rows, V) and str(t.dtype) == "torch.float32" and
+                                  (V <= 1 or t.stride(2) == 1)))
+    _one_device(fn, p, q, draft, n, u, r, meta, tok, next)
+    par = GivenParams(B, L, V, flags, vis_lo, p.stride(1), p.stride(0), q.stride(1) if q is not None else 0,
+                      q.stride(0) if q is not None else 0)
+    io = GivenIO(_ptr(p), _ptr(q), _ptr(draft), _ptr(n), _ptr(u), _ptr(r), _ptr(meta), _ptr(tok), _ptr(next))
+    _check(fn, load_library().sjd_verify_given(C.byref(par), C.byref(io), _stream(stream)))
+
+
+_DTYPES = {"float32": 0, "bfloat16": 1, "e4m3": 2, "bf16": 1}
+
+
+def sjd_rope_axes(q, k, pos, freq, axis, *, out_q=None, out_k=None, inverse=False, stream=None):
+    """Rotary positions with several axes (sjd_rope_axes in include/sjd.h) on
+    rows q [T, H, hd] and k [T, Hkv, hd] (either may be None; bfloat16 or
+    float32), in place unless out_q / out_k are given. pos int32 [T, axes]; freq
+    and axis: one frequency and one axis for each pair of dims."""
+    fn = "sjd_rope_axes"
+    x = q if q is not None else k
+    _expect(fn, x is not None and x.dim() == 3 and pos.dim() == 2 and 1 <= len(freq) <= 128 and len(axis) == len(freq))
+    T, hd, dt = x.shape[0], x.shape[2], str(x.dtype)[6:]
+    _expect(fn, all(0 <= a < pos.shape[1] for a in axis))
+    out_q, out_k = q if out_q is None else out_q, k if out_k is None else out_k
+    par = RopeParams(T, 0, 0, hd, len(freq), pos.shape[1], _DTYPES.get(dt, -1), 1 if inverse else 0)
+    par.freq[:len(freq)] = list(freq)
+    par.axis[:len(axis)] = list(axis)
+    _dense(fn, pos, (T, pos.shape[1]), "int32")
+    if q is not None:
+        par.H = q.shape[1] if q.dim() == 3 else -1
+        par.q_row, par.out_q_row = (_rows_of(fn, t, T, par.H, hd, (dt,)) for t in (q, out_q))
+    if k is not None:
+        par.Hkv = k.shape[1] if k.dim() == 3 else -1
+        par.k_row, par.out_k_row = (_rows_of(fn, t, T, par.Hkv, hd, (dt,)) for t in (k, out_k))
+    _one_device(fn, q, k, pos, out_q, out_k)
+    io = RopeIO(_ptr(q), _ptr(k), _ptr(pos), _ptr(out_q), _ptr(out_k))
+    _check(fn, load_library().sjd_rope_axes(C.byref(par), C.byref(io), _stream(stream)))
+
+
+def page_bytes(page_len, n_kv_heads, head_dim, dtype):
+    """Bytes of a page (dtype "bf16" or "e4m3"); 0 for sizes that no page has."""
+    d = PagesDesc(None, 1, page_len, n_kv_heads, head_dim, _DTYPES[dtype])
+    return load_library().sjd_page_bytes(C.byref(d))
+
+
+class Pages:
+    """A pool of pages (sjd_pages) in the caller's uint8 tensor."""
+
+    def __init__(self, pool, n_pages, page_len, n_kv_heads, head_dim, dtype):
+        fn = "sjd_pages"
+        size = page_bytes(page_len, n_kv_heads, head_dim, dtype)
+        _expect(fn, size > 0 and n_pages >= 1 and str(pool.dtype) == "torch.uint8" and pool.is_contiguous() and
+                pool.numel() >= n_pages * size)
+        self.pool, self.n_kv_heads, self.head_dim = pool, n_kv_heads, head_dim
+        self.desc = PagesDesc(_ptr(pool), n_pages, page_len, n_kv_heads, head_dim, _DTYPES[dtype])
+
+
+class Windows:
+    """Windows of new rows (sjd_windows): seq int32 [B, 4] = (row0, rows, cached,
+    0), table int32 [B, pages], over row tensors of T rows."""
+
+    def __init__(self, seq, table, T, max_rows, max_cached):
+        fn = "sjd_windows"
+        B = seq.shape[0]
+        _dense(fn, seq, (B, 4), "int32")
+        _expect(fn, table.dim() == 2)
+        _dense(fn, table, (B, table.shape[1]), "int32")
+        self.seq, self.table, self.T = seq, table, T
+        self.desc = WindowsDesc(B, T, max_rows, max_cached, table.shape[1], _ptr(seq), _ptr(table))
+
+
+def _kv_call(fn, pages, win, k, v, stream):
+    dt = str(k.dtype)[6:]
+    rows = KvRows(_ptr(k), _ptr(v), *(_rows_of(fn, t, win.T, pages.n_kv_heads, pages.head_dim, (dt,)) for t in (k, v)),
+                  _DTYPES.get(dt, -1))
+    _one_device(fn, pages.pool, win.seq, win.table, k, v)
+    _check(fn, getattr(load_library(), fn)(C.byref(pages.desc), C.byref(win.desc), C.byref(rows), _stream(stream)))
+
+
+def sjd_kv_append(pages, win, k, v, stream=None):
+    """Writes rows k, v [T, Hkv, hd] (bfloat16 or float32) into the windows'
+    pages (sjd_kv_append in include/sjd.h)."""
+    _kv_call("sjd_kv_append", pages, win, k, v, stream)
+
+
+def sjd_kv_read(pages, win, k, v, stream=None):
+    """Reads the windows' positions back into rows k, v [T, Hkv, hd]
+    (sjd_kv_read in include/sjd.h)."""
+    _kv_call("sjd_kv_read", pages, win, k, v, stream)
+
+
+def attention_workspace(pages, win, H):
+    """Scratch for sjd_paged_attention with these pages and windows (calls that
+    overlap in time need one each)."""
+    import torch
+    n = load_library().sjd_paged_attention_workspace(C.byref(pages.desc), C.byref(win.desc), H)
+    return torch.empty(n, dtype=torch.uint8, device=pages.pool.device)
+
+
+def sjd_paged_attention(pages, win, q, out, ws, *, scale, anc=None, stream=None):
+    """Attention of rows q [T, H, hd] over the windows' pages into out
+    (sjd_paged_attention in include/sjd.h); bfloat16. ws: attention_workspace;
+    anc: int64 [T] ancestor masks of tree windows, or None (causal)."""
+    fn = "sjd_paged_attention"
+    _expect(fn, q.dim() == 3)
+    H = q.shape[1]
+    io = AttentionIO(H, scale, _ptr(q), _ptr(out), *(_rows_of(fn, t, win.T, H, pages.head_dim, ("bfloat16",))
+                                                     for t in (q, out)), _ptr(anc))
+    _dense(fn, anc, (win.T,), "int64")
+    _expect(fn, str(ws.dtype) == "torch.uint8" and ws.is_contiguous())
+    _one_device(fn, pages.pool, win.seq, win.table, q, out, anc, ws if ws.numel() else None)
+    _check(fn, load_library().sjd_paged_attention(C.byref(pages.desc), C.byref(win.desc), C.byref(io), _ptr(ws),
+                                                   ws.numel(), _stream(stream)))
 
 
 class Engine:

@@ -1,0 +1,301 @@
+"""sjd_paged_attention against the plain 64-bit form, over the cache as it
+was written (values decoded from the pages' bytes)."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2603_18599_amd as sjd
+from ops_util import Pool, attention, attention_tolerance, quantise, table_for
+
+pytestmark = pytest.mark.gpu
+
+
+class Case:
+    """Sequences (rows, cached), their pages filled by sjd_kv_append, and q."""
+
+    def __init__(self, seqs, plen, Hkv, G, hd, cache, seed=0, gap=2, scale=1.0, fill=0xFF):
+        self.seqs, self.Hkv, self.G, self.H, self.hd, self.cache = seqs, Hkv, G, Hkv * G, hd, cache
+        self.plen = plen
+        self.table, n_pages = table_for(seqs, plen, seed)
+        self.pool = Pool(n_pages, plen, Hkv, hd, cache, fill)
+        g = torch.Generator().manual_seed(seed + 1)
+        self.k, self.v = ([torch.randn(r + n, Hkv, hd, generator=g).to(torch.bfloat16) for r, n in seqs] for _ in range(2))
+        self.seq, at = [], gap
+        for r, n in seqs:
+            self.seq.append([at, r, n, 0])
+            at += r + gap
+        self.T = at
+        self.q = (torch.randn(self.T, self.H, hd, generator=g) * scale).to(torch.bfloat16)
+        self.st = torch.tensor(self.seq, dtype=torch.int32).cuda()
+        self.tt = torch.from_numpy(self.table).cuda()
+        self.scale = hd ** -0.5
+        self.fill_pages()
+
+    def fill_pages(self):
+        rows = [r + n for r, n in self.seqs]
+        if not sum(rows):
+            return
+        whole = torch.tensor([[sum(rows[:z]), m, 0, 0] for z, m in enumerate(rows)], dtype=torch.int32).cuda()
+        win = sjd.Windows(whole, self.tt, sum(rows), max(rows), 0)
+        sjd.sjd_kv_append(self.pool.pages, win, torch.cat(self.k).cuda(), torch.cat(self.v).cuda())
+
+    def windows(self, slack=0):
+        return sjd.Windows(self.st, self.tt, self.T, max(r for r, _ in self.seqs), max(n for _, n in self.seqs) + slack)
+
+    def run(self, anc=None, q=None, slack=0):
+        win = self.windows(slack)
+        ws = sjd.attention_workspace(self.pool.pages, win, self.H)
+        ws.fill_(0xFF)  # (NaN: nothing of it may be read before it is written)
+        out = torch.full((self.T, self.H, self.hd), 3.0, dtype=torch.bfloat16, device="cuda")
+        sjd.sjd_paged_attention(self.pool.pages, win, self.q.cuda() if q is None else q, out, ws, scale=self.scale,
+                                anc=anc)
+        return out
+
+    def value(self, x):
+        x = x.double().numpy()
+        return quantise(x)[0] if self.cache == "e4m3" else x
+
+    def seen(self, z, anc=None, left_out=()):
+        r, n = self.seqs[z]
+        p = np.arange(n + r)
+        s = (p[None] - n) <= np.arange(r)[:, None]
+        if anc is not None:
+            first = self.seq[z][0]
+            s = np.array([[x < n or (int(anc[first + i]) >> int(x - n)) & 1 for x in p] for i in range(r)], bool).reshape(r, n + r)
+        for a, b in left_out:
+            s[:, a:b] = False
+        return s
+
+    def check(self, out, anc=None, left_out=(), skip=()):
+        got = out.double().cpu().numpy()
+        named = np.zeros(self.T, bool)
+        for z, (first, r, n, _) in enumerate(self.seq):
+            if z in skip or r == 0:
+                continue
+            named[first:first + r] = True
+            k, v = self.value(self.k[z]), self.value(self.v[z])
+            seen = self.seen(z, anc, left_out)
+            for h in range(self.H):
+                qh = self.q[first:first + r, h].double().numpy()
+                kh, vh = k[:, h // self.G], v[:, h // self.G]
+                want, mag = attention(qh, kh, vh, self.scale, seen)
+                tol = attention_tolerance(qh, kh[seen.any(0)], self.scale, mag, want, n + r)
+                err = np.abs(got[first:first + r, h] - want)
+                assert (err <= tol).all(), (z, h, float((err - tol).max()))
+        assert (got[~named] == 3.0).all()  # rows that nobody names
+
+
+SEQS = [
+    [(1, 0)], [(1, 1239)], [(1, 31), (1, 32), (1, 95), (0, 40), (1, 0), (1, 700)],
+    [(32, 333), (7, 64), (31, 0)], [(64, 5), (33, 1000)], [(130, 0), (1, 259)], [(300, 421)]]
+
+
+@pytest.mark.parametrize("cache", ["e4m3", "bf16"])
+@pytest.mark.parametrize("hd,Hkv,G,plen", [(128, 2, 4, 64), (64, 3, 1, 32), (128, 1, 7, 128), (64, 2, 16, 1024)])
+@pytest.mark.parametrize("seqs", SEQS, ids=[str(i) for i in range(len(SEQS))])
+def test_causal(seqs, hd, Hkv, G, plen, cache):
+    c = Case(seqs, plen, Hkv, G, hd, cache, scale=2.0)
+    c.check(c.run())
+
+
+@pytest.mark.parametrize("cache", ["e4m3", "bf16"])
+@pytest.mark.parametrize("hd,Hkv,G", [(128, 1, 4), (64, 2, 2), (128, 2, 1)])
+def test_tree(hd, Hkv, G, cache):
+    """Ancestor masks: any of them, also of later rows, rows without any bit
+    (and, with nothing cached, without any key: zeros), bits behind the window."""
+    c = Case([(64, 700), (5, 0), (33, 31), (64, 0)], 32, Hkv, G, hd, cache)
+    g = np.random.RandomState(3)
+    anc = g.randint(0, 2 ** 32, c.T).astype(np.uint64) << np.uint64(32) | g.randint(0, 2 ** 32, c.T).astype(np.uint64)
+    anc[c.seq[0][0]:c.seq[0][0] + 40] = [(1 << (i + 1)) - 1 for i in range(40)]
+    anc[c.seq[0][0] + 50] = 0
+    anc[c.seq[1][0] + 2] = 0
+    anc[c.seq[1][0] + 3] = 1 << 60
+    anc[c.seq[3][0] + 7] = 0
+    out = c.run(torch.from_numpy(anc.astype(np.int64)).cuda())
+    c.check(out, anc)
+    assert not out[c.seq[1][0] + 2].any() and not out[c.seq[1][0] + 3].any() and not out[c.seq[3][0] + 7].any()
+
+
+def test_long_cache_is_split():
+    for seqs in ([(1, 20000)], [(3, 6000), (1, 17), (2, 0)]):
+        c = Case(seqs, 256, 1, 4, 128, "e4m3", scale=3.0)
+        assert sjd.attention_workspace(c.pool.pages, c.windows(), c.H).numel() > 0
+        c.check(c.run())
+
+
+def test_bounds_larger_than_the_data():
+    c = Case([(3, 77), (1, 200)], 64, 2, 4, 128, "e4m3")
+    a, b = c.run(), c.run(slack=5000)
+    c.check(a)
+    c.check(b)
+
+
+def test_strided_rows():
+    """q inside the rows of a joint projection, out inside wider rows."""
+    c = Case([(20, 100), (1, 3)], 32, 2, 2, 64, "bf16")
+    wide = torch.randn(c.T, 7 * 64 + 8, device="cuda").to(torch.bfloat16)
+    q = wide[:, 8:8 + c.H * 64].view(c.T, c.H, 64)
+    q.copy_(c.q.cuda())
+    win = c.windows()
+    out = torch.full((c.T, c.H * 64 + 24), 3.0, dtype=torch.bfloat16, device="cuda")
+    o = out[:, 16:16 + c.H * 64].view(c.T, c.H, 64)
+    ws = sjd.attention_workspace(c.pool.pages, win, c.H)
+    sjd.sjd_paged_attention(c.pool.pages, win, q, o, ws, scale=c.scale)
+    c.check(o)
+    assert bool((out[:, :16] == 3.0).all()) and bool((out[:, 16 + c.H * 64:] == 3.0).all())
+
+
+def test_pages_outside_the_pool_are_left_out():
+    c = Case([(40, 130), (1, 300)], 64, 2, 4, 64, "e4m3")
+    c.tt[:, 1] = 1 << 28
+    c.check(c.run(), left_out=[(64, 128)])
+    c.tt.fill_(-1)
+    out = c.run()
+    for first, r, _, _ in c.seq:
+        assert not out[first:first + r].any()
+
+
+def test_wrong_sequences_are_left_out():
+    c = Case([(4, 60), (3, 10), (2, 5), (1, 9)], 32, 1, 2, 64, "bf16")
+    c.st[1] = torch.tensor([c.T - 2, 3, 10, 0])
+    c.st[2] = torch.tensor([c.seq[2][0], 2, -1, 0])
+    c.check(c.run(), skip=(1, 2))
+
+
+@pytest.mark.parametrize("cache", ["e4m3", "bf16"])
+@pytest.mark.parametrize("rows", [40, 200])
+def test_non_finite_values_reach_only_rows_that_attend(cache, rows):
+    c = Case([(rows, 70)], 32, 1, 2, 64, cache)
+    clean = c.run()
+    bad = 23  # window row whose key and value are not finite
+    p = 70 + bad
+    for x in (float("nan"),) if cache == "e4m3" else (float("nan"), float("inf"), float("-inf")):
+        keep_k, keep_v = c.k[0].clone(), c.v[0].clone()
+        c.v[0][p, 0, 11] = x
+        c.v[0][p, 0, 40] = x
+        c.fill_pages()
+        out = c.run()
+        first = c.seq[0][0]
+        assert torch.equal(out[first:first + bad], clean[first:first + bad])
+        hit = out[first + bad:first + rows]
+        want = torch.tensor(x).expand_as(hit[..., 11])
+        assert torch.equal(torch.nan_to_num(hit[..., 11].float().cpu(), 1e9), torch.nan_to_num(want, 1e9))
+        assert bool(torch.isfinite(hit[..., [0, 10, 12, 39, 41, 63]].float()).all())
+        c.k[0], c.v[0] = keep_k.clone(), keep_v.clone()
+        c.k[0][p, 0, 3] = x  # a key: whole rows, of those that attend
+        c.fill_pages()
+        out = c.run()
+        assert torch.equal(out[first:first + bad], clean[first:first + bad])
+        c.k[0] = keep_k
+        c.fill_pages()
+    # masked by a tree: nobody attends to it
+    if rows <= 64:
+        c.v[0][p] = float("nan")
+        c.k[0][p] = float("nan")
+        c.fill_pages()
+        anc = np.array([((1 << 64) - 1) & ~(1 << bad)] * c.T, np.uint64)
+        out = c.run(torch.from_numpy(anc.astype(np.int64)).cuda())
+        assert bool(torch.isfinite(out.float()).all())
+
+
+def test_large_scores_and_lowest_values():
+    """Scores of some thousands (one key takes all), and keys of bf16's lowest
+    value, whose scores are huge or minus infinity."""
+    c = Case([(3, 200)], 32, 1, 1, 64, "bf16", scale=200.0)
+    c.check(c.run())
+    c.q.abs_()
+    c.k[0][5:60] = torch.finfo(torch.bfloat16).min
+    c.fill_pages()
+    out = c.run()
+    c.check(out, left_out=[(5, 60)])
+
+
+def test_runs_agree_and_follow_their_stream():
+    """The same call twice, and on another stream behind its inputs' copies:
+    the same bits."""
+    c = Case([(32, 900), (1, 2000)], 64, 2, 4, 128, "e4m3")
+    a = c.run()
+    assert torch.equal(a, c.run())
+    s = torch.cuda.Stream()
+    q = torch.zeros_like(c.q, device="cuda")
+    win = c.windows()
+    ws, out = sjd.attention_workspace(c.pool.pages, win, c.H), torch.full_like(a, 3.0)
+    torch.cuda.synchronize()
+    src = c.q.pin_memory()
+    with torch.cuda.stream(s):
+        q.copy_(src, non_blocking=True)
+        sjd.sjd_paged_attention(c.pool.pages, win, q, out, ws, scale=c.scale)
+    s.synchronize()
+    assert torch.equal(a, out)
+
+
+def test_the_operators_together_and_captured():
+    """A serving step: rows placed, written, attended to. Captured once and
+    replayed while the sequences grow (their numbers live in device memory), each
+    replay against the same calls made eagerly and against the plain form."""
+    B, rows, Hkv, G, hd, plen = 3, 5, 2, 4, 128, 64
+    H, T, steps = Hkv * G, 3 * 5, 6
+    for cache in ("e4m3", "bf16"):
+        table, n_pages = table_for([(rows * steps, 100 * z) for z in range(B)], plen)
+        pools = [Pool(n_pages, plen, Hkv, hd, cache, fill=0) for _ in range(2)]
+        tt = torch.from_numpy(table).cuda()
+        seq = torch.tensor([[rows * z, rows, 100 * z, 0] for z in range(B)], dtype=torch.int32).cuda()
+        g = torch.Generator().manual_seed(1)
+        P = hd // 2
+        freq, axis = [1e4 ** (-i / P) for i in range(P)], [i % 3 for i in range(P)]
+        io = {}
+        for e in range(2):
+            io[e] = dict(qkv=torch.zeros(T, (H + 2 * Hkv) * hd, dtype=torch.bfloat16, device="cuda"),
+                         pos=torch.zeros(T, 3, dtype=torch.int32, device="cuda"),
+                         out=torch.zeros(T, H, hd, dtype=torch.bfloat16, device="cuda"),
+                         win=sjd.Windows(seq.clone(), tt, T, rows, 100 * B + rows * steps))
+            io[e]["ws"] = sjd.attention_workspace(pools[e].pages, io[e]["win"], H)
+        past = []
+        for z in range(B):  # what is cached already
+            past.append([torch.randn(100 * z, Hkv, hd, generator=g).to(torch.bfloat16) for _ in range(2)])
+        for pool in pools:
+            m = [100 * z for z in range(B)]
+            whole = torch.tensor([[sum(m[:z]), m[z], 0, 0] for z in range(B)], dtype=torch.int32).cuda()
+            sjd.sjd_kv_append(pool.pages, sjd.Windows(whole, tt, sum(m), max(m), 0),
+                              *(torch.cat([p[i] for p in past]).cuda() for i in range(2)))
+
+        def step(e):
+            x, c = io[e]["qkv"], io[e]
+            q, k, v = (x[:, a * hd:b * hd].view(T, b - a, hd) for a, b in ((0, H), (H, H + Hkv), (H + Hkv, H + 2 * Hkv)))
+            sjd.sjd_rope_axes(q, k, c["pos"], freq, axis)
+            sjd.sjd_kv_append(pools[e].pages, c["win"], k, v)
+            sjd.sjd_paged_attention(pools[e].pages, c["win"], q, c["out"], c["ws"], scale=hd ** -0.5)
+
+        step(0)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            step(0)
+        kept = [[p[0].double().numpy(), p[1].double().numpy()] for p in past]
+        val = lambda x: quantise(x)[0] if cache == "e4m3" else x  # noqa: E731
+        for i in range(steps):
+            x = torch.randn(T, (H + 2 * Hkv) * hd, generator=g).to(torch.bfloat16)
+            pos = torch.randint(0, 5000, (T, 3), generator=g, dtype=torch.int32)
+            for e in range(2):
+                io[e]["qkv"].copy_(x)
+                io[e]["pos"].copy_(pos)
+            graph.replay()
+            step(1)
+            torch.cuda.synchronize()
+            assert torch.equal(io[0]["out"], io[1]["out"]) and torch.equal(io[0]["qkv"], io[1]["qkv"])
+            assert torch.equal(pools[0].t, pools[1].t)
+            rot = io[1]["qkv"].double().cpu().numpy()
+            for z in range(B):
+                r = slice(rows * z, rows * z + rows)
+                q = rot[r, :H * hd].reshape(rows, H, hd)
+                kv = [rot[r, (H + a * Hkv) * hd:(H + a * Hkv + Hkv) * hd].reshape(rows, Hkv, hd) for a in (0, 1)]
+                kept[z] = [np.concatenate([o, n]) for o, n in zip(kept[z], kv)]
+                n = len(kept[z][0])
+                seen = np.arange(n)[None] - (n - rows) <= np.arange(rows)[:, None]
+                for h in range(H):
+                    k, v = (val(y[:, h // G]) for y in kept[z])
+                    want, mag = attention(q[:, h], k, v, hd ** -0.5, seen)
+                    tol = attention_tolerance(q[:, h], k, hd ** -0.5, mag, want, n)
+                    assert (np.abs(io[1]["out"][r, h].double().cpu().numpy() - want) <= tol).all(), (i, z, h)
+            for e in range(2):
+                io[e]["win"].seq[:, 2] += rows
