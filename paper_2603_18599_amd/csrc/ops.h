@@ -47,10 +47,18 @@ __device__ __forceinline__ Seq load_seq(const sjd_windows& w, const PoolView& pv
   if (!ok) s.rows = 0;
   return s;
 }
-// Start of the page that holds position p of sequence z, or NULL
-__device__ __forceinline__ char* page_of(const sjd_windows& w, const PoolView& pv, int z, int p) {
-  const int id = w.d_table[(int64_t)z * w.table_len + (p >> pv.plen_log2)];
+// Page id of position p of sequence z (scalar load: the table does not change
+// during a call, and every caller asks for one position per wave), and the start of
+// a page, NULL for an id outside the pool
+__device__ __forceinline__ int page_id(const sjd_windows& w, const PoolView& pv, int z, int p) {
+  const auto* t = (const int32_t __attribute__((address_space(4)))*)w.d_table;
+  return __builtin_amdgcn_readfirstlane(t[(int64_t)z * w.table_len + (p >> pv.plen_log2)]);
+}
+__device__ __forceinline__ char* page_at(const PoolView& pv, int id) {
   return (uint32_t)id < (uint32_t)pv.n_pages ? pv.pool + (int64_t)id * pv.page_bytes : nullptr;
+}
+__device__ __forceinline__ char* page_of(const sjd_windows& w, const PoolView& pv, int z, int p) {
+  return page_at(pv, page_id(w, pv, z, p));
 }
 // Byte offsets inside a page, head h: the tile of position `in` (of the page), and
 // the exponent bytes of the page's positions 0 ..
@@ -71,6 +79,7 @@ hipError_t launch_kv_read(const sjd_pages& p, const sjd_windows& w, const sjd_kv
 struct AttnPlan {
   int chunk;   // keys per split, a multiple of the workgroup's keys per round
   int splits;  // most splits of a sequence
+  bool few;    // few slots per window: waves split the keys, not the slots
 };
 AttnPlan paged_attention_plan(const sjd_pages& p, const sjd_windows& w, int H);
 int64_t paged_attention_ws(const sjd_pages& p, const sjd_windows& w, int H);

@@ -8,7 +8,10 @@
 // V^T . P^T takes them in, so they never leave registers (v_mfma_f32_32x32x16_bf16).
 // e4m3 codes become bf16 without rounding, times the key's power of two (an operand
 // of the conversion); a value row's power multiplies its probability.
+#include <cmath>
+
 #include "device.h"
+#include "forward.h"
 #include "ops.h"
 
 namespace sjd {
@@ -28,7 +31,8 @@ struct PagedArgs {
   int64_t q_row, out_row;
   const uint64_t* anc;
   int H, G;
-  float scale;  // times log2(e)
+  float scale;  // |scale| * log2(e);
+  int negate;   // scale < 0: q changes sign
   int chunk, splits;
   float* ws_o;  // [splits][T][H][HD] unnormalised outputs (splits > 1)
   float* ws_ml; // [splits][T][H][2] maximum (log2 domain), sum
@@ -47,87 +51,86 @@ SJD_DEV bf16x8 bf16_of_e4m3(uint2 c, float scale) {
                                                pk_bf16_of_e4m3<false>(c.y, scale), pk_bf16_of_e4m3<true>(c.y, scale)));
 }
 
-// One lane's part of a 32-position tile as it lies in memory
+// One lane's part of a 32-position tile as it lies in memory, as a source of MFMA
+// operands: key(t), 8 dims of a key row (step t); val(d, jj), 8 positions from 16 jj
+// of a value column (dims block d).
 template <int HD, bool FP8>
 struct RawTile {
   static constexpr int NK = FP8 ? HD / 32 : HD / 16;  // 16-byte pieces of keys, and of values
+  static constexpr bool kScaled = FP8;                // values lack their rows' powers of two
   uint4 k[NK], v[NK];
-  uint32_t ke;   // e4m3: exponent byte of the lane's key row,
-  uint2 ve[2];   // and of the 16 positions that its score registers hold
+  uint32_t ke;  // e4m3: exponent byte of the lane's key row,
+  uint2 ve[2];  // and of the 16 positions that its score registers hold
+
+  // positions p0 .. p0 + 31 of a page's head
+  SJD_DEV void load(const PagedArgs& a, const char* page, int h, int p0) {
+    constexpr int ES = FP8 ? 1 : 2;
+    const int in = p0 & ((1 << a.pv.plen_log2) - 1), lane = threadIdx.x & 63;
+    const uint4* kp = (const uint4*)(page + tile_off<HD, ES>(a.pv, h, in, 0)) + lane;
+    const uint4* vp = (const uint4*)(page + tile_off<HD, ES>(a.pv, h, in, 1)) + lane;
+#pragma unroll
+    for (int i = 0; i < NK; ++i) k[i] = kp[64 * i];
+#pragma unroll
+    for (int i = 0; i < NK; ++i) v[i] = vp[64 * i];
+    if constexpr (FP8) {
+      // a lane's MFMA key row is position swap23(lane % 32); its score registers 8 jj
+      // + e hold positions 16 jj + 8 half + e
+      ke = (uint8_t)page[exp_off<HD>(a.pv, h, 0) + in + swap23(lane & 31)];
+      const char* e = page + exp_off<HD>(a.pv, h, 1) + in + 8 * (lane >> 5);
+      ve[0] = *(const uint2*)e;
+      ve[1] = *(const uint2*)(e + 16);
+    }
+  }
+  SJD_DEV bf16x8 key(int t) const {
+    if constexpr (FP8) {
+      const uint4 x = k[t >> 1];
+      return bf16_of_e4m3(t & 1 ? make_uint2(x.z, x.w) : make_uint2(x.x, x.y), __uint_as_float(ke << 23));
+    } else {
+      return __builtin_bit_cast(bf16x8, k[t]);
+    }
+  }
+  SJD_DEV bf16x8 val(int d, int jj) const {
+    if constexpr (FP8) {
+      const uint4 x = v[d];
+      return bf16_of_e4m3(jj ? make_uint2(x.z, x.w) : make_uint2(x.x, x.y), 1.0f);
+    } else {
+      return __builtin_bit_cast(bf16x8, v[d * 2 + jj]);
+    }
+  }
+  SJD_DEV float power(int i) const {  // of score register i's value row
+    const uint32_t w = (i & 7) < 4 ? ve[i >> 3].x : ve[i >> 3].y;
+    return __uint_as_float(((w >> (8 * (i & 3))) & 0xFFu) << 23);
+  }
 };
 
-// MFMA operand of 8 dims of a key row (step t), of 8 positions of a value column
-// (dims block d, positions 16 jj ..)
-template <int HD, bool FP8>
-SJD_DEV bf16x8 key_frag(const RawTile<HD, FP8>& r, int t, float ks) {
-  if constexpr (FP8) {
-    const uint4 x = r.k[t >> 1];
-    return bf16_of_e4m3(t & 1 ? make_uint2(x.z, x.w) : make_uint2(x.x, x.y), ks);
-  } else {
-    return __builtin_bit_cast(bf16x8, r.k[t]);
+// The same of a tile in LDS, widened to bf16: [key steps, then value blocks][lane]
+template <int HD>
+struct LdsTile {
+  static constexpr bool kScaled = false;
+  const uint4* at;
+  SJD_DEV bf16x8 key(int t) const { return __builtin_bit_cast(bf16x8, at[64 * t + (threadIdx.x & 63)]); }
+  SJD_DEV bf16x8 val(int d, int jj) const {
+    return __builtin_bit_cast(bf16x8, at[64 * (HD / 16 + 2 * d + jj) + (threadIdx.x & 63)]);
   }
-}
-template <int HD, bool FP8>
-SJD_DEV bf16x8 val_frag(const RawTile<HD, FP8>& r, int d, int jj) {
-  if constexpr (FP8) {
-    const uint4 x = r.v[d];
-    return bf16_of_e4m3(jj ? make_uint2(x.z, x.w) : make_uint2(x.x, x.y), 1.0f);
-  } else {
-    return __builtin_bit_cast(bf16x8, r.v[d * 2 + jj]);
+  SJD_DEV float power(int) const { return 1.0f; }
+};
+
+// Value operand with the positions from `lim` on cleared; bad: whether another
+// element is not finite
+SJD_DEV bf16x8 clear_from(bf16x8 v, int pos, int lim, bool& bad) {
+  uint4 u = __builtin_bit_cast(uint4, v);
+  uint32_t* w = (uint32_t*)&u;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    if (pos + 2 * e >= lim) w[e] &= ~0xFFFFu;
+    if (pos + 2 * e + 1 >= lim) w[e] &= 0xFFFFu;
+    bad |= (w[e] & 0x7F80u) == 0x7F80u || (w[e] & 0x7F800000u) == 0x7F800000u;
   }
+  return __builtin_bit_cast(bf16x8, u);
 }
 
-// Loads the tile of positions p0 .. p0 + 31 (page: its page)
-template <int HD, bool FP8>
-SJD_DEV void load_tile(RawTile<HD, FP8>& r, const PagedArgs& a, const char* page, int h, int p0) {
-  constexpr int ES = FP8 ? 1 : 2;
-  const int in = p0 & ((1 << a.pv.plen_log2) - 1), lane = threadIdx.x & 63;
-  const uint4* k = (const uint4*)(page + tile_off<HD, ES>(a.pv, h, in, 0)) + lane;
-  const uint4* v = (const uint4*)(page + tile_off<HD, ES>(a.pv, h, in, 1)) + lane;
-#pragma unroll
-  for (int i = 0; i < RawTile<HD, FP8>::NK; ++i) r.k[i] = k[64 * i];
-#pragma unroll
-  for (int i = 0; i < RawTile<HD, FP8>::NK; ++i) r.v[i] = v[64 * i];
-  if constexpr (FP8) {
-    // a lane's MFMA key row is position swap23(lane % 32); its score registers 8 jj
-    // + e hold positions 16 jj + 8 half + e
-    const int i = lane & 31, sw = (i & ~12) | ((i & 4) << 1) | ((i & 8) >> 1);
-    r.ke = (uint8_t)page[exp_off<HD>(a.pv, h, 0) + in + sw];
-    const char* e = page + exp_off<HD>(a.pv, h, 1) + in + 8 * (lane >> 5);
-    r.ve[0] = *(const uint2*)e;
-    r.ve[1] = *(const uint2*)(e + 16);
-  }
-}
-
-// Clears the values of positions from `lim` of the tile on, and says whether any
-// other value of this lane is not finite
-template <int HD, bool FP8>
-SJD_DEV bool clean_values(RawTile<HD, FP8>& r, int lim) {
-  const int half = (threadIdx.x & 63) >> 5;
-  bool bad = false;
-  auto fix = [&](uint32_t w, int pos) {  // 4 codes or 2 bf16 from position pos on
-    constexpr int PER = FP8 ? 4 : 2, BITS = 32 / PER;
-#pragma unroll
-    for (int e = 0; e < PER; ++e) {
-      const uint32_t m = (FP8 ? 0xFFu : 0xFFFFu) << (BITS * e);
-      if (pos + e >= lim) w &= ~m;
-      const uint32_t x = (w >> (BITS * e)) & (FP8 ? 0x7Fu : 0x7F80u);
-      bad |= x == (FP8 ? 0x7Fu : 0x7F80u);
-    }
-    return w;
-  };
-#pragma unroll
-  for (int i = 0; i < RawTile<HD, FP8>::NK; ++i) {
-    const int p = 8 * half + (FP8 ? 0 : 16 * (i & 1));
-    r.v[i].x = fix(r.v[i].x, p);
-    r.v[i].y = fix(r.v[i].y, p + (FP8 ? 4 : 2));
-    r.v[i].z = fix(r.v[i].z, p + (FP8 ? 16 : 4));
-    r.v[i].w = fix(r.v[i].w, p + (FP8 ? 20 : 6));
-  }
-  return bad;
-}
-
-// One wave's state: 32 slots
+// One wave's state: 32 slots. m is the reference that probabilities are relative
+// to: the largest score when it was last moved (log2 domain).
 template <int HD>
 struct WaveState {
   bf16x8 q[HD / 16];
@@ -135,108 +138,154 @@ struct WaveState {
   float m, l;
 };
 
-// Bit r of a lane's mask: its score register r is visible
-template <int HD, bool FP8, bool MASKED>
-SJD_DEV void attend_tile(WaveState<HD>& s, RawTile<HD, FP8>& r, float scale, uint32_t vis, int lim) {
+// The reference moves only when a score exceeds it by kLag: probabilities up to 2^8
+// lose nothing (bf16 and float are relative), and most tiles skip the rescaling
+// of HD / 2 output registers.
+constexpr float kLag = 8.0f;
+
+// N tiles of 32 keys. vis[n]: bit i says that score register i is visible; lim[n]:
+// positions of the tile that hold anything.
+template <int HD, int N, bool MASKED, class Tile>
+SJD_DEV void attend(WaveState<HD>& s, const Tile (&tile)[N], float scale, const uint32_t (&vis)[N], const int (&lim)[N]) {
   constexpr int ND = HD / 32;
-  f32x16 c;
-#pragma unroll
-  for (int i = 0; i < 16; ++i) c[i] = 0.0f;
-  const float ks = FP8 ? __uint_as_float(r.ke << 23) : 1.0f;
-#pragma unroll
-  for (int t = 0; t < HD / 16; ++t)
-    c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(key_frag<HD, FP8>(r, t, ks), s.q[t], c, 0, 0, 0);
+  f32x16 c[N];
   float mx = -INFINITY;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    c[i] = !MASKED || ((vis >> i) & 1) ? c[i] * scale : -INFINITY;
-    mx = fmaxf(mx, c[i]);
-  }
-  mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
-  const float m = fmaxf(s.m, mx), base = m == -INFINITY ? 0.0f : m;
-  const float alpha = __builtin_amdgcn_exp2f(s.m - base);
-  s.m = m;
-  float sum = 0.0f;
+  for (int n = 0; n < N; ++n) {
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    c[i] = __builtin_amdgcn_exp2f(c[i] - base);
-    sum += c[i];
-  }
-  s.l = s.l * alpha + sum;
+    for (int i = 0; i < 16; ++i) c[n][i] = 0.0f;
 #pragma unroll
-  for (int d = 0; d < ND; ++d)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) s.o[d][i] *= alpha;
-  if constexpr (FP8) {
+    for (int t = 0; t < HD / 16; ++t) c[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tile[n].key(t), s.q[t], c[n], 0, 0, 0);
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      const uint32_t w = (i & 7) < 4 ? r.ve[i >> 3].x : r.ve[i >> 3].y;
-      const float f = __uint_as_float(((w >> (8 * (i & 3))) & 0xFFu) << 23);
-      // (a masked position's exponent may be anything)
-      c[i] = MASKED && !((vis >> i) & 1) ? 0.0f : c[i] * f;
+      if (MASKED) c[n][i] = (vis[n] >> i) & 1 ? c[n][i] : -INFINITY;
+      mx = fmaxf(mx, c[n][i]);
     }
   }
-  bf16x8 p[2];
+  mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
+  mx = mx == -INFINITY ? mx : mx * scale;
+  const bool move = mx > s.m + kLag;
+  if (__any(move)) {
+    // (each slot by itself: what its wave's other slots hold changes no bit of it)
+    const float alpha = move ? __builtin_amdgcn_exp2f(s.m - mx) : 1.0f;
+    s.m = move ? mx : s.m;
+    s.l *= alpha;
 #pragma unroll
-  for (int jj = 0; jj < 2; ++jj)
-    p[jj] = __builtin_bit_cast(bf16x8, make_uint4(pk_bf16(c[8 * jj], c[8 * jj + 1]), pk_bf16(c[8 * jj + 2], c[8 * jj + 3]),
-                                                  pk_bf16(c[8 * jj + 4], c[8 * jj + 5]),
-                                                  pk_bf16(c[8 * jj + 6], c[8 * jj + 7])));
-  if constexpr (MASKED) {
-    if (__any(clean_values<HD, FP8>(r, lim))) {
-      // A value that is not finite: 0 * it would reach slots that do not attend
-      // to its position. It is taken out, and each slot that attends to one of its
-      // kind gets one added.
-      auto kind_of = [](float x) { return x != x ? 2 : x == INFINITY ? 0 : x == -INFINITY ? 1 : 3; };
-      bf16x8 see[2];
+    for (int d = 0; d < ND; ++d)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) see[i >> 3][i & 7] = (__bf16)((vis >> i) & 1 ? 1.0f : 0.0f);
+      for (int i = 0; i < 16; ++i) s.o[d][i] *= alpha;
+  }
+  const float base = s.m == -INFINITY ? 0.0f : s.m;
+  bf16x8 p[N][2];
 #pragma unroll
-      for (int d = 0; d < ND; ++d) {
+  for (int n = 0; n < N; ++n) {
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(c[n][i], scale, -base));
+      // (a masked position may hold anything, its exponent byte too)
+      c[n][i] = MASKED && !((vis[n] >> i) & 1) ? 0.0f : e;
+      sum += c[n][i];
+    }
+    s.l += sum;
+    if constexpr (Tile::kScaled) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) c[n][i] = MASKED && !((vis[n] >> i) & 1) ? 0.0f : c[n][i] * tile[n].power(i);
+    }
+#pragma unroll
+    for (int jj = 0; jj < 2; ++jj)
+      p[n][jj] = __builtin_bit_cast(
+          bf16x8, make_uint4(pk_bf16(c[n][8 * jj], c[n][8 * jj + 1]), pk_bf16(c[n][8 * jj + 2], c[n][8 * jj + 3]),
+                             pk_bf16(c[n][8 * jj + 4], c[n][8 * jj + 5]), pk_bf16(c[n][8 * jj + 6], c[n][8 * jj + 7])));
+  }
+  const int half = (threadIdx.x & 63) >> 5;
+#pragma unroll
+  for (int n = 0; n < N; ++n)
+#pragma unroll
+    for (int d = 0; d < ND; ++d) {
+      bf16x8 v[2];
+      bool bad = false;
+#pragma unroll
+      for (int jj = 0; jj < 2; ++jj) {
+        v[jj] = tile[n].val(d, jj);
+        if (MASKED) v[jj] = clear_from(v[jj], 16 * jj + 8 * half, lim[n], bad);
+      }
+      if (MASKED && __any(bad)) {
+        // A value that is not finite: 0 * it would reach slots that do not attend
+        // to its position. It is taken out, and each slot that attends to one of
+        // its kind gets one added.
+        auto kind_of = [](float x) { return x != x ? 2 : x == INFINITY ? 0 : x == -INFINITY ? 1 : 3; };
         for (int kind = 0; kind < 3; ++kind) {
-          f32x16 n;
+          f32x16 cnt;
 #pragma unroll
-          for (int i = 0; i < 16; ++i) n[i] = 0.0f;
+          for (int i = 0; i < 16; ++i) cnt[i] = 0.0f;
 #pragma unroll
           for (int jj = 0; jj < 2; ++jj) {
-            const bf16x8 v = val_frag<HD, FP8>(r, d, jj);
-            bf16x8 w;
+            bf16x8 w, see;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) w[e] = (__bf16)(kind_of((float)v[e]) == kind ? 1.0f : 0.0f);
-            n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w, see[jj], n, 0, 0, 0);
+            for (int e = 0; e < 8; ++e) {
+              w[e] = (__bf16)(kind_of((float)v[jj][e]) == kind ? 1.0f : 0.0f);
+              see[e] = (__bf16)((vis[n] >> (8 * jj + e)) & 1 ? 1.0f : 0.0f);
+            }
+            cnt = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w, see, cnt, 0, 0, 0);
           }
           const float add = kind == 0 ? INFINITY : kind == 1 ? -INFINITY : __builtin_nanf("");
 #pragma unroll
-          for (int i = 0; i < 16; ++i) s.o[d][i] += n[i] > 0.0f ? add : 0.0f;
+          for (int i = 0; i < 16; ++i) s.o[d][i] += cnt[i] > 0.0f ? add : 0.0f;
         }
 #pragma unroll
-        for (int jj = 0; jj < 2; ++jj) {
-          bf16x8 v = val_frag<HD, FP8>(r, d, jj);
+        for (int jj = 0; jj < 2; ++jj)
 #pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = kind_of((float)v[e]) == 3 ? v[e] : (__bf16)0.0f;
-          s.o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p[jj], s.o[d], 0, 0, 0);
-        }
+          for (int e = 0; e < 8; ++e) v[jj][e] = kind_of((float)v[jj][e]) == 3 ? v[jj][e] : (__bf16)0.0f;
       }
-      return;
+#pragma unroll
+      for (int jj = 0; jj < 2; ++jj) s.o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[jj], p[n][jj], s.o[d], 0, 0, 0);
     }
-  }
-#pragma unroll
-  for (int d = 0; d < ND; ++d)
-#pragma unroll
-    for (int jj = 0; jj < 2; ++jj)
-      s.o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(val_frag<HD, FP8>(r, d, jj), p[jj], s.o[d], 0, 0, 0);
 }
 
-// Visible score registers of a lane whose slot is window row `row` (ok: there is
-// such a row), for the tile of positions p0 ..
-SJD_DEV uint32_t visible(const Seq& sq, int p0, int row, bool ok, const uint64_t* anc, uint64_t mask) {
+// A lane's slot: row f / G of the window, query head f % G of the group
+struct Slot {
+  int row, head;
+  bool ok;
+  int64_t t;  // row of the tensors
+  uint64_t mask;
+};
+SJD_DEV Slot slot_of(const PagedArgs& a, const Seq& sq, int h, int f) {
+  Slot s;
+  s.ok = f < sq.rows * a.G;
+  s.row = f / a.G;
+  s.head = h * a.G + f % a.G;
+  s.t = sq.row0 + (s.ok ? s.row : 0);
+  s.mask = a.anc && s.ok ? a.anc[s.t] : 0;
+  return s;
+}
+template <int HD>
+SJD_DEV void start(WaveState<HD>& s, const PagedArgs& a, const Slot& sl) {
+  const int half = (threadIdx.x & 63) >> 5;
+  const uint4* q = (const uint4*)(a.q + sl.t * a.q_row + (sl.ok ? sl.head : 0) * HD + half * (HD / 2));
+  const uint32_t sign = a.negate ? 0x80008000u : 0u;
+#pragma unroll
+  for (int i = 0; i < HD / 16; ++i) {
+    const uint4 x = sl.ok ? q[i] : make_uint4(0, 0, 0, 0);
+    s.q[i] = __builtin_bit_cast(bf16x8, make_uint4(x.x ^ sign, x.y ^ sign, x.z ^ sign, x.w ^ sign));
+  }
+#pragma unroll
+  for (int d = 0; d < HD / 32; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s.o[d][i] = 0.0f;
+  s.m = -INFINITY;
+  s.l = 0.0f;
+}
+
+// Visible score registers of a lane with slot sl, for the tile of positions p0 ..
+SJD_DEV uint32_t visible(const PagedArgs& a, const Seq& sq, int p0, const Slot& sl) {
   const int half = (threadIdx.x & 63) >> 5, nk = sq.cached + sq.rows;
   uint32_t v = 0;
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     const int p = p0 + 16 * (i >> 3) + 8 * half + (i & 7), w = p - sq.cached;
-    const bool see = p < nk && (w < 0 || (anc ? (mask >> (w & 63)) & 1 : w <= row));
-    v |= (uint32_t)(ok && see) << i;
+    const bool see = p < nk && (w < 0 || (a.anc ? (sl.mask >> (w & 63)) & 1 : w <= sl.row));
+    v |= (uint32_t)(sl.ok && see) << i;
   }
   return v;
 }
@@ -257,35 +306,28 @@ __global__ __launch_bounds__(256) void k_paged_attn(PagedArgs a) {
   const Seq sq = load_seq(a.w, a.pv, z);
   const int slots = sq.rows * a.G, f0 = blockIdx.y * 32;
   if (f0 >= slots) return;
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, half = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5;
   // causal: the last row of these slots bounds their keys
   const int last = min(sq.rows - 1, (f0 + 31) / a.G);
   const int nk = sq.cached + (a.anc ? sq.rows : last + 1);
   const int beg = sp * a.chunk, end = min(nk, beg + a.chunk);
   if (beg >= sq.cached + sq.rows) return;
-  const int f = f0 + (lane & 31), row = f / a.G, head = h * a.G + f % a.G;
-  const bool ok = f < slots;
-  const int64_t t = sq.row0 + (ok ? row : 0);
+  const Slot sl = slot_of(a, sq, h, f0 + (lane & 31));
   WaveState<HD> s;
-  {
-    const uint4* q = (const uint4*)(a.q + t * a.q_row + (ok ? head : 0) * HD + half * (HD / 2));
-#pragma unroll
-    for (int i = 0; i < HD / 16; ++i) s.q[i] = __builtin_bit_cast(bf16x8, ok ? q[i] : make_uint4(0, 0, 0, 0));
-  }
-  const uint64_t mask = a.anc && ok ? a.anc[t] : 0;
-#pragma unroll
-  for (int d = 0; d < ND; ++d)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) s.o[d][i] = 0.0f;
-  s.m = -INFINITY;
-  s.l = 0.0f;
+  start(s, a, sl);
   for (int p0 = beg + 32 * wave; p0 < end; p0 += 128) {
     const char* page = page_of(a.w, a.pv, z, p0);
     if (!page) continue;
-    RawTile<HD, FP8> r;
-    load_tile<HD, FP8>(r, a, page, h, p0);
-    if (p0 + 32 <= sq.cached) attend_tile<HD, FP8, false>(s, r, a.scale, 0xFFFFu, 32);
-    else attend_tile<HD, FP8, true>(s, r, a.scale, visible(sq, p0, row, ok, a.anc, mask), sq.cached + sq.rows - p0);
+    RawTile<HD, FP8> r[1];
+    r[0].load(a, page, h, p0);
+    const int lim[1] = {sq.cached + sq.rows - p0};
+    if (p0 + 32 <= sq.cached) {
+      const uint32_t vis[1] = {0xFFFFu};
+      attend<HD, 1, false>(s, r, a.scale, vis, lim);
+    } else {
+      const uint32_t vis[1] = {visible(a, sq, p0, sl)};
+      attend<HD, 1, true>(s, r, a.scale, vis, lim);
+    }
   }
   s.l += __shfl_xor(s.l, 32, kWave);
   // register i of block d holds dim 32 d + 8 (i / 4) + 4 half + i % 4
@@ -299,17 +341,17 @@ __global__ __launch_bounds__(256) void k_paged_attn(PagedArgs a) {
   }
   __syncthreads();
   constexpr int DPT = HD / 8;
-  const int sl = threadIdx.x >> 3, d0 = (threadIdx.x & 7) * DPT;
-  const int g = f0 + sl;
+  const int sn = threadIdx.x >> 3, d0 = (threadIdx.x & 7) * DPT;
+  const int g = f0 + sn;
   if (g >= slots) return;
   float mx = -INFINITY;
-  for (int w = 0; w < 4; ++w) mx = fmaxf(mx, sm.m[w][sl]);
+  for (int w = 0; w < 4; ++w) mx = fmaxf(mx, sm.m[w][sn]);
   float v[DPT] = {}, l = 0.0f;
   for (int w = 0; w < 4; ++w) {
-    const float fw = mx == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(sm.m[w][sl] - mx);
-    l += sm.l[w][sl] * fw;
+    const float fw = mx == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(sm.m[w][sn] - mx);
+    l += sm.l[w][sn] * fw;
 #pragma unroll
-    for (int i = 0; i < DPT; ++i) v[i] += sm.o[w][sl][d0 + i] * fw;
+    for (int i = 0; i < DPT; ++i) v[i] += sm.o[w][sn][d0 + i] * fw;
   }
   const int64_t tt = sq.row0 + g / a.G;
   const int hh = h * a.G + g % a.G;
@@ -327,6 +369,195 @@ __global__ __launch_bounds__(256) void k_paged_attn(PagedArgs a) {
   for (int i = 0; i < DPT; i += 4)
     *(float4*)(a.ws_o + at * HD + d0 + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
   if ((threadIdx.x & 7) == 0) *(float2*)(a.ws_ml + at * 2) = make_float2(mx, l);
+}
+
+// Many slots: 128 of them per workgroup, 32 per wave, and every wave takes every
+// key. Steps of 64 keys pass through LDS, widened to bf16 by the threads that load
+// them (once for the four waves), in two buffers: a step's loads are issued before
+// the arithmetic of the step before it and stored behind it.
+constexpr int kStep = 64, kStepTiles = kStep / kTile;
+
+template <int HD, bool FP8>
+struct Stage {
+  static constexpr int HP = FP8 ? HD * 2 : HD * 4;     // 16-byte pieces of a tile's keys
+  static constexpr int N = kStepTiles * 2 * HP / 256;  // pieces per thread
+  static constexpr int TILE = 2 * (HD / 16) * 64;      // uint4 of a tile in LDS
+  uint4 x[FP8 ? N : 1];
+  uint2 e[FP8 ? N : 1][2];  // exponent bytes: a key row's, or those of 16 positions
+  // piece i of this thread: tile, key or value, place in its part
+  static SJD_DEV void where(int i, int& tile, int& kv, int& u) {
+    static_assert(2 * HP % 256 == 0, "a round of the workgroup stays inside a tile");
+    const int tid = (int)threadIdx.x, n = i * 256;
+    tile = n / (2 * HP);
+    kv = HP >= 256 ? n / HP & 1 : __builtin_amdgcn_readfirstlane(tid / HP);
+    u = HP >= 256 ? n % HP + tid : tid % HP;
+  }
+  // Starts the loads of positions p0 .. (a page that is NULL: its tile is not read;
+  // nor is what LDS holds there used)
+  SJD_DEV void load(const PagedArgs& a, const char* const (&page)[kStepTiles], int h, int p0, uint4* lds) {
+    constexpr int ES = FP8 ? 1 : 2;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      int tile, kv, u;
+      where(i, tile, kv, u);
+      const char* pg = tile ? page[1] : page[0];
+      if (!pg) continue;
+      const int in = (p0 + 32 * tile) & ((1 << a.pv.plen_log2) - 1);
+      const uint4* src = (const uint4*)(pg + tile_off<HD, ES>(a.pv, h, in, kv)) + u;
+      if constexpr (FP8) {
+        x[i] = *src;
+        const char* ep = pg + exp_off<HD>(a.pv, h, kv) + in;
+        if (kv) {
+          e[i][0] = *(const uint2*)(ep + 8 * ((u & 63) >> 5));
+          e[i][1] = *(const uint2*)(ep + 16 + 8 * ((u & 63) >> 5));
+        } else {
+          e[i][0].x = (uint8_t)ep[swap23(u & 31)];
+        }
+      } else {
+        // a wave's 1 KB lands in lane order behind a uniform address
+        uint4* d = lds + tile * TILE + kv * (TILE / 2) + (u & ~63);
+        __builtin_amdgcn_global_load_lds((const void __attribute__((address_space(1)))*)src,
+                                         (void __attribute__((address_space(3)))*)d, 16, 0, 0);
+      }
+    }
+  }
+  // Ends them: what was loaded is in LDS (of this wave's pieces)
+  SJD_DEV void store(uint4* lds) const {
+    if constexpr (!FP8) {
+      __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        int tile, kv, u;
+        where(i, tile, kv, u);
+        uint4* d = lds + tile * TILE + kv * (TILE / 2) + (u >> 6) * 128 + (u & 63);
+        if (kv) {
+          d[0] = widen(make_uint2(x[i].x, x[i].y), e[i][0]);
+          d[64] = widen(make_uint2(x[i].z, x[i].w), e[i][1]);
+        } else {
+          const float f = __uint_as_float(e[i][0].x << 23);
+          d[0] = __builtin_bit_cast(uint4, bf16_of_e4m3(make_uint2(x[i].x, x[i].y), f));
+          d[64] = __builtin_bit_cast(uint4, bf16_of_e4m3(make_uint2(x[i].z, x[i].w), f));
+        }
+      }
+    }
+  }
+  // 8 codes, each with its own exponent byte
+  static SJD_DEV uint4 widen(uint2 c, uint2 e) {
+    uint32_t w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t cc = j < 2 ? c.x : c.y, ee = (j < 2 ? e.x : e.y) >> (16 * (j & 1));
+      const f32x2 v = j & 1 ? __builtin_amdgcn_cvt_pk_f32_fp8((int)cc, true) : __builtin_amdgcn_cvt_pk_f32_fp8((int)cc, false);
+      w[j] = pk_bf16(v[0] * __uint_as_float((ee & 0xFFu) << 23), v[1] * __uint_as_float((ee >> 8 & 0xFFu) << 23));
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+};
+
+template <int HD, bool FP8>
+__global__ __launch_bounds__(256, 2) void k_paged_chunk(PagedArgs a) {
+  constexpr int ND = HD / 32;
+  using St = Stage<HD, FP8>;
+  __shared__ uint4 lds[2][kStepTiles * St::TILE];
+  const int h = blockIdx.x % a.pv.Hkv, sp = blockIdx.x / a.pv.Hkv, z = blockIdx.z;
+  const Seq sq = load_seq(a.w, a.pv, z);
+  // (the last slots of a causal window have the most keys: they start first)
+  const int slots = sq.rows * a.G, f0 = ((int)gridDim.y - 1 - (int)blockIdx.y) * 128;
+  if (f0 >= slots) return;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5;
+  const int total = sq.cached + sq.rows;
+  const int nk = a.anc ? total : sq.cached + min(sq.rows - 1, (f0 + 127) / a.G) + 1;
+  const int beg = sp * a.chunk, end = min(nk, beg + a.chunk);
+  if (beg >= total) return;
+  const int w0 = f0 + 32 * wave;
+  const Slot sl = slot_of(a, sq, h, w0 + (lane & 31));
+  WaveState<HD> s;
+  start(s, a, sl);
+  // keys that every slot of the workgroup sees, and that any slot of this wave sees
+  const int all = a.anc ? sq.cached : sq.cached + f0 / a.G + 1;
+  const int any = w0 >= slots ? 0 : a.anc ? total : sq.cached + min(sq.rows - 1, (w0 + 31) / a.G) + 1;
+
+  // page ids are read two steps ahead of their use, loads of the pages one
+  auto ids = [&](int p0, int (&id)[kStepTiles]) {
+#pragma unroll
+    for (int n = 0; n < kStepTiles; ++n) id[n] = p0 + 32 * n < end ? page_id(a.w, a.pv, z, p0 + 32 * n) : -1;
+  };
+  auto pages = [&](const int (&id)[kStepTiles], const char* (&pg)[kStepTiles]) {
+#pragma unroll
+    for (int n = 0; n < kStepTiles; ++n) pg[n] = page_at(a.pv, id[n]);
+  };
+  St st;
+  const char* pg[kStepTiles];
+  int id[kStepTiles];
+  ids(beg, id);
+  pages(id, pg);
+  ids(beg + kStep, id);
+  st.load(a, pg, h, beg, lds[0]);
+  st.store(lds[0]);
+  __syncthreads();
+  int buf = 0, p0 = beg;
+  // One step: the next one's loads, `work` on this one, and the loads' end
+  auto step = [&](auto work) {
+    const char* next[kStepTiles];
+    const bool more = p0 + kStep < end;
+    if (more) {
+      pages(id, next);
+      ids(p0 + 2 * kStep, id);
+      st.load(a, next, h, p0 + kStep, lds[buf ^ 1]);
+    }
+    work();
+    if (more) {
+      st.store(lds[buf ^ 1]);
+      pg[0] = next[0];
+      pg[1] = next[1];
+    }
+    __syncthreads();
+    buf ^= 1;
+    p0 += kStep;
+  };
+  // keys without a mask (in a loop of its own: it needs fewer registers), then the rest
+  while (p0 + kStep <= min(all, end) && pg[0] && pg[1])
+    step([&] {
+      const LdsTile<HD> t[kStepTiles] = {{lds[buf]}, {lds[buf] + St::TILE}};
+      const uint32_t vis[kStepTiles] = {0xFFFFu, 0xFFFFu};
+      const int lim[kStepTiles] = {32, 32};
+      attend<HD, kStepTiles, false>(s, t, a.scale, vis, lim);
+    });
+  while (p0 < end)
+    step([&] {
+#pragma unroll 1
+      for (int n = 0; n < kStepTiles; ++n) {
+        const int p = p0 + 32 * n;
+        if (!pg[n] || p >= any) continue;
+        const LdsTile<HD> t[1] = {{lds[buf] + n * St::TILE}};
+        const uint32_t vis[1] = {visible(a, sq, p, sl)};
+        const int lim[1] = {total - p};
+        attend<HD, 1, true>(s, t, a.scale, vis, lim);
+      }
+    });
+  s.l += __shfl_xor(s.l, 32, kWave);
+  if (!sl.ok) return;
+  // register i of block d holds dim 32 d + 8 (i / 4) + 4 half + i % 4
+  if (a.splits == 1) {
+    const float inv = s.l == 0.0f ? 0.0f : 1.0f / s.l;  // (no key at all: zeros)
+    uint16_t* o = a.out + sl.t * a.out_row + sl.head * HD + 4 * half;
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; i += 4)
+        *(uint2*)(o + d * 32 + 2 * i) = make_uint2(pk_bf16(s.o[d][i] * inv, s.o[d][i + 1] * inv),
+                                                   pk_bf16(s.o[d][i + 2] * inv, s.o[d][i + 3] * inv));
+    return;
+  }
+  const int64_t at = ((int64_t)sp * a.w.T + sl.t) * a.H + sl.head;
+#pragma unroll
+  for (int d = 0; d < ND; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; i += 4)
+      *(float4*)(a.ws_o + at * HD + d * 32 + 2 * i + 4 * half) =
+          make_float4(s.o[d][i], s.o[d][i + 1], s.o[d][i + 2], s.o[d][i + 3]);
+  if (half == 0) *(float2*)(a.ws_ml + at * 2) = make_float2(s.m, s.l);
 }
 
 // Joins the splits of a row: one wave per (row, head).
@@ -357,20 +588,30 @@ __global__ __launch_bounds__(256) void k_paged_join(PagedArgs a) {
   else *o = (uint16_t)pk_bf16(v[0] * inv, 0.0f);
 }
 
+template <int HD, bool FP8>
+void launch_head(const PagedArgs& a, const AttnPlan& pl, dim3 grid, hipStream_t s) {
+  if (pl.few) hipLaunchKernelGGL((k_paged_attn<HD, FP8>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((k_paged_chunk<HD, FP8>), grid, dim3(256), 0, s, a);
+}
+
 }  // namespace
+
+// Few slots: every wave its own keys. More: keys shared by four waves of slots.
+constexpr int kFewSlots = 32;
 
 // Keys per split: one split where sequences, heads and slots fill the compute
 // units twice, else as many as do that, of 256 keys at least.
 AttnPlan paged_attention_plan(const sjd_pages& p, const sjd_windows& w, int H) {
   const int64_t most = (int64_t)w.max_cached + w.max_rows;
   const int64_t slots = (int64_t)w.max_rows * (H / p.n_kv_heads);
-  const int64_t wgs = (int64_t)w.B * p.n_kv_heads * ((slots + 31) / 32);
+  const bool few = slots <= kFewSlots;
+  const int64_t wgs = (int64_t)w.B * p.n_kv_heads * (few ? 1 : (slots + 127) / 128);
   int64_t S = wgs >= 512 ? 1 : (512 + wgs - 1) / wgs;
   const int64_t cap = (most + 255) / 256;
   if (S > cap) S = cap;
   if (S < 1) S = 1;
   const int64_t chunk = ((most + S - 1) / S + 127) / 128 * 128;
-  return AttnPlan{(int)chunk, (int)((most + chunk - 1) / chunk)};
+  return AttnPlan{(int)chunk, (int)((most + chunk - 1) / chunk), few};
 }
 
 int64_t paged_attention_ws(const sjd_pages& p, const sjd_windows& w, int H) {
@@ -385,19 +626,16 @@ hipError_t launch_paged_attention(const sjd_pages& p, const sjd_windows& w, cons
   PagedArgs a{};
   a.pv = pool_view(p); a.w = w; a.q = (const uint16_t*)io.d_q; a.out = (uint16_t*)io.d_out;
   a.q_row = io.q_row; a.out_row = io.out_row; a.anc = io.d_anc; a.H = io.H; a.G = io.H / p.n_kv_heads;
-  a.scale = (float)(1.4426950408889634 * (double)io.scale);
+  a.scale = (float)(1.4426950408889634 * std::fabs((double)io.scale));
+  a.negate = io.scale < 0.0f ? 1 : 0;
   a.chunk = pl.chunk; a.splits = pl.splits;
   a.ws_o = (float*)ws;
   a.ws_ml = ws ? (float*)ws + (int64_t)pl.splits * w.T * io.H * p.head_dim : nullptr;
-  const dim3 grid(p.n_kv_heads * pl.splits, (w.max_rows * a.G + 31) / 32, w.B);
+  const int slots = w.max_rows * a.G, per = pl.few ? 32 : 128;
+  const dim3 grid(p.n_kv_heads * pl.splits, (slots + per - 1) / per, w.B);
   const bool f8 = p.dtype == SJD_E4M3;
-  if (p.head_dim == 128) {
-    if (f8) hipLaunchKernelGGL((k_paged_attn<128, true>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((k_paged_attn<128, false>), grid, dim3(256), 0, s, a);
-  } else {
-    if (f8) hipLaunchKernelGGL((k_paged_attn<64, true>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((k_paged_attn<64, false>), grid, dim3(256), 0, s, a);
-  }
+  if (p.head_dim == 128) f8 ? launch_head<128, true>(a, pl, grid, s) : launch_head<128, false>(a, pl, grid, s);
+  else f8 ? launch_head<64, true>(a, pl, grid, s) : launch_head<64, false>(a, pl, grid, s);
   if (pl.splits > 1) {
     const dim3 jg((unsigned)(((int64_t)w.max_rows * io.H + 3) / 4), w.B);
     if (p.head_dim == 128) hipLaunchKernelGGL(k_paged_join<128>, jg, dim3(256), 0, s, a);
