@@ -3,11 +3,12 @@
 //
 // Bound by memory: only a row that is drawn from needs more than two of its
 // entries, and it needs p and q once. One workgroup takes a drawn row: each of 16
-// waves sums a contiguous stretch of it in 64 bits, the stretch that holds r *
-// total is summed again in 16 parts (it lies in the cache), and a wave finds the
-// token in its part. Differences and products of floats are exact or rounded
-// once in 64 bits, so another summation order moves a draw only where r * total
-// lies within some 1e-15 of the total from a border.
+// waves sums a contiguous stretch of it in 64 bits, with 8 16-byte loads per lane in
+// flight; the stretch that holds r * total is read again (it lies in the cache),
+// 4 entries to a lane, and a wave finds the token in its 256. Differences and
+// products of floats are exact or rounded once in 64 bits, so another summation
+// order moves a draw only where r * total lies within some 1e-15 of the total from
+// a border.
 #include "device.h"
 #include "ops.h"
 
@@ -24,85 +25,147 @@ struct GivenArgs {
 
 SJD_DEV double wave_sum64(double v) { return wave_sum_d_dpp(v); }
 
-// The weights of a row
+// The weights of a row. VEC: its entries start on 16 bytes
+template <bool VEC>
 struct Row {
   const float *p, *q;  // q NULL: p alone, but for entry `skip`
   int V, skip;
-  SJD_DEV double at(int x) const {
-    double d = p[x];
-    if (q) d -= (double)q[x];
-    else if (x == skip) d = 0.0;
+  SJD_DEV double weight(int x, float pv, float qv) const {
+    const double d = q ? (double)pv - (double)qv : x == skip ? 0.0 : (double)pv;
     return d > 0.0 ? d : 0.0;  // (NaN: 0)
+  }
+  // entries x .. x + 3, those from `end` on as zeros
+  SJD_DEV void four(int x, int end, float4& a, float4& b) const {
+    a = b = make_float4(0, 0, 0, 0);
+    if (VEC && x + 4 <= end) {
+      a = *(const float4*)(p + x);
+      if (q) b = *(const float4*)(q + x);
+    } else {
+      float* u = &a.x;
+      float* v = &b.x;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (x + i < end) {
+          u[i] = p[x + i];
+          if (q) v[i] = q[x + i];
+        }
+    }
+  }
+  SJD_DEV void weights(int x, const float4& a, const float4& b, double (&w)[4]) const {
+    w[0] = weight(x, a.x, b.x);
+    w[1] = weight(x + 1, a.y, b.y);
+    w[2] = weight(x + 2, a.z, b.z);
+    w[3] = weight(x + 3, a.w, b.w);
+  }
+  // sum over [lo, hi) by one wave
+  SJD_DEV double sum(int lo, int hi) const {
+    double s = 0.0;
+    for (int x0 = lo + 4 * (int)(threadIdx.x & 63); x0 < hi; x0 += 16 * kWave) {
+      float4 a[4], b[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) four(x0 + 4 * kWave * i, hi, a[i], b[i]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        double w[4];
+        weights(x0 + 4 * kWave * i, a[i], b[i], w);
+        s += (w[0] + w[1]) + (w[2] + w[3]);
+      }
+    }
+    return wave_sum64(s);
   }
 };
 
-// Sum of w over [lo, hi) by one wave, and the largest x with mass (-1: none)
-SJD_DEV double stretch_sum(const Row& w, int lo, int hi) {
-  double s = 0.0;
-  for (int x = lo + (threadIdx.x & 63); x < hi; x += kWave) s += w.at(x);
-  return wave_sum64(s);
-}
-
 struct DrawSmem {
-  double seg[kWaves];
+  double part[2][kWaves];
   int tok;
 };
 
 // Least x with cum(x) > r * total, or -1 for a row without mass (every thread
 // gets the result).
-SJD_DEV int draw(const Row& w, float r, DrawSmem& sm) {
+template <bool VEC>
+SJD_DEV int draw(const Row<VEC>& w, float r, DrawSmem& sm) {
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int seg = ((w.V + kWaves - 1) / kWaves + kWave - 1) / kWave * kWave;  // entries per wave
-  auto sums = [&](int base, int end, int len) {
-    const int lo = min(base + wave * len, end), hi = min(lo + len, end);
-    const double s = stretch_sum(w, lo, hi);
-    __syncthreads();  // (the last round's sums have been read)
-    if (lane == 0) sm.seg[wave] = s;
-    __syncthreads();
-  };
-  sums(0, w.V, seg);
-  double total = 0.0;
-  for (int i = 0; i < kWaves; ++i) total += sm.seg[i];
-  if (!(total > 0.0)) return -1;
-  const double target = (double)r * total;
-  // the part that holds the target: the first whose end lies above it, else
-  // (r * total rounded up to the total) the last one with mass
-  auto find = [&](double& before) {
-    double cum = before, at = before;
+  constexpr int kPart = 4 * kWave;  // entries of a wave in the last round
+  auto split = [](int len) { return ((len + kWaves - 1) / kWaves + kPart - 1) / kPart * kPart; };
+  int round = 0;
+  double target = 0.0, before = 0.0;
+  // The part that holds the target: the first whose end lies above it, else (r *
+  // total rounded up to the total) the last one with mass.
+  auto find = [&](const double* part) {
+    double cum = before, at = before, last_at = before;
     int pick = -1, last = 0;
-    double last_before = before;
     for (int i = 0; i < kWaves; ++i) {
-      const double s = sm.seg[i];
-      if (s > 0.0) { last = i; last_before = cum; }
-      if (pick < 0 && cum + s > target && s > 0.0) { pick = i; at = cum; }
+      const double s = part[i];
+      if (s > 0.0) {
+        last = i;
+        last_at = cum;
+        if (pick < 0 && cum + s > target) {
+          pick = i;
+          at = cum;
+        }
+      }
       cum += s;
     }
-    if (pick < 0) { pick = last; at = last_before; }
-    before = at;
-    return pick;
+    before = pick < 0 ? last_at : at;
+    return pick < 0 ? last : pick;
   };
-  double before = 0.0;
-  int base = find(before) * seg, end = min(base + seg, w.V), len = seg;
-  while (len > kWave) {
-    len = ((len + kWaves - 1) / kWaves + kWave - 1) / kWave * kWave;
-    sums(base, end, len);
-    base += find(before) * len;
-    end = min(base + len, end);
-  }
-  if (wave == 0) {  // at most 64 entries, in lane order
-    const int x = base + lane;
-    const double v = x < end ? w.at(x) : 0.0;
-    double cum = v;
-#pragma unroll
-    for (int o = 1; o < kWave; o <<= 1) {
-      const double u = __shfl_up(cum, o, kWave);
-      if (lane >= o) cum += u;
+  int base = 0, end = w.V, len = split(w.V);
+  // rounds of sums (two buffers: a round's sums are read while the next one writes
+  // its own, and the barrier between them is enough)
+  for (;; len = split(len)) {
+    const int lo = min(base + wave * len, end), hi = min(lo + len, end);
+    double* part = sm.part[round & 1];
+    double x[4], s;
+    if (len > kPart) {
+      s = w.sum(lo, hi);
+    } else {
+      float4 a, b;
+      const int at = lo + 4 * lane;
+      w.four(at, hi, a, b);
+      w.weights(at, a, b, x);
+      s = wave_sum64((x[0] + x[1]) + (x[2] + x[3]));
     }
-    const uint64_t above = __ballot(v > 0.0 && before + cum > target), some = __ballot(v > 0.0);
-    if (lane == 0) sm.tok = base + (above ? __builtin_ctzll(above) : 63 - __builtin_clzll(some));
+    if (lane == 0) part[wave] = s;
+    __syncthreads();
+    if (round++ == 0) {
+      double total = 0.0;
+      for (int i = 0; i < kWaves; ++i) total += part[i];
+      if (!(total > 0.0)) {
+        __syncthreads();  // (a draw that follows writes the same buffer)
+        return -1;
+      }
+      target = (double)r * total;
+    }
+    const int pick = find(part);
+    if (len > kPart) {
+      base += pick * len;
+      end = min(base + len, end);
+      continue;
+    }
+    if (wave == pick) {
+      const double own = (x[0] + x[1]) + (x[2] + x[3]);
+      double cum = own;
+#pragma unroll
+      for (int o = 1; o < kWave; o <<= 1) {
+        const double u = __shfl_up(cum, o, kWave);
+        if (lane >= o) cum += u;
+      }
+      const uint64_t above = __ballot(own > 0.0 && before + cum > target), some = __ballot(own > 0.0);
+      if (lane == (above ? __builtin_ctzll(above) : 63 - __builtin_clzll(some))) {
+        double c = before + (cum - own);
+        int t = -1, last = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          c += x[i];
+          if (x[i] > 0.0) last = i;
+          if (t < 0 && x[i] > 0.0 && c > target) t = i;
+        }
+        sm.tok = lo + 4 * lane + (t < 0 ? last : t);
+      }
+    }
+    __syncthreads();
+    return sm.tok;
   }
-  __syncthreads();
-  return sm.tok;
 }
 
 // Draft j of window b: accepted?  (*x: its entry, -1 if it is no token of the row)
@@ -120,8 +183,9 @@ SJD_DEV bool accepts(const GivenArgs& a, int b, int j, int* x) {
 }
 
 // Token drawn at row j (drafts: the residual; x < 0 or row n: p itself)
+template <bool VEC>
 SJD_DEV int draw_row(const GivenArgs& a, int b, int j, bool residual, int x, DrawSmem& sm) {
-  Row w{a.io.d_p + b * a.p.p_win + j * a.p.p_row, nullptr, a.p.V, -1};
+  Row<VEC> w{a.io.d_p + b * a.p.p_win + j * a.p.p_row, nullptr, a.p.V, -1};
   const float r = a.io.d_r[(int64_t)b * (a.p.L + 1) + j];
   int t = -1;
   if (residual) {
@@ -141,6 +205,7 @@ SJD_DEV int drafts_of(const GivenArgs& a, int b) {
 }
 
 // One window: up to its first rejection.
+template <bool VEC>
 __global__ __launch_bounds__(kThreads) void k_given_chain(GivenArgs a) {
   __shared__ DrawSmem sm;
   __shared__ int s_first, s_x;
@@ -162,7 +227,7 @@ __global__ __launch_bounds__(kThreads) void k_given_chain(GivenArgs a) {
   __syncthreads();
   const int first = s_first;
   const bool drawn = first < n || (a.p.flags & SJD_BONUS);
-  const int t = drawn ? draw_row(a, b, first, first < n && s_x >= 0, s_x, sm) : -1;
+  const int t = drawn ? draw_row<VEC>(a, b, first, first < n && s_x >= 0, s_x, sm) : -1;
   const int n_c = first + (drawn ? 1 : 0);
   if (j <= L)
     a.io.d_tok[(int64_t)b * (L + 1) + j] = j < first ? a.io.d_draft[(int64_t)b * L + j] : j < n_c ? t : -1;
@@ -172,6 +237,7 @@ __global__ __launch_bounds__(kThreads) void k_given_chain(GivenArgs a) {
 
 // Adaptive continuation: every row by itself, its token (the draft, or what was
 // drawn) into d_tok.
+template <bool VEC>
 __global__ __launch_bounds__(kThreads) void k_given_rows(GivenArgs a) {
   __shared__ DrawSmem sm;
   const int rows = a.p.L + (a.p.flags & SJD_BONUS ? 1 : 0);
@@ -179,7 +245,7 @@ __global__ __launch_bounds__(kThreads) void k_given_rows(GivenArgs a) {
   if (j > n || (j == n && rows == a.p.L)) return;
   int x = -1, t;
   if (j < n && accepts(a, b, j, &x)) t = a.io.d_draft[(int64_t)b * a.p.L + j];
-  else t = draw_row(a, b, j, j < n && x >= 0, x, sm);
+  else t = draw_row<VEC>(a, b, j, j < n && x >= 0, x, sm);
   if (threadIdx.x == 0) a.io.d_tok[(int64_t)b * (a.p.L + 1) + j] = t;
 }
 // The rows' tokens into committed ones and next drafts (the accept tests, two
@@ -214,12 +280,19 @@ __global__ __launch_bounds__(128) void k_given_end(GivenArgs a) {
 
 hipError_t launch_verify_given(const sjd_given_params& p, const sjd_given_io& io, hipStream_t s) {
   const GivenArgs a{p, io};
+  auto fine = [](const float* x, int64_t row, int64_t win) {
+    return ((uintptr_t)x & 15) == 0 && row % 4 == 0 && win % 4 == 0;
+  };
+  const bool vec = fine(io.d_p, p.p_row, p.p_win) && (!io.d_q || fine(io.d_q, p.q_row, p.q_win));
   if (p.flags & SJD_AC) {
     const int rows = p.L + (p.flags & SJD_BONUS ? 1 : 0);
-    hipLaunchKernelGGL(k_given_rows, dim3(p.B * rows), dim3(kThreads), 0, s, a);
+    if (vec) hipLaunchKernelGGL(k_given_rows<true>, dim3(p.B * rows), dim3(kThreads), 0, s, a);
+    else hipLaunchKernelGGL(k_given_rows<false>, dim3(p.B * rows), dim3(kThreads), 0, s, a);
     hipLaunchKernelGGL(k_given_end, dim3(p.B), dim3(128), 0, s, a);
+  } else if (vec) {
+    hipLaunchKernelGGL(k_given_chain<true>, dim3(p.B), dim3(kThreads), 0, s, a);
   } else {
-    hipLaunchKernelGGL(k_given_chain, dim3(p.B), dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL(k_given_chain<false>, dim3(p.B), dim3(kThreads), 0, s, a);
   }
   return hipGetLastError();
 }

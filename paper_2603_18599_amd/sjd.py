@@ -7,6 +7,7 @@ fallback path.
 """
 import ctypes as C
 import os
+from array import array
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_NAME = "libsjd.so"
@@ -220,30 +221,50 @@ def verify_outputs(B, L, K, D, device="cuda"):
             "sib": torch.zeros(B, max(D, 0), max(K - 1, 0), dtype=torch.int32, device=device)}
 
 
+# ---- the standalone operators. A call costs some microseconds on the GPU, so the
+# checks here are kept to comparisons of what a tensor already holds.
+_DTYPES = {"float32": 0, "bfloat16": 1, "fp32": 0, "bf16": 1, "e4m3": 2}
+
+
+def _types():
+    """torch and {torch type: sjd_dtype}, once torch is needed."""
+    global _types
+    import torch
+    t = (torch, {torch.float32: 0, torch.bfloat16: 1})
+    _types = lambda: t  # noqa: E731
+    return t
+
+
 def _expect(fn, ok):
     """The library reads device memory by the sizes that it is told: a tensor of
-    another type, shape or layout is refused like any other bad argument."""
+    another type, shape, layout or device is refused like any other bad
+    argument."""
     if not ok:
         raise SjdError(fn, -1)
 
 
-def _rows_of(fn, t, T, heads, hd, dtypes):
+def _launch(fn, stream, device, *args):
+    """The call on `stream`, or the device's current one. Its tensors lie on
+    `device`, which must be the current GPU (the library launches there)."""
+    torch = _types()[0]
+    _expect(fn, device >= 0 and device == torch.cuda.current_device())
+    raw = stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(device)
+    rc = getattr(_lib or load_library(), fn)(*args, raw)
+    if rc != 0:
+        raise SjdError(fn, rc)
+
+
+def _row_stride(fn, t, T, heads, hd):
     """Row stride of [T, heads, hd] rows whose heads lie one behind the other."""
-    _expect(fn, t.dim() == 3 and tuple(t.shape) == (T, heads, hd) and str(t.dtype)[6:] in dtypes)
-    _expect(fn, T == 0 or heads == 0 or (t.stride(2) == 1 and (heads == 1 or t.stride(1) == hd)))
-    return t.stride(0) if T > 1 else max(t.stride(0), heads * hd)
+    _expect(fn, t.shape == (T, heads, hd))
+    s = t.stride()
+    _expect(fn, T == 0 or (s[2] == 1 and (heads == 1 or s[1] == hd)))
+    return s[0] if T > 1 else max(s[0], heads * hd)
 
 
-def _one_device(fn, *tensors):
-    """Every tensor on the current GPU (the library launches there)."""
-    import torch
-    for t in tensors:
-        if t is not None:
-            _expect(fn, t.device.type == "cuda" and t.device.index == torch.cuda.current_device())
-
-
-def _dense(fn, t, shape, dtype):
-    _expect(fn, t is None or (tuple(t.shape) == tuple(shape) and t.is_contiguous() and str(t.dtype)[6:] == dtype))
+def _dense(fn, t, shape, dtype, device):
+    _expect(fn, t.shape == shape and t.dtype is dtype and t.is_contiguous() and t.get_device() == device)
+    return t.data_ptr()
 
 
 def sjd_verify_given(p, q, draft, n, u, r, meta, tok, next=None, *, flags=0, vis_lo=0, stream=None):
@@ -254,26 +275,26 @@ def sjd_verify_given(p, q, draft, n, u, r, meta, tok, next=None, *, flags=0, vis
     float32 [B, L + 1]; outputs int32 meta [B, 4], tok [B, L + 1], next [B, L]
     (None without SJD_AC)."""
     fn = "sjd_verify_given"
+    torch = _types()[0]
+    i32, f32 = torch.int32, torch.float32
     _expect(fn, draft.dim() == 2 and p.dim() == 3)
-    (B, L), V = draft.shape, p.shape[2]
-    _dense(fn, draft, (B, L), "int32")
-    _dense(fn, n, (B,), "int32")
-    _dense(fn, u, (B, L), "float32")
-    _dense(fn, r, (B, L + 1), "float32")
-    _dense(fn, meta, (B, 4), "int32")
-    _dense(fn, tok, (B, L + 1), "int32")
-    _dense(fn, next, (B, L), "int32")
-    for t, rows in ((p, L + (1 if flags & SJD_BONUS else 0)), (q, L)):
-        _expect(fn, t is None or (tuple(t.shape) == (B, rows, V) and str(t.dtype) == "torch.float32" and
-                                  (V <= 1 or t.stride(2) == 1)))
-    _one_device(fn, p, q, draft, n, u, r, meta, tok, next)
-    par = GivenParams(B, L, V, flags, vis_lo, p.stride(1), p.stride(0), q.stride(1) if q is not None else 0,
-                      q.stride(0) if q is not None else 0)
-    io = GivenIO(_ptr(p), _ptr(q), _ptr(draft), _ptr(n), _ptr(u), _ptr(r), _ptr(meta), _ptr(tok), _ptr(next))
-    _check(fn, load_library().sjd_verify_given(C.byref(par), C.byref(io), _stream(stream)))
+    (B, L), V, dev = draft.shape, p.shape[2], p.get_device()
 
+    def rows(t, count):
+        _expect(fn, t.shape == (B, count, V) and t.dtype is f32 and t.get_device() == dev)
+        s = t.stride()
+        _expect(fn, V == 1 or s[2] == 1)
+        # (a stride that separates nothing may be anything)
+        return t.data_ptr(), max(s[1], V) if count <= 1 else s[1], s[0]
 
-_DTYPES = {"float32": 0, "bfloat16": 1, "e4m3": 2, "bf16": 1}
+    pp, p_row, p_win = rows(p, L + 1 if flags & SJD_BONUS else L)
+    qp, q_row, q_win = (None, 0, 0) if q is None else rows(q, L)
+    io = GivenIO(pp, qp, _dense(fn, draft, (B, L), i32, dev), None if n is None else _dense(fn, n, (B,), i32, dev),
+                 _dense(fn, u, (B, L), f32, dev), _dense(fn, r, (B, L + 1), f32, dev),
+                 _dense(fn, meta, (B, 4), i32, dev), _dense(fn, tok, (B, L + 1), i32, dev),
+                 None if next is None else _dense(fn, next, (B, L), i32, dev))
+    par = GivenParams(B, L, V, flags, vis_lo, p_row, p_win, q_row, q_win)
+    _launch(fn, stream, dev, C.byref(par), C.byref(io))
 
 
 def sjd_rope_axes(q, k, pos, freq, axis, *, out_q=None, out_k=None, inverse=False, stream=None):
@@ -282,29 +303,34 @@ def sjd_rope_axes(q, k, pos, freq, axis, *, out_q=None, out_k=None, inverse=Fals
     float32), in place unless out_q / out_k are given. pos int32 [T, axes]; freq
     and axis: one frequency and one axis for each pair of dims."""
     fn = "sjd_rope_axes"
+    torch, types = _types()
     x = q if q is not None else k
-    _expect(fn, x is not None and x.dim() == 3 and pos.dim() == 2 and 1 <= len(freq) <= 128 and len(axis) == len(freq))
-    T, hd, dt = x.shape[0], x.shape[2], str(x.dtype)[6:]
-    _expect(fn, all(0 <= a < pos.shape[1] for a in axis))
-    out_q, out_k = q if out_q is None else out_q, k if out_k is None else out_k
-    par = RopeParams(T, 0, 0, hd, len(freq), pos.shape[1], _DTYPES.get(dt, -1), 1 if inverse else 0)
-    par.freq[:len(freq)] = list(freq)
-    par.axis[:len(axis)] = list(axis)
-    _dense(fn, pos, (T, pos.shape[1]), "int32")
+    P = len(freq)
+    _expect(fn, x is not None and x.dim() == 3 and pos.dim() == 2 and 1 <= P <= 128 and len(axis) == P)
+    (T, _, hd), dt, dev, axes = x.shape, x.dtype, x.get_device(), pos.shape[1]
+    par = RopeParams(T, 0, 0, hd, P, axes, types.get(dt, -1), 1 if inverse else 0)
+    C.memmove(C.byref(par, RopeParams.freq.offset), array("d", freq).tobytes(), 8 * P)
+    C.memmove(C.byref(par, RopeParams.axis.offset), bytes(axis), P)
+    io = RopeIO(None, None, _dense(fn, pos, (T, axes), torch.int32, dev))
     if q is not None:
-        par.H = q.shape[1] if q.dim() == 3 else -1
-        par.q_row, par.out_q_row = (_rows_of(fn, t, T, par.H, hd, (dt,)) for t in (q, out_q))
+        o = q if out_q is None else out_q
+        _expect(fn, o.dtype is dt and o.get_device() == dev)
+        par.H = H = q.shape[1]
+        par.q_row, par.out_q_row = _row_stride(fn, q, T, H, hd), _row_stride(fn, o, T, H, hd)
+        io.d_q, io.d_out_q = q.data_ptr(), o.data_ptr()
     if k is not None:
-        par.Hkv = k.shape[1] if k.dim() == 3 else -1
-        par.k_row, par.out_k_row = (_rows_of(fn, t, T, par.Hkv, hd, (dt,)) for t in (k, out_k))
-    _one_device(fn, q, k, pos, out_q, out_k)
-    io = RopeIO(_ptr(q), _ptr(k), _ptr(pos), _ptr(out_q), _ptr(out_k))
-    _check(fn, load_library().sjd_rope_axes(C.byref(par), C.byref(io), _stream(stream)))
+        o = k if out_k is None else out_k
+        _expect(fn, k.dim() == 3 and k.dtype is dt and k.get_device() == dev and o.dtype is dt and
+                o.get_device() == dev)
+        par.Hkv = H = k.shape[1]
+        par.k_row, par.out_k_row = _row_stride(fn, k, T, H, hd), _row_stride(fn, o, T, H, hd)
+        io.d_k, io.d_out_k = k.data_ptr(), o.data_ptr()
+    _launch(fn, stream, dev, C.byref(par), C.byref(io))
 
 
 def page_bytes(page_len, n_kv_heads, head_dim, dtype):
     """Bytes of a page (dtype "bf16" or "e4m3"); 0 for sizes that no page has."""
-    d = PagesDesc(None, 1, page_len, n_kv_heads, head_dim, _DTYPES[dtype])
+    d = PagesDesc(None, 1, page_len, n_kv_heads, head_dim, _DTYPES.get(dtype, -1))
     return load_library().sjd_page_bytes(C.byref(d))
 
 
@@ -312,12 +338,11 @@ class Pages:
     """A pool of pages (sjd_pages) in the caller's uint8 tensor."""
 
     def __init__(self, pool, n_pages, page_len, n_kv_heads, head_dim, dtype):
-        fn = "sjd_pages"
         size = page_bytes(page_len, n_kv_heads, head_dim, dtype)
-        _expect(fn, size > 0 and n_pages >= 1 and str(pool.dtype) == "torch.uint8" and pool.is_contiguous() and
+        _expect("sjd_pages", size > 0 and n_pages >= 1 and pool.dtype is _types()[0].uint8 and pool.is_contiguous() and
                 pool.numel() >= n_pages * size)
-        self.pool, self.n_kv_heads, self.head_dim = pool, n_kv_heads, head_dim
-        self.desc = PagesDesc(_ptr(pool), n_pages, page_len, n_kv_heads, head_dim, _DTYPES[dtype])
+        self.pool, self.n_kv_heads, self.head_dim, self.device = pool, n_kv_heads, head_dim, pool.get_device()
+        self.desc = PagesDesc(pool.data_ptr(), n_pages, page_len, n_kv_heads, head_dim, _DTYPES[dtype])
 
 
 class Windows:
@@ -325,21 +350,20 @@ class Windows:
     0), table int32 [B, pages], over row tensors of T rows."""
 
     def __init__(self, seq, table, T, max_rows, max_cached):
-        fn = "sjd_windows"
-        B = seq.shape[0]
-        _dense(fn, seq, (B, 4), "int32")
-        _expect(fn, table.dim() == 2)
-        _dense(fn, table, (B, table.shape[1]), "int32")
+        fn, i32, self.device = "sjd_windows", _types()[0].int32, seq.get_device()
+        _expect(fn, seq.dim() == 2 and table.dim() == 2)
+        B, cols = seq.shape[0], table.shape[1]
         self.seq, self.table, self.T = seq, table, T
-        self.desc = WindowsDesc(B, T, max_rows, max_cached, table.shape[1], _ptr(seq), _ptr(table))
+        self.desc = WindowsDesc(B, T, max_rows, max_cached, cols, _dense(fn, seq, (B, 4), i32, self.device),
+                                _dense(fn, table, (B, cols), i32, self.device))
 
 
 def _kv_call(fn, pages, win, k, v, stream):
-    dt = str(k.dtype)[6:]
-    rows = KvRows(_ptr(k), _ptr(v), *(_rows_of(fn, t, win.T, pages.n_kv_heads, pages.head_dim, (dt,)) for t in (k, v)),
-                  _DTYPES.get(dt, -1))
-    _one_device(fn, pages.pool, win.seq, win.table, k, v)
-    _check(fn, getattr(load_library(), fn)(C.byref(pages.desc), C.byref(win.desc), C.byref(rows), _stream(stream)))
+    T, H, hd, dev = win.T, pages.n_kv_heads, pages.head_dim, pages.device
+    _expect(fn, k.dtype is v.dtype and win.device == dev and k.get_device() == dev and v.get_device() == dev)
+    rows = KvRows(k.data_ptr(), v.data_ptr(), _row_stride(fn, k, T, H, hd), _row_stride(fn, v, T, H, hd),
+                  _types()[1].get(k.dtype, -1))
+    _launch(fn, stream, dev, C.byref(pages.desc), C.byref(win.desc), C.byref(rows))
 
 
 def sjd_kv_append(pages, win, k, v, stream=None):
@@ -357,9 +381,8 @@ def sjd_kv_read(pages, win, k, v, stream=None):
 def attention_workspace(pages, win, H):
     """Scratch for sjd_paged_attention with these pages and windows (calls that
     overlap in time need one each)."""
-    import torch
     n = load_library().sjd_paged_attention_workspace(C.byref(pages.desc), C.byref(win.desc), H)
-    return torch.empty(n, dtype=torch.uint8, device=pages.pool.device)
+    return _types()[0].empty(n, dtype=_types()[0].uint8, device=pages.pool.device)
 
 
 def sjd_paged_attention(pages, win, q, out, ws, *, scale, anc=None, stream=None):
@@ -367,15 +390,15 @@ def sjd_paged_attention(pages, win, q, out, ws, *, scale, anc=None, stream=None)
     (sjd_paged_attention in include/sjd.h); bfloat16. ws: attention_workspace;
     anc: int64 [T] ancestor masks of tree windows, or None (causal)."""
     fn = "sjd_paged_attention"
-    _expect(fn, q.dim() == 3)
-    H = q.shape[1]
-    io = AttentionIO(H, scale, _ptr(q), _ptr(out), *(_rows_of(fn, t, win.T, H, pages.head_dim, ("bfloat16",))
-                                                     for t in (q, out)), _ptr(anc))
-    _dense(fn, anc, (win.T,), "int64")
-    _expect(fn, str(ws.dtype) == "torch.uint8" and ws.is_contiguous())
-    _one_device(fn, pages.pool, win.seq, win.table, q, out, anc, ws if ws.numel() else None)
-    _check(fn, load_library().sjd_paged_attention(C.byref(pages.desc), C.byref(win.desc), C.byref(io), _ptr(ws),
-                                                   ws.numel(), _stream(stream)))
+    torch = _types()[0]
+    dev, hd, T = pages.device, pages.head_dim, win.T
+    _expect(fn, q.dim() == 3 and q.dtype is torch.bfloat16 and out.dtype is torch.bfloat16 and win.device == dev and
+            q.get_device() == dev and out.get_device() == dev)
+    H, size = q.shape[1], ws.numel()
+    _expect(fn, ws.dtype is torch.uint8 and ws.is_contiguous() and (size == 0 or ws.get_device() == dev))
+    io = AttentionIO(H, scale, q.data_ptr(), out.data_ptr(), _row_stride(fn, q, T, H, hd), _row_stride(fn, out, T, H, hd),
+                     None if anc is None else _dense(fn, anc, (T,), torch.int64, dev))
+    _launch(fn, stream, dev, C.byref(pages.desc), C.byref(win.desc), C.byref(io), ws.data_ptr(), size)
 
 
 class Engine:
