@@ -9,6 +9,7 @@
 // e4m3 codes become bf16 without rounding, times the key's power of two (an operand
 // of the conversion); a value row's power multiplies its probability.
 #include <cmath>
+#include <type_traits>
 
 #include "device.h"
 #include "forward.h"
@@ -51,59 +52,62 @@ SJD_DEV bf16x8 bf16_of_e4m3(uint2 c, float scale) {
                                                pk_bf16_of_e4m3<false>(c.y, scale), pk_bf16_of_e4m3<true>(c.y, scale)));
 }
 
-// One lane's part of a 32-position tile as it lies in memory, as a source of MFMA
-// operands: key(t), 8 dims of a key row (step t); val(d, jj), 8 positions from 16 jj
-// of a value column (dims block d).
+// One lane's part of a 32-position tile's keys, or of its values, as it lies in
+// memory, and the MFMA operands that it makes: of keys step t, 8 dims of a key row;
+// of values (d, jj), 8 positions from 16 jj of a column of dims block d.
 template <int HD, bool FP8>
-struct RawTile {
-  static constexpr int NK = FP8 ? HD / 32 : HD / 16;  // 16-byte pieces of keys, and of values
-  static constexpr bool kScaled = FP8;                // values lack their rows' powers of two
-  uint4 k[NK], v[NK];
-  uint32_t ke;  // e4m3: exponent byte of the lane's key row,
-  uint2 ve[2];  // and of the 16 positions that its score registers hold
-
-  // positions p0 .. p0 + 31 of a page's head
+struct RawKeys {
+  static constexpr int N = FP8 ? HD / 32 : HD / 16;
+  uint4 x[N];
+  uint32_t e;  // e4m3: exponent byte of the lane's key row, position swap23(lane % 32)
   SJD_DEV void load(const PagedArgs& a, const char* page, int h, int p0) {
-    constexpr int ES = FP8 ? 1 : 2;
     const int in = p0 & ((1 << a.pv.plen_log2) - 1), lane = threadIdx.x & 63;
-    const uint4* kp = (const uint4*)(page + tile_off<HD, ES>(a.pv, h, in, 0)) + lane;
-    const uint4* vp = (const uint4*)(page + tile_off<HD, ES>(a.pv, h, in, 1)) + lane;
+    const uint4* p = (const uint4*)(page + tile_off<HD, FP8 ? 1 : 2>(a.pv, h, in, 0)) + lane;
 #pragma unroll
-    for (int i = 0; i < NK; ++i) k[i] = kp[64 * i];
-#pragma unroll
-    for (int i = 0; i < NK; ++i) v[i] = vp[64 * i];
-    if constexpr (FP8) {
-      // a lane's MFMA key row is position swap23(lane % 32); its score registers 8 jj
-      // + e hold positions 16 jj + 8 half + e
-      ke = (uint8_t)page[exp_off<HD>(a.pv, h, 0) + in + swap23(lane & 31)];
-      const char* e = page + exp_off<HD>(a.pv, h, 1) + in + 8 * (lane >> 5);
-      ve[0] = *(const uint2*)e;
-      ve[1] = *(const uint2*)(e + 16);
-    }
+    for (int i = 0; i < N; ++i) x[i] = p[64 * i];
+    if constexpr (FP8) e = (uint8_t)page[exp_off<HD>(a.pv, h, 0) + in + swap23(lane & 31)];
   }
   SJD_DEV bf16x8 key(int t) const {
     if constexpr (FP8) {
-      const uint4 x = k[t >> 1];
-      return bf16_of_e4m3(t & 1 ? make_uint2(x.z, x.w) : make_uint2(x.x, x.y), __uint_as_float(ke << 23));
+      const uint4 y = x[t >> 1];
+      return bf16_of_e4m3(t & 1 ? make_uint2(y.z, y.w) : make_uint2(y.x, y.y), __uint_as_float(e << 23));
     } else {
-      return __builtin_bit_cast(bf16x8, k[t]);
+      return __builtin_bit_cast(bf16x8, x[t]);
+    }
+  }
+};
+template <int HD, bool FP8>
+struct RawValues {
+  static constexpr int N = FP8 ? HD / 32 : HD / 16;
+  static constexpr bool kScaled = FP8;  // the operands lack their rows' powers of two
+  uint4 x[N];
+  uint2 e[2];  // e4m3: exponent bytes of positions 16 jj + 8 half + 0 .. 7, the score registers'
+  SJD_DEV void load(const PagedArgs& a, const char* page, int h, int p0) {
+    const int in = p0 & ((1 << a.pv.plen_log2) - 1), lane = threadIdx.x & 63;
+    const uint4* p = (const uint4*)(page + tile_off<HD, FP8 ? 1 : 2>(a.pv, h, in, 1)) + lane;
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = p[64 * i];
+    if constexpr (FP8) {
+      const char* q = page + exp_off<HD>(a.pv, h, 1) + in + 8 * (lane >> 5);
+      e[0] = *(const uint2*)q;
+      e[1] = *(const uint2*)(q + 16);
     }
   }
   SJD_DEV bf16x8 val(int d, int jj) const {
     if constexpr (FP8) {
-      const uint4 x = v[d];
-      return bf16_of_e4m3(jj ? make_uint2(x.z, x.w) : make_uint2(x.x, x.y), 1.0f);
+      const uint4 y = x[d];
+      return bf16_of_e4m3(jj ? make_uint2(y.z, y.w) : make_uint2(y.x, y.y), 1.0f);
     } else {
-      return __builtin_bit_cast(bf16x8, v[d * 2 + jj]);
+      return __builtin_bit_cast(bf16x8, x[d * 2 + jj]);
     }
   }
   SJD_DEV float power(int i) const {  // of score register i's value row
-    const uint32_t w = (i & 7) < 4 ? ve[i >> 3].x : ve[i >> 3].y;
+    const uint32_t w = (i & 7) < 4 ? e[i >> 3].x : e[i >> 3].y;
     return __uint_as_float(((w >> (8 * (i & 3))) & 0xFFu) << 23);
   }
 };
 
-// The same of a tile in LDS, widened to bf16: [key steps, then value blocks][lane]
+// Both of a tile in LDS, widened to bf16: [key steps, then value blocks][lane]
 template <int HD>
 struct LdsTile {
   static constexpr bool kScaled = false;
@@ -133,35 +137,36 @@ SJD_DEV bf16x8 clear_from(bf16x8 v, int pos, int lim, bool& bad) {
 // to: the largest score when it was last moved (log2 domain).
 template <int HD>
 struct WaveState {
-  bf16x8 q[HD / 16];
   f32x16 o[HD / 32];
   float m, l;
 };
+
+// S^T of 32 keys. vis (MASKED): bit i says that register i's key is visible.
+template <int HD, bool MASKED, class Keys, class Q>
+SJD_DEV void scores(f32x16& c, const Keys& k, const Q& q, uint32_t vis) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) c[i] = 0.0f;
+#pragma unroll
+  for (int t = 0; t < HD / 16; ++t) c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k.key(t), q(t), c, 0, 0, 0);
+  if (MASKED)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) c[i] = (vis >> i) & 1 ? c[i] : -INFINITY;
+}
 
 // The reference moves only when a score exceeds it by kLag: probabilities up to 2^8
 // lose nothing (bf16 and float are relative), and most tiles skip the rescaling
 // of HD / 2 output registers.
 constexpr float kLag = 8.0f;
 
-// N tiles of 32 keys. vis[n]: bit i says that score register i is visible; lim[n]:
-// positions of the tile that hold anything.
-template <int HD, int N, bool MASKED, class Tile>
-SJD_DEV void attend(WaveState<HD>& s, const Tile (&tile)[N], float scale, const uint32_t (&vis)[N], const int (&lim)[N]) {
-  constexpr int ND = HD / 32;
-  f32x16 c[N];
-  float mx = -INFINITY;
+// Moves the reference if these scores ask for it, makes them probabilities and adds
+// them to the sum.
+template <int HD, int N, bool MASKED>
+SJD_DEV void weigh(WaveState<HD>& s, f32x16 (&c)[N], float scale, const uint32_t (&vis)[N]) {
+  float mx = c[0][0];
 #pragma unroll
-  for (int n = 0; n < N; ++n) {
+  for (int n = 0; n < N; ++n)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) c[n][i] = 0.0f;
-#pragma unroll
-    for (int t = 0; t < HD / 16; ++t) c[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tile[n].key(t), s.q[t], c[n], 0, 0, 0);
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      if (MASKED) c[n][i] = (vis[n] >> i) & 1 ? c[n][i] : -INFINITY;
-      mx = fmaxf(mx, c[n][i]);
-    }
-  }
+    for (int i = 0; i < 16; ++i) mx = fmaxf(mx, c[n][i]);
   mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
   mx = mx == -INFINITY ? mx : mx * scale;
   const bool move = mx > s.m + kLag;
@@ -171,76 +176,79 @@ SJD_DEV void attend(WaveState<HD>& s, const Tile (&tile)[N], float scale, const 
     s.m = move ? mx : s.m;
     s.l *= alpha;
 #pragma unroll
-    for (int d = 0; d < ND; ++d)
+    for (int d = 0; d < HD / 32; ++d)
 #pragma unroll
       for (int i = 0; i < 16; ++i) s.o[d][i] *= alpha;
   }
   const float base = s.m == -INFINITY ? 0.0f : s.m;
-  bf16x8 p[N][2];
-#pragma unroll
-  for (int n = 0; n < N; ++n) {
-    float sum = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(c[n][i], scale, -base));
-      // (a masked position may hold anything, its exponent byte too)
-      c[n][i] = MASKED && !((vis[n] >> i) & 1) ? 0.0f : e;
-      sum += c[n][i];
-    }
-    s.l += sum;
-    if constexpr (Tile::kScaled) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) c[n][i] = MASKED && !((vis[n] >> i) & 1) ? 0.0f : c[n][i] * tile[n].power(i);
-    }
-#pragma unroll
-    for (int jj = 0; jj < 2; ++jj)
-      p[n][jj] = __builtin_bit_cast(
-          bf16x8, make_uint4(pk_bf16(c[n][8 * jj], c[n][8 * jj + 1]), pk_bf16(c[n][8 * jj + 2], c[n][8 * jj + 3]),
-                             pk_bf16(c[n][8 * jj + 4], c[n][8 * jj + 5]), pk_bf16(c[n][8 * jj + 6], c[n][8 * jj + 7])));
-  }
-  const int half = (threadIdx.x & 63) >> 5;
+  float sum[4] = {};
 #pragma unroll
   for (int n = 0; n < N; ++n)
 #pragma unroll
-    for (int d = 0; d < ND; ++d) {
-      bf16x8 v[2];
-      bool bad = false;
-#pragma unroll
-      for (int jj = 0; jj < 2; ++jj) {
-        v[jj] = tile[n].val(d, jj);
-        if (MASKED) v[jj] = clear_from(v[jj], 16 * jj + 8 * half, lim[n], bad);
-      }
-      if (MASKED && __any(bad)) {
-        // A value that is not finite: 0 * it would reach slots that do not attend
-        // to its position. It is taken out, and each slot that attends to one of
-        // its kind gets one added.
-        auto kind_of = [](float x) { return x != x ? 2 : x == INFINITY ? 0 : x == -INFINITY ? 1 : 3; };
-        for (int kind = 0; kind < 3; ++kind) {
-          f32x16 cnt;
-#pragma unroll
-          for (int i = 0; i < 16; ++i) cnt[i] = 0.0f;
-#pragma unroll
-          for (int jj = 0; jj < 2; ++jj) {
-            bf16x8 w, see;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              w[e] = (__bf16)(kind_of((float)v[jj][e]) == kind ? 1.0f : 0.0f);
-              see[e] = (__bf16)((vis[n] >> (8 * jj + e)) & 1 ? 1.0f : 0.0f);
-            }
-            cnt = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w, see, cnt, 0, 0, 0);
-          }
-          const float add = kind == 0 ? INFINITY : kind == 1 ? -INFINITY : __builtin_nanf("");
-#pragma unroll
-          for (int i = 0; i < 16; ++i) s.o[d][i] += cnt[i] > 0.0f ? add : 0.0f;
-        }
-#pragma unroll
-        for (int jj = 0; jj < 2; ++jj)
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[jj][e] = kind_of((float)v[jj][e]) == 3 ? v[jj][e] : (__bf16)0.0f;
-      }
-#pragma unroll
-      for (int jj = 0; jj < 2; ++jj) s.o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[jj], p[n][jj], s.o[d], 0, 0, 0);
+    for (int i = 0; i < 16; ++i) {
+      const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(c[n][i], scale, -base));
+      c[n][i] = MASKED && !((vis[n] >> i) & 1) ? 0.0f : e;
+      sum[i & 3] += c[n][i];
     }
+  s.l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+}
+
+// O^T += V^T . P^T for the 32 keys of c. MASKED: `lim` positions of the tile hold
+// anything.
+template <int HD, bool MASKED, class Values>
+SJD_DEV void collect(WaveState<HD>& s, f32x16& c, const Values& r, uint32_t vis, int lim) {
+  if constexpr (Values::kScaled)
+#pragma unroll
+    for (int i = 0; i < 16; ++i)  // (a masked position's exponent byte may be anything)
+      c[i] = MASKED && !((vis >> i) & 1) ? 0.0f : c[i] * r.power(i);
+  bf16x8 p[2];
+#pragma unroll
+  for (int jj = 0; jj < 2; ++jj)
+    p[jj] = __builtin_bit_cast(bf16x8, make_uint4(pk_bf16(c[8 * jj], c[8 * jj + 1]), pk_bf16(c[8 * jj + 2], c[8 * jj + 3]),
+                                                  pk_bf16(c[8 * jj + 4], c[8 * jj + 5]),
+                                                  pk_bf16(c[8 * jj + 6], c[8 * jj + 7])));
+  const int half = (threadIdx.x & 63) >> 5;
+#pragma unroll
+  for (int d = 0; d < HD / 32; ++d) {
+    bf16x8 v[2];
+    bool bad = false;
+#pragma unroll
+    for (int jj = 0; jj < 2; ++jj) {
+      v[jj] = r.val(d, jj);
+      if (MASKED) v[jj] = clear_from(v[jj], 16 * jj + 8 * half, lim, bad);
+    }
+    if (MASKED && __any(bad)) {
+      // A value that is not finite: 0 * it would reach slots that do not attend
+      // to its position. It is taken out, and each slot that attends to one of
+      // its kind gets one added.
+      auto kind_of = [](float x) { return x != x ? 2 : x == INFINITY ? 0 : x == -INFINITY ? 1 : 3; };
+#pragma unroll 1
+      for (int kind = 0; kind < 3; ++kind) {
+        f32x16 cnt;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) cnt[i] = 0.0f;
+#pragma unroll
+        for (int jj = 0; jj < 2; ++jj) {
+          bf16x8 w, see;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            w[e] = (__bf16)(kind_of((float)v[jj][e]) == kind ? 1.0f : 0.0f);
+            see[e] = (__bf16)((vis >> (8 * jj + e)) & 1 ? 1.0f : 0.0f);
+          }
+          cnt = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w, see, cnt, 0, 0, 0);
+        }
+        const float add = kind == 0 ? INFINITY : kind == 1 ? -INFINITY : __builtin_nanf("");
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s.o[d][i] += cnt[i] > 0.0f ? add : 0.0f;
+      }
+#pragma unroll
+      for (int jj = 0; jj < 2; ++jj)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[jj][e] = kind_of((float)v[jj][e]) == 3 ? v[jj][e] : (__bf16)0.0f;
+    }
+#pragma unroll
+    for (int jj = 0; jj < 2; ++jj) s.o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[jj], p[jj], s.o[d], 0, 0, 0);
+  }
 }
 
 // A lane's slot: row f / G of the window, query head f % G of the group
@@ -259,16 +267,17 @@ SJD_DEV Slot slot_of(const PagedArgs& a, const Seq& sq, int h, int f) {
   s.mask = a.anc && s.ok ? a.anc[s.t] : 0;
   return s;
 }
+// Piece i of a slot's q: dims half * HD / 2 + 8 i .. (zeros for a slot that is not there)
 template <int HD>
-SJD_DEV void start(WaveState<HD>& s, const PagedArgs& a, const Slot& sl) {
+SJD_DEV uint4 load_q(const PagedArgs& a, const Slot& sl, int i) {
   const int half = (threadIdx.x & 63) >> 5;
-  const uint4* q = (const uint4*)(a.q + sl.t * a.q_row + (sl.ok ? sl.head : 0) * HD + half * (HD / 2));
   const uint32_t sign = a.negate ? 0x80008000u : 0u;
-#pragma unroll
-  for (int i = 0; i < HD / 16; ++i) {
-    const uint4 x = sl.ok ? q[i] : make_uint4(0, 0, 0, 0);
-    s.q[i] = __builtin_bit_cast(bf16x8, make_uint4(x.x ^ sign, x.y ^ sign, x.z ^ sign, x.w ^ sign));
-  }
+  if (!sl.ok) return make_uint4(0, 0, 0, 0);
+  const uint4 x = ((const uint4*)(a.q + sl.t * a.q_row + sl.head * HD + half * (HD / 2)))[i];
+  return make_uint4(x.x ^ sign, x.y ^ sign, x.z ^ sign, x.w ^ sign);
+}
+template <int HD>
+SJD_DEV void start(WaveState<HD>& s) {
 #pragma unroll
   for (int d = 0; d < HD / 32; ++d)
 #pragma unroll
@@ -290,51 +299,80 @@ SJD_DEV uint32_t visible(const PagedArgs& a, const Seq& sq, int p0, const Slot& 
   return v;
 }
 
-// 32 slots of one key / value head of one sequence per workgroup; the four waves
-// take every fourth tile of the split's keys and merge in LDS.
+// Few slots: 32 of one key / value head of one sequence per workgroup; its four
+// waves take every fourth tile of the split's keys, straight from memory to
+// registers with the next tile's loads behind this one's arithmetic, and merge in
+// LDS.
+constexpr int kRound = 4 * kTile;  // keys of the four waves
+
 template <int HD>
 struct MergeSmem {
+  uint4 q[HD / 16][kWave];
   float o[4][32][HD + 1];
   float m[4][32], l[4][32];
 };
 
 template <int HD, bool FP8>
-__global__ __launch_bounds__(256) void k_paged_attn(PagedArgs a) {
+__global__ __launch_bounds__(256, 2) void k_paged_attn(PagedArgs a) {
   constexpr int ND = HD / 32;
   __shared__ MergeSmem<HD> sm;
   const int h = blockIdx.x % a.pv.Hkv, sp = blockIdx.x / a.pv.Hkv, z = blockIdx.z;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5;
+  const int beg = sp * a.chunk;
+  int p0 = beg + kTile * wave;
+  // (page ids do not wait for the sequence: inside the table there is something to read)
+  auto id_of = [&](int p) { return (p >> a.pv.plen_log2) < a.w.table_len ? page_id(a.w, a.pv, z, p) : -1; };
+  const int id = id_of(p0);
+  int id_next = id_of(p0 + kRound);
   const Seq sq = load_seq(a.w, a.pv, z);
   const int slots = sq.rows * a.G, f0 = blockIdx.y * 32;
   if (f0 >= slots) return;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5;
   // causal: the last row of these slots bounds their keys
-  const int last = min(sq.rows - 1, (f0 + 31) / a.G);
-  const int nk = sq.cached + (a.anc ? sq.rows : last + 1);
-  const int beg = sp * a.chunk, end = min(nk, beg + a.chunk);
-  if (beg >= sq.cached + sq.rows) return;
+  const int total = sq.cached + sq.rows, last = min(sq.rows - 1, (f0 + 31) / a.G);
+  const int end = min(a.anc ? total : sq.cached + last + 1, beg + a.chunk), full = min(sq.cached, end);
+  if (beg >= total) return;
   const Slot sl = slot_of(a, sq, h, f0 + (lane & 31));
-  WaveState<HD> s;
-  start(s, a, sl);
-  for (int p0 = beg + 32 * wave; p0 < end; p0 += 128) {
-    const char* page = page_of(a.w, a.pv, z, p0);
-    if (!page) continue;
-    RawTile<HD, FP8> r[1];
-    r[0].load(a, page, h, p0);
-    const int lim[1] = {sq.cached + sq.rows - p0};
-    if (p0 + 32 <= sq.cached) {
-      const uint32_t vis[1] = {0xFFFFu};
-      attend<HD, 1, false>(s, r, a.scale, vis, lim);
-    } else {
-      const uint32_t vis[1] = {visible(a, sq, p0, sl)};
-      attend<HD, 1, true>(s, r, a.scale, vis, lim);
-    }
+  RawKeys<HD, FP8> k;
+  RawValues<HD, FP8> v;
+  const char* page = p0 < end ? page_at(a.pv, id) : nullptr;
+  if (page) {
+    k.load(a, page, h, p0);
+    v.load(a, page, h, p0);
   }
+#pragma unroll
+  for (int i = wave; i < HD / 16; i += 4) sm.q[i][lane] = load_q<HD>(a, sl, i);
+  WaveState<HD> s;
+  start(s);
+  __syncthreads();
+  const auto q = [&](int t) { return __builtin_bit_cast(bf16x8, sm.q[t][lane]); };
+  // A tile (page NULL: left out): the next tile's keys are loaded into the registers
+  // of this one's once the scores are formed, its values once they are used up.
+  auto step = [&](auto masked) {
+    constexpr bool MASKED = decltype(masked)::value;
+    const int np = p0 + kRound;
+    const char* next = np < end ? page_at(a.pv, id_next) : nullptr;
+    id_next = id_of(np + kRound);
+    const uint32_t vis[1] = {MASKED && page ? visible(a, sq, p0, sl) : 0xFFFFu};
+    f32x16 c[1];
+    if (page) scores<HD, MASKED>(c[0], k, q, vis[0]);
+    if (next) k.load(a, next, h, np);
+    if (page) {
+      weigh<HD, 1, MASKED>(s, c, a.scale, vis);
+      collect<HD, MASKED>(s, c[0], v, vis[0], total - p0);
+    }
+    if (next) v.load(a, next, h, np);
+    page = next;
+    p0 = np;
+  };
+  while (p0 + kTile <= full) step(std::false_type{});
+  while (p0 < end) step(std::true_type{});
   s.l += __shfl_xor(s.l, 32, kWave);
   // register i of block d holds dim 32 d + 8 (i / 4) + 4 half + i % 4
+  if (sl.ok)
 #pragma unroll
-  for (int d = 0; d < ND; ++d)
+    for (int d = 0; d < ND; ++d)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) sm.o[wave][lane & 31][d * 32 + 8 * (i >> 2) + 4 * half + (i & 3)] = s.o[d][i];
+      for (int i = 0; i < 16; ++i) sm.o[wave][lane & 31][d * 32 + 8 * (i >> 2) + 4 * half + (i & 3)] = s.o[d][i];
   if (half == 0) {
     sm.m[wave][lane] = s.m;
     sm.l[wave][lane] = s.l;
@@ -346,12 +384,12 @@ __global__ __launch_bounds__(256) void k_paged_attn(PagedArgs a) {
   if (g >= slots) return;
   float mx = -INFINITY;
   for (int w = 0; w < 4; ++w) mx = fmaxf(mx, sm.m[w][sn]);
-  float v[DPT] = {}, l = 0.0f;
+  float y[DPT] = {}, l = 0.0f;
   for (int w = 0; w < 4; ++w) {
     const float fw = mx == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(sm.m[w][sn] - mx);
     l += sm.l[w][sn] * fw;
 #pragma unroll
-    for (int i = 0; i < DPT; ++i) v[i] += sm.o[w][sn][d0 + i] * fw;
+    for (int i = 0; i < DPT; ++i) y[i] += sm.o[w][sn][d0 + i] * fw;
   }
   const int64_t tt = sq.row0 + g / a.G;
   const int hh = h * a.G + g % a.G;
@@ -360,14 +398,14 @@ __global__ __launch_bounds__(256) void k_paged_attn(PagedArgs a) {
     uint4* o = (uint4*)(a.out + tt * a.out_row + hh * HD + d0);
 #pragma unroll
     for (int i = 0; i < DPT / 8; ++i)
-      o[i] = make_uint4(pk_bf16(v[8 * i] * inv, v[8 * i + 1] * inv), pk_bf16(v[8 * i + 2] * inv, v[8 * i + 3] * inv),
-                        pk_bf16(v[8 * i + 4] * inv, v[8 * i + 5] * inv), pk_bf16(v[8 * i + 6] * inv, v[8 * i + 7] * inv));
+      o[i] = make_uint4(pk_bf16(y[8 * i] * inv, y[8 * i + 1] * inv), pk_bf16(y[8 * i + 2] * inv, y[8 * i + 3] * inv),
+                        pk_bf16(y[8 * i + 4] * inv, y[8 * i + 5] * inv), pk_bf16(y[8 * i + 6] * inv, y[8 * i + 7] * inv));
     return;
   }
   const int64_t at = ((int64_t)sp * a.w.T + tt) * a.H + hh;
 #pragma unroll
   for (int i = 0; i < DPT; i += 4)
-    *(float4*)(a.ws_o + at * HD + d0 + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+    *(float4*)(a.ws_o + at * HD + d0 + i) = make_float4(y[i], y[i + 1], y[i + 2], y[i + 3]);
   if ((threadIdx.x & 7) == 0) *(float2*)(a.ws_ml + at * 2) = make_float2(mx, l);
 }
 
@@ -472,8 +510,12 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(PagedArgs a) {
   if (beg >= total) return;
   const int w0 = f0 + 32 * wave;
   const Slot sl = slot_of(a, sq, h, w0 + (lane & 31));
+  uint4 qr[HD / 16];
+#pragma unroll
+  for (int i = 0; i < HD / 16; ++i) qr[i] = load_q<HD>(a, sl, i);
+  const auto q = [&](int t) { return __builtin_bit_cast(bf16x8, qr[t]); };
   WaveState<HD> s;
-  start(s, a, sl);
+  start(s);
   // keys that every slot of the workgroup sees, and that any slot of this wave sees
   const int all = a.anc ? sq.cached : sq.cached + f0 / a.G + 1;
   const int any = w0 >= slots ? 0 : a.anc ? total : sq.cached + min(sq.rows - 1, (w0 + 31) / a.G) + 1;
@@ -519,10 +561,13 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(PagedArgs a) {
   // keys without a mask (in a loop of its own: it needs fewer registers), then the rest
   while (p0 + kStep <= min(all, end) && pg[0] && pg[1])
     step([&] {
-      const LdsTile<HD> t[kStepTiles] = {{lds[buf]}, {lds[buf] + St::TILE}};
       const uint32_t vis[kStepTiles] = {0xFFFFu, 0xFFFFu};
-      const int lim[kStepTiles] = {32, 32};
-      attend<HD, kStepTiles, false>(s, t, a.scale, vis, lim);
+      f32x16 c[kStepTiles];
+#pragma unroll
+      for (int n = 0; n < kStepTiles; ++n) scores<HD, false>(c[n], LdsTile<HD>{lds[buf] + n * St::TILE}, q, vis[n]);
+      weigh<HD, kStepTiles, false>(s, c, a.scale, vis);
+#pragma unroll
+      for (int n = 0; n < kStepTiles; ++n) collect<HD, false>(s, c[n], LdsTile<HD>{lds[buf] + n * St::TILE}, vis[n], 32);
     });
   while (p0 < end)
     step([&] {
@@ -530,10 +575,12 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(PagedArgs a) {
       for (int n = 0; n < kStepTiles; ++n) {
         const int p = p0 + 32 * n;
         if (!pg[n] || p >= any) continue;
-        const LdsTile<HD> t[1] = {{lds[buf] + n * St::TILE}};
+        const LdsTile<HD> t{lds[buf] + n * St::TILE};
         const uint32_t vis[1] = {visible(a, sq, p, sl)};
-        const int lim[1] = {total - p};
-        attend<HD, 1, true>(s, t, a.scale, vis, lim);
+        f32x16 c[1];
+        scores<HD, true>(c[0], t, q, vis[0]);
+        weigh<HD, 1, true>(s, c, a.scale, vis);
+        collect<HD, true>(s, c[0], t, vis[0], total - p);
       }
     });
   s.l += __shfl_xor(s.l, 32, kWave);
@@ -570,17 +617,35 @@ __global__ __launch_bounds__(256) void k_paged_join(PagedArgs a) {
   const int hh = i % a.H;
   const int n = (sq.cached + sq.rows + a.chunk - 1) / a.chunk;
   const int64_t at = t * a.H + hh, step = (int64_t)a.w.T * a.H;
-  float mx = -INFINITY;
-  for (int k = lane; k < n; k += kWave) mx = fmaxf(mx, a.ws_ml[(at + k * step) * 2]);
-  mx = wave_max(mx);
-  float l = 0.0f, v[HD / 64] = {};
-  for (int k = 0; k < n; ++k) {
-    const int64_t j = at + k * step;
-    const float2 ml = *(const float2*)(a.ws_ml + j * 2);
+  // 64 splits at a time: a lane reads one split's statistics, then every lane its
+  // dims of each of them
+  constexpr int W = HD / 64;
+  float m = -INFINITY, l = 0.0f, v[W] = {};
+  for (int k0 = 0; k0 < n; k0 += kWave) {
+    const float2 ml = k0 + lane < n ? *(const float2*)(a.ws_ml + (at + (k0 + lane) * step) * 2) : make_float2(-INFINITY, 0.0f);
+    const float mx = fmaxf(m, wave_max_dpp(ml.x));
     const float f = mx == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ml.x - mx);
-    l += ml.y * f;
+    const float old = mx == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - mx);
+    l = l * old + wave_sum(k0 + lane < n ? ml.y * f : 0.0f);
 #pragma unroll
-    for (int e = 0; e < HD / 64; ++e) v[e] += a.ws_o[j * HD + lane * (HD / 64) + e] * f;
+    for (int e = 0; e < W; ++e) v[e] *= old;
+    m = mx;
+    const int c = min(kWave, n - k0);
+    for (int k = 0; k < c; k += 8) {
+      float x[8][W];
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+#pragma unroll
+        for (int e = 0; e < W; ++e)
+          x[u][e] = k + u < c ? a.ws_o[(at + (k0 + k + u) * step) * HD + lane * W + e] : 0.0f;
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        if (k + u < c) {
+          const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), k + u));
+#pragma unroll
+          for (int e = 0; e < W; ++e) v[e] += x[u][e] * w;
+        }
+    }
   }
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
   uint16_t* o = a.out + t * a.out_row + hh * HD + lane * (HD / 64);
@@ -599,15 +664,17 @@ void launch_head(const PagedArgs& a, const AttnPlan& pl, dim3 grid, hipStream_t 
 // Few slots: every wave its own keys. More: keys shared by four waves of slots.
 constexpr int kFewSlots = 32;
 
-// Keys per split: one split where sequences, heads and slots fill the compute
-// units twice, else as many as do that, of 256 keys at least.
+// Keys per split. Few slots: enough workgroups for four rounds of two per compute
+// unit, so that sequences of unequal length even out, down to one tile per wave.
+// Many: as many as fill the compute units twice, of 256 keys at least.
 AttnPlan paged_attention_plan(const sjd_pages& p, const sjd_windows& w, int H) {
   const int64_t most = (int64_t)w.max_cached + w.max_rows;
   const int64_t slots = (int64_t)w.max_rows * (H / p.n_kv_heads);
   const bool few = slots <= kFewSlots;
   const int64_t wgs = (int64_t)w.B * p.n_kv_heads * (few ? 1 : (slots + 127) / 128);
-  int64_t S = wgs >= 512 ? 1 : (512 + wgs - 1) / wgs;
-  const int64_t cap = (most + 255) / 256;
+  const int64_t target = few ? 2048 : 512, least = few ? 128 : 256;
+  int64_t S = (target + wgs - 1) / wgs;
+  const int64_t cap = (most + least - 1) / least;
   if (S > cap) S = cap;
   if (S < 1) S = 1;
   const int64_t chunk = ((most + S - 1) / S + 127) / 128 * 128;
