@@ -119,18 +119,32 @@ struct LdsTile {
   SJD_DEV float power(int) const { return 1.0f; }
 };
 
-// Value operand with the positions from `lim` on cleared; bad: whether another
-// element is not finite
-SJD_DEV bf16x8 clear_from(bf16x8 v, int pos, int lim, bool& bad) {
+// Largest magnitude bits (of each half of a dword) of value operands seen so far;
+// from kNotFinite on one of them is infinite or NaN
+constexpr uint32_t kNotFinite = 0x7F80u;
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+SJD_DEV uint32_t largest(uint32_t seen, bf16x8 v) {
+  const uint4 u = __builtin_bit_cast(uint4, v);
+  auto top = [](uint32_t a, uint32_t b) {
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+  };
+  constexpr uint32_t kMag = 0x7FFF7FFFu;
+  return top(top(seen, u.x & kMag), top(top(u.y & kMag, u.z & kMag), u.w & kMag));
+}
+SJD_DEV bool not_finite(uint32_t seen) { return (seen & 0xFFFFu) >= kNotFinite || (seen >> 16) >= kNotFinite; }
+// Value operand (positions pos ..) with the positions from `lim` on cleared
+SJD_DEV bf16x8 clear_from(bf16x8 v, int pos, int lim) {
   uint4 u = __builtin_bit_cast(uint4, v);
   uint32_t* w = (uint32_t*)&u;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    if (pos + 2 * e >= lim) w[e] &= ~0xFFFFu;
-    if (pos + 2 * e + 1 >= lim) w[e] &= 0xFFFFu;
-    bad |= (w[e] & 0x7F80u) == 0x7F80u || (w[e] & 0x7F800000u) == 0x7F800000u;
-  }
+  for (int e = 0; e < 4; ++e) w[e] &= (pos + 2 * e < lim ? 0xFFFFu : 0u) | (pos + 2 * e + 1 < lim ? 0xFFFF0000u : 0u);
   return __builtin_bit_cast(bf16x8, u);
+}
+
+// The larger of v in lanes l and l ^ 32
+SJD_DEV float max_of_halves(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
 // One wave's state: 32 slots. m is the reference that probabilities are relative
@@ -167,7 +181,7 @@ SJD_DEV void weigh(WaveState<HD>& s, f32x16 (&c)[N], float scale, const uint32_t
   for (int n = 0; n < N; ++n)
 #pragma unroll
     for (int i = 0; i < 16; ++i) mx = fmaxf(mx, c[n][i]);
-  mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
+  mx = max_of_halves(mx);
   mx = mx == -INFINITY ? mx : mx * scale;
   const bool move = mx > s.m + kLag;
   if (__any(move)) {
@@ -210,14 +224,16 @@ SJD_DEV void collect(WaveState<HD>& s, f32x16& c, const Values& r, uint32_t vis,
   const int half = (threadIdx.x & 63) >> 5;
 #pragma unroll
   for (int d = 0; d < HD / 32; ++d) {
-    bf16x8 v[2];
-    bool bad = false;
-#pragma unroll
-    for (int jj = 0; jj < 2; ++jj) {
-      v[jj] = r.val(d, jj);
-      if (MASKED) v[jj] = clear_from(v[jj], 16 * jj + 8 * half, lim, bad);
+    bf16x8 v[2] = {r.val(d, 0), r.val(d, 1)};
+    uint32_t seen = 0;
+    if (MASKED) {
+      if (lim < kTile) {
+        v[0] = clear_from(v[0], 8 * half, lim);
+        v[1] = clear_from(v[1], 16 + 8 * half, lim);
+      }
+      seen = largest(largest(0, v[0]), v[1]);
     }
-    if (MASKED && __any(bad)) {
+    if (MASKED && __any(not_finite(seen))) {
       // A value that is not finite: 0 * it would reach slots that do not attend
       // to its position. It is taken out, and each slot that attends to one of
       // its kind gets one added.
@@ -286,17 +302,23 @@ SJD_DEV void start(WaveState<HD>& s) {
   s.l = 0.0f;
 }
 
-// Visible score registers of a lane with slot sl, for the tile of positions p0 ..
+// Visible score registers of a lane with slot sl, for the tile of positions p0 ..:
+// first as a mask of the tile's positions, which are visible up to the slot's own
+// row, or where the ancestor mask, moved to the window's place in the tile, says so
 SJD_DEV uint32_t visible(const PagedArgs& a, const Seq& sq, int p0, const Slot& sl) {
-  const int half = (threadIdx.x & 63) >> 5, nk = sq.cached + sq.rows;
-  uint32_t v = 0;
-#pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const int p = p0 + 16 * (i >> 3) + 8 * half + (i & 7), w = p - sq.cached;
-    const bool see = p < nk && (w < 0 || (a.anc ? (sl.mask >> (w & 63)) & 1 : w <= sl.row));
-    v |= (uint32_t)(sl.ok && see) << i;
+  auto below = [](int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; };  // positions 0 .. n - 1
+  const int d = sq.cached - p0;  // the window's first row is position d of the tile
+  uint32_t m;
+  if (a.anc) {
+    const uint32_t moved = d >= 32 ? 0u : d >= 0 ? (uint32_t)sl.mask << d : d > -64 ? (uint32_t)(sl.mask >> -d) : 0u;
+    m = (below(d) | moved) & below(d + sq.rows);
+  } else {
+    m = below(d + min(sl.row + 1, sq.rows));
   }
-  return v;
+  if (!sl.ok) m = 0;
+  // register i holds position 16 (i / 8) + 8 half + i % 8
+  m >>= 8 * ((threadIdx.x & 63) >> 5);
+  return (m & 0xFFu) | (m >> 8 & 0xFF00u);
 }
 
 // Few slots: 32 of one key / value head of one sequence per workgroup; its four
