@@ -62,10 +62,10 @@ struct RawKeys {
   uint32_t e;  // e4m3: exponent byte of the lane's key row, position swap23(lane % 32)
   SJD_DEV void load(const PagedArgs& a, const char* page, int h, int p0) {
     const int in = p0 & ((1 << a.pv.plen_log2) - 1), lane = threadIdx.x & 63;
-    const uint4* p = (const uint4*)(page + tile_off<HD, FP8 ? 1 : 2>(a.pv, h, in, 0)) + lane;
+    const char* p = page + tile_off<HD, FP8 ? 1 : 2>(a.pv, h, in, 0);
 #pragma unroll
-    for (int i = 0; i < N; ++i) x[i] = p[64 * i];
-    if constexpr (FP8) e = (uint8_t)page[exp_off<HD>(a.pv, h, 0) + in + swap23(lane & 31)];
+    for (int i = 0; i < N; ++i) x[i] = *(const uint4*)(p + (uint32_t)(16 * lane) + 1024 * i);
+    if constexpr (FP8) e = (uint8_t)(page + exp_off<HD>(a.pv, h, 0) + in)[(uint32_t)swap23(lane & 31)];
   }
   SJD_DEV bf16x8 key(int t) const {
     if constexpr (FP8) {
@@ -84,13 +84,13 @@ struct RawValues {
   uint2 e[2];  // e4m3: exponent bytes of positions 16 jj + 8 half + 0 .. 7, the score registers'
   SJD_DEV void load(const PagedArgs& a, const char* page, int h, int p0) {
     const int in = p0 & ((1 << a.pv.plen_log2) - 1), lane = threadIdx.x & 63;
-    const uint4* p = (const uint4*)(page + tile_off<HD, FP8 ? 1 : 2>(a.pv, h, in, 1)) + lane;
+    const char* p = page + tile_off<HD, FP8 ? 1 : 2>(a.pv, h, in, 1);
 #pragma unroll
-    for (int i = 0; i < N; ++i) x[i] = p[64 * i];
+    for (int i = 0; i < N; ++i) x[i] = *(const uint4*)(p + (uint32_t)(16 * lane) + 1024 * i);
     if constexpr (FP8) {
-      const char* q = page + exp_off<HD>(a.pv, h, 1) + in + 8 * (lane >> 5);
-      e[0] = *(const uint2*)q;
-      e[1] = *(const uint2*)(q + 16);
+      const char* q = page + exp_off<HD>(a.pv, h, 1) + in;
+      e[0] = *(const uint2*)(q + (uint32_t)((lane & 32) >> 2));
+      e[1] = *(const uint2*)(q + (uint32_t)((lane & 32) >> 2) + 16);
     }
   }
   SJD_DEV bf16x8 val(int d, int jj) const {
@@ -288,9 +288,10 @@ template <int HD>
 SJD_DEV uint4 load_q(const PagedArgs& a, const Slot& sl, int i) {
   const int half = (threadIdx.x & 63) >> 5;
   const uint32_t sign = a.negate ? 0x80008000u : 0u;
-  if (!sl.ok) return make_uint4(0, 0, 0, 0);
-  const uint4 x = ((const uint4*)(a.q + sl.t * a.q_row + sl.head * HD + half * (HD / 2)))[i];
-  return make_uint4(x.x ^ sign, x.y ^ sign, x.z ^ sign, x.w ^ sign);
+  // (a slot that is not there reads the window's first row: no branch, no wait)
+  const uint4 x = ((const uint4*)(a.q + sl.t * a.q_row + (sl.ok ? sl.head : 0) * HD + half * (HD / 2)))[i];
+  const uint32_t keep = sl.ok ? ~0u : 0u;
+  return make_uint4((x.x ^ sign) & keep, (x.y ^ sign) & keep, (x.z ^ sign) & keep, (x.w ^ sign) & keep);
 }
 template <int HD>
 SJD_DEV void start(WaveState<HD>& s) {
@@ -447,7 +448,9 @@ struct Stage {
   // piece i of this thread: tile, key or value, place in its part
   static SJD_DEV void where(int i, int& tile, int& kv, int& u) {
     static_assert(2 * HP % 256 == 0, "a round of the workgroup stays inside a tile");
-    const int tid = (int)threadIdx.x, n = i * 256;
+    int tid = (int)threadIdx.x;
+    const int n = i * 256;
+    asm volatile("" : "+v"(tid));  // (lane offsets are made anew: kept across the step they cost registers that it lacks)
     tile = n / (2 * HP);
     kv = HP >= 256 ? n / HP & 1 : __builtin_amdgcn_readfirstlane(tid / HP);
     u = HP >= 256 ? n % HP + tid : tid % HP;
@@ -463,15 +466,16 @@ struct Stage {
       const char* pg = tile ? page[1] : page[0];
       if (!pg) continue;
       const int in = (p0 + 32 * tile) & ((1 << a.pv.plen_log2) - 1);
-      const uint4* src = (const uint4*)(pg + tile_off<HD, ES>(a.pv, h, in, kv)) + u;
+      const uint4* src = (const uint4*)(pg + tile_off<HD, ES>(a.pv, h, in, kv)) + (uint32_t)u;
       if constexpr (FP8) {
         x[i] = *src;
         const char* ep = pg + exp_off<HD>(a.pv, h, kv) + in;
         if (kv) {
-          e[i][0] = *(const uint2*)(ep + 8 * ((u & 63) >> 5));
-          e[i][1] = *(const uint2*)(ep + 16 + 8 * ((u & 63) >> 5));
+          const uint2* e2 = (const uint2*)ep + (uint32_t)(u >> 5 & 1);
+          e[i][0] = e2[0];
+          e[i][1] = e2[2];
         } else {
-          e[i][0].x = (uint8_t)ep[swap23(u & 31)];
+          e[i][0].x = (uint8_t)ep[(uint32_t)swap23(u & 31)];
         }
       } else {
         // a wave's 1 KB lands in lane order behind a uniform address
@@ -520,16 +524,14 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(PagedArgs a) {
   constexpr int ND = HD / 32;
   using St = Stage<HD, FP8>;
   __shared__ uint4 lds[2][kStepTiles * St::TILE];
-  const int h = blockIdx.x % a.pv.Hkv, sp = blockIdx.x / a.pv.Hkv, z = blockIdx.z;
+  const int h = blockIdx.x, z = blockIdx.z;
   const Seq sq = load_seq(a.w, a.pv, z);
   // (the last slots of a causal window have the most keys: they start first)
   const int slots = sq.rows * a.G, f0 = ((int)gridDim.y - 1 - (int)blockIdx.y) * 128;
   if (f0 >= slots) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5;
   const int total = sq.cached + sq.rows;
-  const int nk = a.anc ? total : sq.cached + min(sq.rows - 1, (f0 + 127) / a.G) + 1;
-  const int beg = sp * a.chunk, end = min(nk, beg + a.chunk);
-  if (beg >= total) return;
+  const int end = a.anc ? total : sq.cached + min(sq.rows - 1, (f0 + 127) / a.G) + 1;
   const int w0 = f0 + 32 * wave;
   const Slot sl = slot_of(a, sq, h, w0 + (lane & 31));
   uint4 qr[HD / 16];
@@ -554,13 +556,13 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(PagedArgs a) {
   St st;
   const char* pg[kStepTiles];
   int id[kStepTiles];
-  ids(beg, id);
+  ids(0, id);
   pages(id, pg);
-  ids(beg + kStep, id);
-  st.load(a, pg, h, beg, lds[0]);
+  ids(kStep, id);
+  st.load(a, pg, h, 0, lds[0]);
   st.store(lds[0]);
   __syncthreads();
-  int buf = 0, p0 = beg;
+  int buf = 0, p0 = 0;
   // One step: the next one's loads, `work` on this one, and the loads' end
   auto step = [&](auto work) {
     const char* next[kStepTiles];
@@ -608,25 +610,14 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(PagedArgs a) {
   s.l += __shfl_xor(s.l, 32, kWave);
   if (!sl.ok) return;
   // register i of block d holds dim 32 d + 8 (i / 4) + 4 half + i % 4
-  if (a.splits == 1) {
-    const float inv = s.l == 0.0f ? 0.0f : 1.0f / s.l;  // (no key at all: zeros)
-    uint16_t* o = a.out + sl.t * a.out_row + sl.head * HD + 4 * half;
-#pragma unroll
-    for (int d = 0; d < ND; ++d)
-#pragma unroll
-      for (int i = 0; i < 16; i += 4)
-        *(uint2*)(o + d * 32 + 2 * i) = make_uint2(pk_bf16(s.o[d][i] * inv, s.o[d][i + 1] * inv),
-                                                   pk_bf16(s.o[d][i + 2] * inv, s.o[d][i + 3] * inv));
-    return;
-  }
-  const int64_t at = ((int64_t)sp * a.w.T + sl.t) * a.H + sl.head;
+  const float inv = s.l == 0.0f ? 0.0f : 1.0f / s.l;  // (no key at all: zeros)
+  uint16_t* o = a.out + sl.t * a.out_row + sl.head * HD + 4 * half;
 #pragma unroll
   for (int d = 0; d < ND; ++d)
 #pragma unroll
     for (int i = 0; i < 16; i += 4)
-      *(float4*)(a.ws_o + at * HD + d * 32 + 2 * i + 4 * half) =
-          make_float4(s.o[d][i], s.o[d][i + 1], s.o[d][i + 2], s.o[d][i + 3]);
-  if (half == 0) *(float2*)(a.ws_ml + at * 2) = make_float2(s.m, s.l);
+      *(uint2*)(o + d * 32 + 2 * i) = make_uint2(pk_bf16(s.o[d][i] * inv, s.o[d][i + 1] * inv),
+                                                 pk_bf16(s.o[d][i + 2] * inv, s.o[d][i + 3] * inv));
 }
 
 // Joins the splits of a row: one wave per (row, head).
@@ -683,23 +674,29 @@ void launch_head(const PagedArgs& a, const AttnPlan& pl, dim3 grid, hipStream_t 
 
 }  // namespace
 
-// Few slots: every wave its own keys. More: keys shared by four waves of slots.
-constexpr int kFewSlots = 32;
-
-// Keys per split. Few slots: enough workgroups for four rounds of two per compute
-// unit, so that sequences of unequal length even out, down to one tile per wave.
-// Many: as many as fill the compute units twice, of 256 keys at least.
+// Up to this many tiles of 32 slots the waves of a workgroup share out the keys;
+// more are many slots for one sequence and head, whose keys are worth sharing. us,
+// 32 query and 8 key / value heads of 128, e4m3 (bf16), keys shared out -> shared:
+//   1536 tiles (24 windows of 64 rows, 1239 cached)    39 (38) -> 78 (72)
+//   2048 tiles (32 of 64, 1239)                        52 (50) -> 50 (44)
+//   2048 tiles (32 of 64, 4172)                       117 (148) -> 139 (127)
+//   16384 tiles (1 of 4096, 4172)                     618 (656) -> 466 (436)
+// With up to 64 slots half of a 128-slot workgroup idles (64 of 16 rows, 4172: 115
+// -> 139).
+constexpr int kFewTiles = 1536;
+// Splits: as many as give two workgroups to each of 256 compute units, of one tile
+// per wave at least. More even out ragged sequences, but their partial outputs and
+// the second launch cost more: 64 single tokens over up to 8190 keys, 512 / 1024 /
+// 2048 workgroups: 140 / 148 / 156 us; 4 of them 18 / 23 / 31.
+constexpr int kSplitWgs = 512;
 AttnPlan paged_attention_plan(const sjd_pages& p, const sjd_windows& w, int H) {
   const int64_t most = (int64_t)w.max_cached + w.max_rows;
   const int64_t slots = (int64_t)w.max_rows * (H / p.n_kv_heads);
-  const bool few = slots <= kFewSlots;
-  const int64_t wgs = (int64_t)w.B * p.n_kv_heads * (few ? 1 : (slots + 127) / 128);
-  const int64_t target = few ? 2048 : 512, least = few ? 128 : 256;
-  int64_t S = (target + wgs - 1) / wgs;
-  const int64_t cap = (most + least - 1) / least;
-  if (S > cap) S = cap;
-  if (S < 1) S = 1;
-  const int64_t chunk = ((most + S - 1) / S + 127) / 128 * 128;
+  const int64_t tiles = (int64_t)w.B * p.n_kv_heads * ((slots + 31) / 32);
+  const bool few = slots <= 64 || tiles <= kFewTiles;
+  int64_t S = few ? (kSplitWgs + tiles - 1) / tiles : 1;
+  if (S > (most + kRound - 1) / kRound) S = (most + kRound - 1) / kRound;
+  const int64_t chunk = ((most + S - 1) / S + kRound - 1) / kRound * kRound;
   return AttnPlan{(int)chunk, (int)((most + chunk - 1) / chunk), few};
 }
 

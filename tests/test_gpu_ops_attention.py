@@ -11,9 +11,14 @@ pytestmark = pytest.mark.gpu
 
 
 class Case:
-    """Sequences (rows, cached), their pages filled by sjd_kv_append, and q."""
+    """Sequences (rows, cached), their pages filled by sjd_kv_append, and q.
+    many: with so many empty sequences behind them that a launch counts as one of
+    many query slots (keys shared by 128 slots rather than shared out)."""
 
-    def __init__(self, seqs, plen, Hkv, G, hd, cache, seed=0, gap=2, scale=1.0, fill=0xFF):
+    def __init__(self, seqs, plen, Hkv, G, hd, cache, seed=0, gap=2, scale=1.0, fill=0xFF, many=False):
+        if many:
+            tiles = Hkv * -(-max(r for r, _ in seqs) * G // 32)
+            seqs = seqs + [(0, 0)] * (1536 // tiles + 1)
         self.seqs, self.Hkv, self.G, self.H, self.hd, self.cache = seqs, Hkv, G, Hkv * G, hd, cache
         self.plen = plen
         self.table, n_pages = table_for(seqs, plen, seed)
@@ -99,11 +104,22 @@ def test_causal(seqs, hd, Hkv, G, plen, cache):
 
 
 @pytest.mark.parametrize("cache", ["e4m3", "bf16"])
+@pytest.mark.parametrize("hd,Hkv,G,plen", [(128, 2, 4, 64), (64, 3, 3, 32), (128, 1, 7, 128), (64, 2, 16, 1024)])
+@pytest.mark.parametrize("seqs", [[(32, 333), (7, 64), (31, 0)], [(33, 1000), (64, 5), (0, 9)], [(130, 0), (1, 259)],
+                                  [(300, 421)], [(65, 64), (64, 128)]], ids=[str(i) for i in range(5)])
+def test_causal_many_slots(seqs, hd, Hkv, G, plen, cache):
+    c = Case(seqs, plen, Hkv, G, hd, cache, scale=2.0, many=True)
+    assert sjd.attention_workspace(c.pool.pages, c.windows(), c.H).numel() == 0
+    c.check(c.run())
+
+
+@pytest.mark.parametrize("many", [False, True])
+@pytest.mark.parametrize("cache", ["e4m3", "bf16"])
 @pytest.mark.parametrize("hd,Hkv,G", [(128, 1, 4), (64, 2, 2), (128, 2, 1)])
-def test_tree(hd, Hkv, G, cache):
+def test_tree(hd, Hkv, G, cache, many):
     """Ancestor masks: any of them, also of later rows, rows without any bit
     (and, with nothing cached, without any key: zeros), bits behind the window."""
-    c = Case([(64, 700), (5, 0), (33, 31), (64, 0)], 32, Hkv, G, hd, cache)
+    c = Case([(64, 700), (5, 0), (33, 31), (64, 0)], 32, Hkv, G, hd, cache, many=many)
     g = np.random.RandomState(3)
     anc = g.randint(0, 2 ** 32, c.T).astype(np.uint64) << np.uint64(32) | g.randint(0, 2 ** 32, c.T).astype(np.uint64)
     anc[c.seq[0][0]:c.seq[0][0] + 40] = [(1 << (i + 1)) - 1 for i in range(40)]
@@ -145,8 +161,9 @@ def test_strided_rows():
     assert bool((out[:, :16] == 3.0).all()) and bool((out[:, 16 + c.H * 64:] == 3.0).all())
 
 
-def test_pages_outside_the_pool_are_left_out():
-    c = Case([(40, 130), (1, 300)], 64, 2, 4, 64, "e4m3")
+@pytest.mark.parametrize("many", [False, True])
+def test_pages_outside_the_pool_are_left_out(many):
+    c = Case([(40, 130), (1, 300)], 64, 2, 4, 64, "e4m3", many=many)
     c.tt[:, 1] = 1 << 28
     c.check(c.run(), left_out=[(64, 128)])
     c.tt.fill_(-1)
@@ -155,17 +172,18 @@ def test_pages_outside_the_pool_are_left_out():
         assert not out[first:first + r].any()
 
 
-def test_wrong_sequences_are_left_out():
-    c = Case([(4, 60), (3, 10), (2, 5), (1, 9)], 32, 1, 2, 64, "bf16")
+@pytest.mark.parametrize("many", [False, True])
+def test_wrong_sequences_are_left_out(many):
+    c = Case([(40, 60), (3, 10), (2, 5), (1, 9)], 32, 1, 2, 64, "bf16", many=many)
     c.st[1] = torch.tensor([c.T - 2, 3, 10, 0])
     c.st[2] = torch.tensor([c.seq[2][0], 2, -1, 0])
     c.check(c.run(), skip=(1, 2))
 
 
 @pytest.mark.parametrize("cache", ["e4m3", "bf16"])
-@pytest.mark.parametrize("rows", [40, 200])
-def test_non_finite_values_reach_only_rows_that_attend(cache, rows):
-    c = Case([(rows, 70)], 32, 1, 2, 64, cache)
+@pytest.mark.parametrize("rows,many", [(40, False), (200, False), (40, True), (200, True)])
+def test_non_finite_values_reach_only_rows_that_attend(cache, rows, many):
+    c = Case([(rows, 70)], 32, 1, 2, 64, cache, many=many)
     clean = c.run()
     bad = 23  # window row whose key and value are not finite
     p = 70 + bad
@@ -198,10 +216,11 @@ def test_non_finite_values_reach_only_rows_that_attend(cache, rows):
         assert bool(torch.isfinite(out.float()).all())
 
 
-def test_large_scores_and_lowest_values():
+@pytest.mark.parametrize("many", [False, True])
+def test_large_scores_and_lowest_values(many):
     """Scores of some thousands (one key takes all), and keys of bf16's lowest
     value, whose scores are huge or minus infinity."""
-    c = Case([(3, 200)], 32, 1, 1, 64, "bf16", scale=200.0)
+    c = Case([(33 if many else 3, 200)], 32, 1, 3 if many else 1, 64, "bf16", scale=200.0, many=many)
     c.check(c.run())
     c.q.abs_()
     c.k[0][5:60] = torch.finfo(torch.bfloat16).min
@@ -214,6 +233,8 @@ def test_runs_agree_and_follow_their_stream():
     """The same call twice, and on another stream behind its inputs' copies:
     the same bits."""
     c = Case([(32, 900), (1, 2000)], 64, 2, 4, 128, "e4m3")
+    m = Case([(32, 900), (1, 2000)], 64, 2, 4, 128, "e4m3", many=True)
+    assert torch.equal(m.run(), m.run())
     a = c.run()
     assert torch.equal(a, c.run())
     s = torch.cuda.Stream()
