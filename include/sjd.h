@@ -91,6 +91,20 @@ typedef enum {
  * changed, if one is found. sjd_verify: in sjd_verify_params.flags;
  * decoder contexts: in sjd_config.flags. */
 #define SJD_CHECK_FINITE 32u
+/* decoder contexts only: caches in pages (see sjd_pages) instead of two bf16
+ * planes, and attention by sjd_paged_attention. SJD_KV_E4M3 holds keys and values
+ * in 8 bits with a power of two per row and head, a quarter of the default's
+ * memory; with SJD_ROPE_GRID alone the pages are bf16. Rows of q, k and v are rounded
+ * to bf16 before they are placed. SJD_EINVAL together with SJD_TUNE, whose
+ * timings are those of the default path. */
+#define SJD_KV_E4M3 128u
+/* decoder contexts only: image tokens are placed by time, row and column
+ * (sjd_rope_axes) instead of along one axis. The prompt's tokens take their
+ * position on all three; generated token g, with a prompt of n_p tokens, takes n_p,
+ * n_p + g / (row_len + 1) and n_p + g % (row_len + 1). Of a head's pairs of dims (by
+ * falling frequency rope_theta^(-2i / head_dim)) the first quarter turns by time, of
+ * the others those with even i by row and those with odd i by column. Needs row_len >= 1 (SJD_EINVAL otherwise). */
+#define SJD_ROPE_GRID 256u
 /* sjd_verify_given only: the row behind a window's last draft holds the
  * target's probabilities too, and a window whose drafts are all accepted
  * commits one more token, drawn from it */
@@ -393,7 +407,7 @@ typedef struct {
   int32_t L, K, D;       /* window slots (1..64), candidates per depth (1..8), depth   */
   uint32_t flags;        /* SJD_AC | SJD_PD (0 = vanilla SJD; Sec. 5.3's ablation),
                             optionally | SJD_EAGER | SJD_NO_TUNE | SJD_TUNE |
-                            SJD_CHECK_FINITE                                              */
+                            SJD_CHECK_FINITE | SJD_KV_E4M3 | SJD_ROPE_GRID                */
   float rms_eps, rope_theta;
   int32_t eol_id, row_len;
   int32_t weights_f32;   /* 1: weights are fp32, 0: bf16                                */

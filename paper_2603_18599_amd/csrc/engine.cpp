@@ -17,6 +17,7 @@
 #include <vector>
 
 #include "forward.h"
+#include "ops.h"
 #include "sjd.h"
 #include "step.h"
 #include "verify.h"
@@ -64,6 +65,17 @@ struct Ctx {
   int nstreams = 1;
   size_t kv_elems = 0;
   int delta[sjd::kMaxStreams] = {0, 0, 0, 0};  // per image (host copy, for the cache-fill bound)
+  // caches in pages (SJD_KV_E4M3, SJD_ROPE_GRID) instead of the planes above: one
+  // pool per layer, every stream's pages in it under one table
+  bool paged = false, grid = false;
+  sjd_pages pages{};        // layer 0's; layer l's pool lies l * pool_bytes behind it
+  int64_t pool_bytes = 0;
+  int page_cols = 0;        // pages of a stream
+  int32_t* ptable = nullptr;
+  int32_t *pseq = nullptr, *ppos = nullptr;  // [kMaxStreams][4], [Mpad][axes]
+  uint16_t *qkv_rows = nullptr, *att_rows = nullptr;  // [Mpad][q, k, v], [Mpad][q]
+  void* attn_ws = nullptr;
+  sjd_rope_params rp{};
   float2* rope = nullptr;
   float* logits[2] = {nullptr, nullptr};
   // target-row statistics of the step that wrote logits[i] ([B][L]); the
@@ -147,7 +159,10 @@ int check_config(const sjd_config* c) {
   if (c->L < 1 || c->L > 64 || c->K < 1 || c->K > 8 || c->D < 0 || (long)c->K * c->D > c->L) return SJD_EINVAL;
   if (c->V > 65536) return SJD_ENOTSUP;
   if (c->max_seq < c->L + 2) return SJD_EINVAL;
-  if (c->flags & ~(SJD_AC | SJD_PD | SJD_EAGER | SJD_NO_TUNE | SJD_TUNE | SJD_CHECK_FINITE)) return SJD_EINVAL;
+  if (c->flags & ~(SJD_AC | SJD_PD | SJD_EAGER | SJD_NO_TUNE | SJD_TUNE | SJD_CHECK_FINITE | SJD_KV_E4M3 | SJD_ROPE_GRID))
+    return SJD_EINVAL;
+  if ((c->flags & (SJD_KV_E4M3 | SJD_ROPE_GRID)) && (c->flags & SJD_TUNE)) return SJD_EINVAL;
+  if ((c->flags & SJD_ROPE_GRID) && c->row_len < 1) return SJD_EINVAL;
   if (!(c->rms_eps > 0.0f) || !(c->rope_theta > 0.0f)) return SJD_EINVAL;
   if (!std::isfinite(c->cfg_w)) return SJD_EINVAL;
   if (c->batch < 0) return SJD_EINVAL;
@@ -199,6 +214,48 @@ constexpr int kWideHeadV = 192 * 256;
 // results have the same bits, so the host's estimate of the fill may lag.
 constexpr int kWholeFill = 2 * sjd::kAttnChunk;
 
+// The new rows of a window and the caches that they go to: every stream's, or (a
+// prompt) stream `cache`'s.
+sjd_windows page_windows(const Ctx& x, int M, bool prompt, int cache) {
+  sjd_windows w{};
+  w.B = prompt ? 1 : x.nstreams;
+  w.T = x.Mpad;
+  w.max_rows = prompt ? M : x.c.L;
+  w.max_cached = x.cap;  // (one launch shape for every fill: steps are replayed)
+  w.table_len = x.page_cols;
+  w.d_seq = x.pseq;
+  w.d_table = x.ptable + (size_t)(prompt ? cache : 0) * x.page_cols;
+  return w;
+}
+
+// Attention of a context with paged caches, from QKV partial planes to activation
+// tiles: rows, their places, the cache, the attention over it.
+int paged_layer(Ctx& x, int l, int S, size_t plane, int M, int mt, bool prompt, int cache, hipStream_t s) {
+  const sjd_config& c = x.c;
+  const int hd = c.head_dim, Nq = c.n_heads * hd, Nkv = c.n_kv_heads * hd, N = Nq + 2 * Nkv;
+  HIPTRY(sjd::launch_plane_rows(x.qkv, S, plane, M, N, x.qkv_rows, s));
+  sjd_rope_params rp = x.rp;
+  rp.T = M;
+  const sjd_rope_io rio{x.qkv_rows, x.qkv_rows + Nq, x.ppos, x.qkv_rows, x.qkv_rows + Nq};
+  HIPTRY(sjd::launch_rope_axes(rp, rio, s));
+  sjd_pages p = x.pages;
+  p.d_pool = (char*)x.pages.d_pool + l * x.pool_bytes;
+  const sjd_windows w = page_windows(x, M, prompt, cache);
+  const sjd_kv_rows kv{x.qkv_rows + Nq, x.qkv_rows + Nq + Nkv, N, N, SJD_BF16};
+  HIPTRY(sjd::launch_kv_append(p, w, kv, s));
+  sjd_attention_io io{};
+  io.H = c.n_heads;
+  io.scale = (float)(1.0 / std::sqrt((double)hd));
+  io.d_q = x.qkv_rows;
+  io.d_out = x.att_rows;
+  io.q_row = N;
+  io.out_row = Nq;
+  io.d_anc = prompt ? nullptr : x.win->anc;
+  HIPTRY(sjd::launch_paged_attention(p, w, io, x.attn_ws, s));
+  HIPTRY(sjd::launch_row_tiles(x.att_rows, M, Nq, x.att, mt, s));
+  return SJD_OK;
+}
+
 enum { kProjQkv = 0, kProjO = 1, kProjGu = 2, kProjDown = 3 };
 
 // Window forward of M rows: two streams (sm.mode != kStreamsOne, see
@@ -216,6 +273,10 @@ int forward(Ctx& x, int M, const int32_t* prompt, const int32_t* n_dev, int n_ho
   in.vis_lo = c.vis_lo; in.sm = sm; in.win = x.win; in.E = x.embed; in.d = d; in.vocab = c.vocab_size; in.x = x.x;
   in.g = x.lw[0][0]; in.y = x.xn; in.mtiles = mt; in.ss = x.ss; in.fours = x.fours;
   HIPTRY(sjd::launch_window_in(in, s));
+  if (x.paged) {
+    const sjd::PageWindow pw{x.win, in.st, n_host, M, c.L, x.grid ? 1 : 0, c.row_len, sm, x.pseq, x.ppos};
+    HIPTRY(sjd::launch_page_window(pw, s));
+  }
   const size_t qplane = (size_t)x.Mpad * Nqkv, rplane = (size_t)x.Mpad * d, guplane = (size_t)x.Mpad * 2 * F;
   int pend = 0;  // partial planes of the last residual projection not yet added into x
   // (prefill rows take the 64-row plan in windows of any length, so that a row's
@@ -275,9 +336,13 @@ int forward(Ctx& x, int M, const int32_t* prompt, const int32_t* n_dev, int n_ho
     g.A = x.xn; g.mtiles = mt; g.M = M; g.W = w[1]; g.N = Nqkv; g.K = d; g.S = P[kProjQkv].S;
     g.wide = P[kProjQkv].wide; g.out = x.qkv; g.plane = qplane; g.ldo = Nqkv;
     HIPTRY(sjd::launch_gemm(g, s));
-    HIPTRY(sjd::launch_rope_kv(x.qkv, P[kProjQkv].S, qplane, x.win, n_dev, n_host, M, H, Hkv, hd, x.rope, kv, x.cap_pad,
-                               sm, s));
-    HIPTRY(sjd::launch_attention(a, hd, s));
+    if (x.paged) {
+      TRY(paged_layer(x, l, P[kProjQkv].S, qplane, M, mt, prompt != nullptr, cache, s));
+    } else {
+      HIPTRY(sjd::launch_rope_kv(x.qkv, P[kProjQkv].S, qplane, x.win, n_dev, n_host, M, H, Hkv, hd, x.rope, kv,
+                                 x.cap_pad, sm, s));
+      HIPTRY(sjd::launch_attention(a, hd, s));
+    }
     g = plain;
     g.A = x.att; g.mtiles = mt; g.M = M; g.W = w[4]; g.N = d; g.K = Nq; g.S = P[kProjO].S;
     g.wide = P[kProjO].wide; g.out = x.rpart; g.plane = rplane; g.ldo = d;
@@ -494,6 +559,51 @@ int cache_check(Ctx& x) {
   return SJD_OK;
 }
 
+// Pools, tables and row buffers of a context with paged caches.
+int page_buffers(Ctx& x, hipStream_t s) {
+  const sjd_config& c = x.c;
+  const int hd = c.head_dim, Nq = c.n_heads * hd, N = Nq + 2 * c.n_kv_heads * hd, P = hd / 2;
+  constexpr int kPageLen = 64;
+  x.page_cols = x.cap_pad / kPageLen;
+  const int n_pages = x.page_cols * x.nstreams;
+  x.pages = sjd_pages{nullptr, n_pages, kPageLen, c.n_kv_heads, hd, c.flags & SJD_KV_E4M3 ? SJD_E4M3 : SJD_BF16};
+  x.pool_bytes = sjd::page_bytes(x.pages) * n_pages;
+  char* pool = nullptr;
+  // scratch of the largest launch: a step's, or a prompt's window of any length
+  int64_t ws = sjd::paged_attention_ws(x.pages, page_windows(x, 0, false, 0), c.n_heads);
+  for (int M = 1; M <= x.Mpad; ++M) {
+    const int64_t n = sjd::paged_attention_ws(x.pages, page_windows(x, M, true, 0), c.n_heads);
+    ws = n > ws ? n : ws;
+  }
+  char* w = nullptr;
+  TRY(dalloc(x, &pool, (size_t)x.pool_bytes * c.n_layers));
+  TRY(dalloc(x, &w, (size_t)ws));
+  TRY(dalloc(x, &x.ptable, (size_t)n_pages));
+  TRY(dalloc(x, &x.pseq, 4 * sjd::kMaxStreams));
+  TRY(dalloc(x, &x.ppos, 3 * (size_t)x.Mpad));
+  TRY(dalloc(x, &x.qkv_rows, (size_t)x.Mpad * N));
+  TRY(dalloc(x, &x.att_rows, (size_t)x.Mpad * Nq));
+  x.pages.d_pool = pool;
+  x.attn_ws = w;
+  std::vector<int32_t> table(n_pages);
+  for (int i = 0; i < n_pages; ++i) table[i] = i;
+  // (rows between two streams are read, and never matter: they stay finite)
+  if (hipMemcpyAsync(x.ptable, table.data(), table.size() * 4, hipMemcpyHostToDevice, s) != hipSuccess ||
+      hipMemsetAsync(x.ppos, 0, 12 * (size_t)x.Mpad, s) != hipSuccess ||
+      hipMemsetAsync(x.att_rows, 0, (size_t)x.Mpad * Nq * 2, s) != hipSuccess || hipStreamSynchronize(s) != hipSuccess)
+    return SJD_EHIP;
+  // places: pairs by frequency; with a grid the highest quarter turns by time, the
+  // rest by row and column in turn
+  x.rp.H = c.n_heads; x.rp.Hkv = c.n_kv_heads; x.rp.head_dim = hd; x.rp.pairs = P;
+  x.rp.axes = x.grid ? 3 : 1; x.rp.dtype = SJD_BF16;
+  x.rp.q_row = x.rp.k_row = x.rp.out_q_row = x.rp.out_k_row = N;
+  for (int i = 0; i < P; ++i) {
+    x.rp.freq[i] = std::pow((double)c.rope_theta, -2.0 * i / hd);
+    x.rp.axis[i] = (uint8_t)(!x.grid || i < P / 4 ? 0 : 1 + (i & 1));
+  }
+  return SJD_OK;
+}
+
 }  // namespace
 
 struct sjd_ctx {
@@ -530,7 +640,9 @@ extern "C" int sjd_init(const sjd_config* cfg, const sjd_weights* w, void* strea
   // weights: copied into library memory; matrices repacked into the GEMM
   // tile layout (bf16), fp32 inputs rounded to nearest even
   const int f32 = c.weights_f32 ? 1 : 0;
-  x.fused = fused_shape(c) && !(c.flags & SJD_TUNE);
+  x.paged = (c.flags & (SJD_KV_E4M3 | SJD_ROPE_GRID)) != 0;
+  x.grid = (c.flags & SJD_ROPE_GRID) != 0;
+  x.fused = fused_shape(c) && !(c.flags & SJD_TUNE) && !x.paged;
   auto copy_rows = [&](const void* p, size_t count, const uint16_t** dst) -> int {
     uint16_t* b = nullptr;
     int rc = dalloc(x, &b, count);
@@ -588,7 +700,7 @@ extern "C" int sjd_init(const sjd_config* cfg, const sjd_weights* w, void* strea
   // work buffers
   const int Mp = x.Mpad;
   x.kv_elems = (size_t)c.n_layers * Hkv * x.cap_pad * hd;
-  const size_t kv = x.kv_elems * x.nstreams;  // every stream's caches
+  const size_t kv = x.paged ? 0 : x.kv_elems * x.nstreams;  // every stream's caches
   const size_t xnsz = sjd::act_elems(d, x.mtiles), attsz = sjd::act_elems(Nq, x.mtiles),
                hsz = sjd::act_elems(F, x.mtiles);
   if ((rc = dalloc(x, &x.x, (size_t)Mp * d)) ||
@@ -605,6 +717,7 @@ extern "C" int sjd_init(const sjd_config* cfg, const sjd_weights* w, void* strea
       (rc = dalloc(x, &x.win, 1)) || (rc = dalloc(x, &x.rec, (size_t)x.B * c.L * sjd::kRecInts)) ||
       (rc = dalloc(x, &x.nonfinite, 16)))
     return fail(rc);
+  if (x.paged && (rc = page_buffers(x, s))) return fail(rc);
   x.att = x.xn + xnsz;
   x.hbuf = x.att + attsz;
   x.zeros = x.hbuf + hsz;
@@ -987,8 +1100,11 @@ extern "C" int sjd_step(sjd_ctx* h, const int32_t* d_draft_tok, const float* d_d
   HIPTRY(sjd::launch_verify(a, o, s));
   const sjd::KvPlanes all{nullptr, nullptr, x.kc, x.kc_lo, x.vt, x.vt_lo, x.kv_elems};
   const int slot = (int)(x.steps % kRing);
-  HIPTRY(sjd::launch_step_end(x.st, x.win, all, c.n_layers, c.n_kv_heads, c.head_dim, x.cap_pad, c.K, x.nstreams,
-                              x.guided, d_out_meta, d_out_tok, d_out_next, c.L, x.B, x.h_n_dev + slot * x.B, s));
+  if (x.paged)
+    HIPTRY(sjd::launch_page_commit(x.st, x.win, x.pages, x.pool_bytes, c.n_layers, x.ptable, x.page_cols, c.K,
+                                   x.nstreams, x.guided, s));
+  HIPTRY(sjd::launch_step_end(x.st, x.win, all, c.n_layers, c.n_kv_heads, c.head_dim, x.cap_pad, c.K,
+                              x.paged ? 0 : x.nstreams, x.guided, d_out_meta, d_out_tok, d_out_next, c.L, x.B, x.h_n_dev + slot * x.B, s));
   HIPTRY(hipEventRecord(x.ev[slot], s));
   x.ev_step[slot] = x.steps;
   x.steps += 1;

@@ -4,6 +4,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "forward.h"
 #include "sjd.h"
 
 namespace sjd {
@@ -85,6 +86,29 @@ AttnPlan paged_attention_plan(const sjd_pages& p, const sjd_windows& w, int H);
 int64_t paged_attention_ws(const sjd_pages& p, const sjd_windows& w, int H);
 hipError_t launch_paged_attention(const sjd_pages& p, const sjd_windows& w, const sjd_attention_io& io, void* ws,
                                   hipStream_t s);
+
+// ---- decoder contexts whose caches are pages (paged_step.hip)
+// A window's sequences and places: seq[z] = { row0, rows, cached, 0 } of stream z,
+// pos[m] = the row's position, or with grid { time, row, column } of it: a text
+// token's position three times; image token g (the first one at position n_p): n_p,
+// n_p + g / (row_len + 1), n_p + g % (row_len + 1).
+struct PageWindow {
+  const Window* win;
+  const DevState* st;  // NULL: rows of a prompt from position `start` on, all of them text
+  int start, M, L, grid, row_len;
+  Streams sm;
+  int32_t* seq;
+  int32_t* pos;
+};
+hipError_t launch_page_window(const PageWindow& a, hipStream_t s);
+// rows[m][0 .. N) = bf16 of the sum of S fp32 partial planes (N a multiple of 4)
+hipError_t launch_plane_rows(const float* part, int S, size_t plane, int M, int N, uint16_t* rows, hipStream_t s);
+// bf16 rows [M][K] into activation tiles (K a multiple of 64; the lo planes are zero)
+hipError_t launch_row_tiles(const uint16_t* rows, int M, int K, uint16_t* y, int mtiles, hipStream_t s);
+// An accepted sibling's key and value move to their place in the sequence, in every
+// layer's pool (launch_step_end's move, for pages). pool_bytes: from layer to layer.
+hipError_t launch_page_commit(const DevState* st, const Window* win, const sjd_pages& p, int64_t pool_bytes, int layers,
+                              const int32_t* table, int table_len, int K, int nstreams, bool guided, hipStream_t s);
 
 hipError_t launch_rope_axes(const sjd_rope_params& p, const sjd_rope_io& io, hipStream_t s);
 hipError_t launch_verify_given(const sjd_given_params& p, const sjd_given_io& io, hipStream_t s);

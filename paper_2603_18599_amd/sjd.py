@@ -19,6 +19,8 @@ SJD_NO_TUNE = 8
 SJD_TUNE = 16
 SJD_CHECK_FINITE = 32
 SJD_FULL_SELECT = 64
+SJD_KV_E4M3 = 128
+SJD_ROPE_GRID = 256
 SJD_BONUS = 512
 SJD_VERIFY_NOALLOC_MAX_ROWS = 131072
 
