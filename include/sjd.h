@@ -261,8 +261,7 @@ typedef struct {
 
 /* Outputs must not overlap inputs. A window whose n lies outside [0, L] is not
  * verified: its meta becomes {-1, -1, 0, 0} and its other outputs are left as
- * they were. Nothing is allocated; rows of 16-byte aligned buffers whose
- * strides are multiples of 4 are read fastest. */
+ * they were. Nothing is allocated. */
 SJD_API int sjd_verify_given(const sjd_given_params* params, const sjd_given_io* io, void* stream);
 
 /* ------------------------------------------------------------------------ */

@@ -2,11 +2,11 @@
 // uniforms (definition: sjd.h).
 //
 // Bound by memory: only a row that is drawn from needs more than two of its
-// entries, and it needs p and q once. One workgroup takes a drawn row: each of 16
-// waves sums a contiguous stretch of it in 64 bits, with 8 16-byte loads per lane in
-// flight; the stretch that holds r * total is read again (it lies in the cache),
-// 4 entries to a lane, and a wave finds the token in its 256. Differences and
-// products of floats are exact or rounded once in 64 bits, so another summation
+// entries, and it needs p and q once. One workgroup of W waves takes a drawn row:
+// each wave sums a contiguous stretch of it in 64 bits, with 8 16-byte loads per
+// lane in flight; the stretch that holds r * total is read again (it lies in the
+// cache), 4 entries to a lane, and a wave finds the token in its 256. Differences
+// and products of floats are exact or rounded once in 64 bits, so another summation
 // order moves a draw only where r * total lies within some 1e-15 of the total from
 // a border.
 #include "device.h"
@@ -16,8 +16,6 @@ namespace sjd {
 
 namespace {
 
-constexpr int kThreads = 1024, kWaves = kThreads / kWave;
-
 struct GivenArgs {
   sjd_given_params p;
   sjd_given_io io;
@@ -25,8 +23,13 @@ struct GivenArgs {
 
 SJD_DEV double wave_sum64(double v) { return wave_sum_d_dpp(v); }
 
-// The weights of a row. VEC: its entries start on 16 bytes
-template <bool VEC>
+// Four entries of a row, which may start on any float (16-byte loads need 4-byte
+// alignment only)
+struct Four {
+  float x, y, z, w;
+};
+
+// The weights of a row
 struct Row {
   const float *p, *q;  // q NULL: p alone, but for entry `skip`
   int V, skip;
@@ -35,11 +38,11 @@ struct Row {
     return d > 0.0 ? d : 0.0;  // (NaN: 0)
   }
   // entries x .. x + 3, those from `end` on as zeros
-  SJD_DEV void four(int x, int end, float4& a, float4& b) const {
-    a = b = make_float4(0, 0, 0, 0);
-    if (VEC && x + 4 <= end) {
-      a = *(const float4*)(p + x);
-      if (q) b = *(const float4*)(q + x);
+  SJD_DEV void four(int x, int end, Four& a, Four& b) const {
+    a = b = Four{0, 0, 0, 0};
+    if (x + 4 <= end) {
+      a = *(const Four*)(p + x);
+      if (q) b = *(const Four*)(q + x);
     } else {
       float* u = &a.x;
       float* v = &b.x;
@@ -51,7 +54,7 @@ struct Row {
         }
     }
   }
-  SJD_DEV void weights(int x, const float4& a, const float4& b, double (&w)[4]) const {
+  SJD_DEV void weights(int x, const Four& a, const Four& b, double (&w)[4]) const {
     w[0] = weight(x, a.x, b.x);
     w[1] = weight(x + 1, a.y, b.y);
     w[2] = weight(x + 2, a.z, b.z);
@@ -61,7 +64,7 @@ struct Row {
   SJD_DEV double sum(int lo, int hi) const {
     double s = 0.0;
     for (int x0 = lo + 4 * (int)(threadIdx.x & 63); x0 < hi; x0 += 16 * kWave) {
-      float4 a[4], b[4];
+      Four a[4], b[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) four(x0 + 4 * kWave * i, hi, a[i], b[i]);
 #pragma unroll
@@ -75,92 +78,113 @@ struct Row {
   }
 };
 
+template <int W>
 struct DrawSmem {
-  double part[2][kWaves];
+  double part[2][W];
   int tok;
 };
 
+// The first of n parts whose end lies above the target (parts from `before` on), else
+// (r * total rounded up to the total) the last one with mass; `before` becomes what
+// lies before it.
+template <int N>
+SJD_DEV int find(const double* part, double target, double& before) {
+  double cum = before, at = before, last_at = before;
+  int pick = -1, last = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const double s = part[i];
+    if (s > 0.0) {
+      last = i;
+      last_at = cum;
+      if (pick < 0 && cum + s > target) {
+        pick = i;
+        at = cum;
+      }
+    }
+    cum += s;
+  }
+  before = pick < 0 ? last_at : at;
+  return pick < 0 ? last : pick;
+}
+
 // Least x with cum(x) > r * total, or -1 for a row without mass (every thread
-// gets the result).
-template <bool VEC>
-SJD_DEV int draw(const Row<VEC>& w, float r, DrawSmem& sm) {
+// gets the result). Rounds of sums narrow the row down to what the waves can hold in
+// registers, 1024 entries each; that round ends in one wave.
+template <int W>
+SJD_DEV int draw(const Row& w, float r, DrawSmem<W>& sm) {
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  constexpr int kPart = 4 * kWave;  // entries of a wave in the last round
-  auto split = [](int len) { return ((len + kWaves - 1) / kWaves + kPart - 1) / kPart * kPart; };
+  constexpr int kGroup = 4 * kWave, kGroups = 4, kPart = kGroups * kGroup;
+  // entries per wave; a round leaves at most the W-th part of what it began with, or
+  // kPart (a row for one wave has no more than that)
+  auto split = [](int len) { return ((len + W - 1) / W + kPart - 1) / kPart * kPart; };
   int round = 0;
   double target = 0.0, before = 0.0;
-  // The part that holds the target: the first whose end lies above it, else (r *
-  // total rounded up to the total) the last one with mass.
-  auto find = [&](const double* part) {
-    double cum = before, at = before, last_at = before;
-    int pick = -1, last = 0;
-    for (int i = 0; i < kWaves; ++i) {
-      const double s = part[i];
-      if (s > 0.0) {
-        last = i;
-        last_at = cum;
-        if (pick < 0 && cum + s > target) {
-          pick = i;
-          at = cum;
-        }
-      }
-      cum += s;
-    }
-    before = pick < 0 ? last_at : at;
-    return pick < 0 ? last : pick;
-  };
   int base = 0, end = w.V, len = split(w.V);
-  // rounds of sums (two buffers: a round's sums are read while the next one writes
-  // its own, and the barrier between them is enough)
+  // (two buffers: a round's sums are read while the next one writes its own, and the
+  // barrier between them is enough)
   for (;; len = split(len)) {
     const int lo = min(base + wave * len, end), hi = min(lo + len, end);
     double* part = sm.part[round & 1];
-    double x[4], s;
+    double x[kGroups][4], own[kGroups], group[kGroups], s = 0.0;
     if (len > kPart) {
       s = w.sum(lo, hi);
     } else {
-      float4 a, b;
-      const int at = lo + 4 * lane;
-      w.four(at, hi, a, b);
-      w.weights(at, a, b, x);
-      s = wave_sum64((x[0] + x[1]) + (x[2] + x[3]));
+      Four a[kGroups], b[kGroups];
+#pragma unroll
+      for (int i = 0; i < kGroups; ++i) w.four(lo + kGroup * i + 4 * lane, hi, a[i], b[i]);
+#pragma unroll
+      for (int i = 0; i < kGroups; ++i) {
+        w.weights(lo + kGroup * i + 4 * lane, a[i], b[i], x[i]);
+        own[i] = (x[i][0] + x[i][1]) + (x[i][2] + x[i][3]);
+        group[i] = lo + kGroup * i < hi ? wave_sum64(own[i]) : 0.0;
+        s += group[i];
+      }
     }
     if (lane == 0) part[wave] = s;
     __syncthreads();
     if (round++ == 0) {
       double total = 0.0;
-      for (int i = 0; i < kWaves; ++i) total += part[i];
+      for (int i = 0; i < W; ++i) total += part[i];
       if (!(total > 0.0)) {
         __syncthreads();  // (a draw that follows writes the same buffer)
         return -1;
       }
       target = (double)r * total;
     }
-    const int pick = find(part);
+    const int pick = find<W>(part, target, before);
     if (len > kPart) {
       base += pick * len;
       end = min(base + len, end);
       continue;
     }
     if (wave == pick) {
-      const double own = (x[0] + x[1]) + (x[2] + x[3]);
-      double cum = own;
+      const int g = find<kGroups>(group, target, before);
+      double y[4] = {}, mine = 0.0;
+#pragma unroll
+      for (int i = 0; i < kGroups; ++i)
+        if (i == g) {
+          mine = own[i];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) y[e] = x[i][e];
+        }
+      double cum = mine;
 #pragma unroll
       for (int o = 1; o < kWave; o <<= 1) {
         const double u = __shfl_up(cum, o, kWave);
         if (lane >= o) cum += u;
       }
-      const uint64_t above = __ballot(own > 0.0 && before + cum > target), some = __ballot(own > 0.0);
+      const uint64_t above = __ballot(mine > 0.0 && before + cum > target), some = __ballot(mine > 0.0);
       if (lane == (above ? __builtin_ctzll(above) : 63 - __builtin_clzll(some))) {
-        double c = before + (cum - own);
+        double c = before + (cum - mine);
         int t = -1, last = 0;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          c += x[i];
-          if (x[i] > 0.0) last = i;
-          if (t < 0 && x[i] > 0.0 && c > target) t = i;
+          c += y[i];
+          if (y[i] > 0.0) last = i;
+          if (t < 0 && y[i] > 0.0 && c > target) t = i;
         }
-        sm.tok = lo + 4 * lane + (t < 0 ? last : t);
+        sm.tok = lo + kGroup * g + 4 * lane + (t < 0 ? last : t);
       }
     }
     __syncthreads();
@@ -183,9 +207,9 @@ SJD_DEV bool accepts(const GivenArgs& a, int b, int j, int* x) {
 }
 
 // Token drawn at row j (drafts: the residual; x < 0 or row n: p itself)
-template <bool VEC>
-SJD_DEV int draw_row(const GivenArgs& a, int b, int j, bool residual, int x, DrawSmem& sm) {
-  Row<VEC> w{a.io.d_p + b * a.p.p_win + j * a.p.p_row, nullptr, a.p.V, -1};
+template <int W>
+SJD_DEV int draw_row(const GivenArgs& a, int b, int j, bool residual, int x, DrawSmem<W>& sm) {
+  Row w{a.io.d_p + b * a.p.p_win + j * a.p.p_row, nullptr, a.p.V, -1};
   const float r = a.io.d_r[(int64_t)b * (a.p.L + 1) + j];
   int t = -1;
   if (residual) {
@@ -205,9 +229,9 @@ SJD_DEV int drafts_of(const GivenArgs& a, int b) {
 }
 
 // One window: up to its first rejection.
-template <bool VEC>
-__global__ __launch_bounds__(kThreads) void k_given_chain(GivenArgs a) {
-  __shared__ DrawSmem sm;
+template <int W>
+__global__ __launch_bounds__(W * kWave) void k_given_chain(GivenArgs a) {
+  __shared__ DrawSmem<W> sm;
   __shared__ int s_first, s_x;
   const int b = blockIdx.x, L = a.p.L, n = drafts_of(a, b);
   int32_t* meta = a.io.d_meta + 4 * (int64_t)b;
@@ -227,25 +251,26 @@ __global__ __launch_bounds__(kThreads) void k_given_chain(GivenArgs a) {
   __syncthreads();
   const int first = s_first;
   const bool drawn = first < n || (a.p.flags & SJD_BONUS);
-  const int t = drawn ? draw_row<VEC>(a, b, first, first < n && s_x >= 0, s_x, sm) : -1;
+  const int t = drawn ? draw_row<W>(a, b, first, first < n && s_x >= 0, s_x, sm) : -1;
   const int n_c = first + (drawn ? 1 : 0);
-  if (j <= L)
-    a.io.d_tok[(int64_t)b * (L + 1) + j] = j < first ? a.io.d_draft[(int64_t)b * L + j] : j < n_c ? t : -1;
-  if (j < L && a.io.d_next) a.io.d_next[(int64_t)b * L + j] = -1;
+  for (int i = j; i <= L; i += W * kWave) {  // (L + 1 may be one more than a wave)
+    a.io.d_tok[(int64_t)b * (L + 1) + i] = i < first ? a.io.d_draft[(int64_t)b * L + i] : i < n_c ? t : -1;
+    if (i < L && a.io.d_next) a.io.d_next[(int64_t)b * L + i] = -1;
+  }
   if (j == 0) *(int4*)meta = make_int4(n_c, first < n ? first : -1, first, 0);
 }
 
 // Adaptive continuation: every row by itself, its token (the draft, or what was
 // drawn) into d_tok.
-template <bool VEC>
-__global__ __launch_bounds__(kThreads) void k_given_rows(GivenArgs a) {
-  __shared__ DrawSmem sm;
+template <int W>
+__global__ __launch_bounds__(W * kWave) void k_given_rows(GivenArgs a) {
+  __shared__ DrawSmem<W> sm;
   const int rows = a.p.L + (a.p.flags & SJD_BONUS ? 1 : 0);
   const int b = blockIdx.x / rows, j = blockIdx.x % rows, n = drafts_of(a, b);
   if (j > n || (j == n && rows == a.p.L)) return;
   int x = -1, t;
   if (j < n && accepts(a, b, j, &x)) t = a.io.d_draft[(int64_t)b * a.p.L + j];
-  else t = draw_row<VEC>(a, b, j, j < n && x >= 0, x, sm);
+  else t = draw_row<W>(a, b, j, j < n && x >= 0, x, sm);
   if (threadIdx.x == 0) a.io.d_tok[(int64_t)b * (a.p.L + 1) + j] = t;
 }
 // The rows' tokens into committed ones and next drafts (the accept tests, two
@@ -276,24 +301,27 @@ __global__ __launch_bounds__(128) void k_given_end(GivenArgs a) {
   if (j == 0) *(int4*)meta = make_int4(n_c, first < n ? first : -1, first, carried);
 }
 
+template <int W>
+void launch(const GivenArgs& a, hipStream_t s) {
+  if (a.p.flags & SJD_AC) {
+    const int rows = a.p.L + (a.p.flags & SJD_BONUS ? 1 : 0);
+    hipLaunchKernelGGL(k_given_rows<W>, dim3(a.p.B * rows), dim3(W * kWave), 0, s, a);
+    hipLaunchKernelGGL(k_given_end, dim3(a.p.B), dim3(128), 0, s, a);
+  } else {
+    hipLaunchKernelGGL(k_given_chain<W>, dim3(a.p.B), dim3(W * kWave), 0, s, a);
+  }
+}
+
 }  // namespace
 
 hipError_t launch_verify_given(const sjd_given_params& p, const sjd_given_io& io, hipStream_t s) {
   const GivenArgs a{p, io};
-  auto fine = [](const float* x, int64_t row, int64_t win) {
-    return ((uintptr_t)x & 15) == 0 && row % 4 == 0 && win % 4 == 0;
-  };
-  const bool vec = fine(io.d_p, p.p_row, p.p_win) && (!io.d_q || fine(io.d_q, p.q_row, p.q_win));
-  if (p.flags & SJD_AC) {
-    const int rows = p.L + (p.flags & SJD_BONUS ? 1 : 0);
-    if (vec) hipLaunchKernelGGL(k_given_rows<true>, dim3(p.B * rows), dim3(kThreads), 0, s, a);
-    else hipLaunchKernelGGL(k_given_rows<false>, dim3(p.B * rows), dim3(kThreads), 0, s, a);
-    hipLaunchKernelGGL(k_given_end, dim3(p.B), dim3(128), 0, s, a);
-  } else if (vec) {
-    hipLaunchKernelGGL(k_given_chain<true>, dim3(p.B), dim3(kThreads), 0, s, a);
-  } else {
-    hipLaunchKernelGGL(k_given_chain<false>, dim3(p.B), dim3(kThreads), 0, s, a);
-  }
+  // Waves per row: 1024 entries each are one round. us with 1 / 4 / 16 of them: 6475
+  // rows of 236 entries 9.5 / 15 / 62; 3190 of 5795 - / 17 / 37; 1000 of 12000 - / 27 /
+  // 34; 32 of 16384 - / 11.6 / 9.6; 256 of 65536 - / 44 / 27 (134 MB: 5.0 TB/s).
+  if (p.V <= 1024) launch<1>(a, s);
+  else if (p.V <= 12288) launch<4>(a, s);
+  else launch<16>(a, s);
   return hipGetLastError();
 }
 

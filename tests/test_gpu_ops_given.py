@@ -38,7 +38,9 @@ def inputs(B, L, V, seed, bonus, support=None, agree=1.0):
 @pytest.mark.parametrize("ac", [False, True])
 @pytest.mark.parametrize("bonus", [False, True])
 @pytest.mark.parametrize("B,L,V,support", [(1, 1, 1, None), (3, 1, 7, None), (5, 8, 65, None), (9, 4, 1023, 5),
-                                           (2, 33, 1025, None), (2, 64, 4096, 300), (3, 2, 65536, None), (2, 3, 70001, 9)])
+                                           (2, 33, 1025, None), (2, 64, 4096, 300), (3, 2, 65536, None), (2, 3, 70001, 9),
+                                           (40, 64, 1024, 40), (2, 3, 4097, None), (2, 2, 12288, 2000),
+                                           (2, 2, 12289, None), (1, 2, 262145, None)])
 def test_given(B, L, V, support, bonus, ac):
     for certain in (False, True):
         p, q, draft, n, u, r = inputs(B, L, V, B * V + L, bonus, support)
