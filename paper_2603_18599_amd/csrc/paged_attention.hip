@@ -58,6 +58,7 @@ SJD_DEV bf16x8 bf16_of_e4m3(uint2 c, float scale) {
 template <int HD, bool FP8>
 struct RawKeys {
   static constexpr int N = FP8 ? HD / 32 : HD / 16;
+  static constexpr bool kCodes = FP8;
   uint4 x[N];
   uint32_t e;  // e4m3: exponent byte of the lane's key row, position swap23(lane % 32)
   SJD_DEV void load(const PagedArgs& a, const char* page, int h, int p0) {
@@ -79,7 +80,7 @@ struct RawKeys {
 template <int HD, bool FP8>
 struct RawValues {
   static constexpr int N = FP8 ? HD / 32 : HD / 16;
-  static constexpr bool kScaled = FP8;  // the operands lack their rows' powers of two
+  static constexpr bool kCodes = FP8;  // (and the operands lack their rows' powers of two)
   uint4 x[N];
   uint2 e[2];  // e4m3: exponent bytes of positions 16 jj + 8 half + 0 .. 7, the score registers'
   SJD_DEV void load(const PagedArgs& a, const char* page, int h, int p0) {
@@ -110,7 +111,7 @@ struct RawValues {
 // Both of a tile in LDS, widened to bf16: [key steps, then value blocks][lane]
 template <int HD>
 struct LdsTile {
-  static constexpr bool kScaled = false;
+  static constexpr bool kCodes = false;
   const uint4* at;
   SJD_DEV bf16x8 key(int t) const { return __builtin_bit_cast(bf16x8, at[64 * t + (threadIdx.x & 63)]); }
   SJD_DEV bf16x8 val(int d, int jj) const {
@@ -161,7 +162,9 @@ SJD_DEV void scores(f32x16& c, const Keys& k, const Q& q, uint32_t vis) {
 #pragma unroll
   for (int i = 0; i < 16; ++i) c[i] = 0.0f;
 #pragma unroll
-  for (int t = 0; t < HD / 16; ++t) c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k.key(t), q(t), c, 0, 0, 0);
+  for (int t = 0; t < HD / 16; ++t) {
+    c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k.key(t), q(t), c, 0, 0, 0);
+  }
   if (MASKED)
 #pragma unroll
     for (int i = 0; i < 16; ++i) c[i] = (vis >> i) & 1 ? c[i] : -INFINITY;
@@ -211,7 +214,7 @@ SJD_DEV void weigh(WaveState<HD>& s, f32x16 (&c)[N], float scale, const uint32_t
 // anything.
 template <int HD, bool MASKED, class Values>
 SJD_DEV void collect(WaveState<HD>& s, f32x16& c, const Values& r, uint32_t vis, int lim) {
-  if constexpr (Values::kScaled)
+  if constexpr (Values::kCodes)
 #pragma unroll
     for (int i = 0; i < 16; ++i)  // (a masked position's exponent byte may be anything)
       c[i] = MASKED && !((vis >> i) & 1) ? 0.0f : c[i] * r.power(i);
@@ -264,6 +267,7 @@ SJD_DEV void collect(WaveState<HD>& s, f32x16& c, const Values& r, uint32_t vis,
     }
 #pragma unroll
     for (int jj = 0; jj < 2; ++jj) s.o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[jj], p[jj], s.o[d], 0, 0, 0);
+
   }
 }
 
@@ -357,10 +361,16 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn(PagedArgs a) {
   const Slot sl = slot_of(a, sq, h, f0 + (lane & 31));
   RawKeys<HD, FP8> k;
   RawValues<HD, FP8> v;
-  const char* page = p0 < end ? page_at(a.pv, id) : nullptr;
-  if (page) {
-    k.load(a, page, h, p0);
-    v.load(a, page, h, p0);
+  bool ok;  // (a tile that is left out holds the pool's first one: loads without a branch)
+  auto source = [&](bool inside, int page) {
+    const char* pg = inside ? page_at(a.pv, page) : nullptr;
+    ok = pg != nullptr;
+    return ok ? pg : a.pv.pool;
+  };
+  {
+    const char* pg = source(p0 < end, id);
+    k.load(a, pg, h, p0);
+    v.load(a, pg, h, p0);
   }
 #pragma unroll
   for (int i = wave; i < HD / 16; i += 4) sm.q[i][lane] = load_q<HD>(a, sl, i);
@@ -368,24 +378,28 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn(PagedArgs a) {
   start(s);
   __syncthreads();
   const auto q = [&](int t) { return __builtin_bit_cast(bf16x8, sm.q[t][lane]); };
-  // A tile (page NULL: left out): the next tile's keys are loaded into the registers
-  // of this one's once the scores are formed, its values once they are used up.
+  // One tile, and the loads of the next one into its registers: the keys' once the
+  // scores are formed, the values' once they are used up. (A second set of registers
+  // for them is no faster at 64 dims and spills at 128.)
   auto step = [&](auto masked) {
     constexpr bool MASKED = decltype(masked)::value;
-    const int np = p0 + kRound;
-    const char* next = np < end ? page_at(a.pv, id_next) : nullptr;
+    const bool now = ok;
+    const int p = p0, np = p0 + kRound;
+    const char* next = source(np < end, id_next);
     id_next = id_of(np + kRound);
-    const uint32_t vis[1] = {MASKED && page ? visible(a, sq, p0, sl) : 0xFFFFu};
-    f32x16 c[1];
-    if (page) scores<HD, MASKED>(c[0], k, q, vis[0]);
-    if (next) k.load(a, next, h, np);
-    if (page) {
-      weigh<HD, 1, MASKED>(s, c, a.scale, vis);
-      collect<HD, MASKED>(s, c[0], v, vis[0], total - p0);
-    }
-    if (next) v.load(a, next, h, np);
-    page = next;
     p0 = np;
+    if (!now) {
+      k.load(a, next, h, np);
+      v.load(a, next, h, np);
+      return;
+    }
+    const uint32_t vis[1] = {MASKED ? visible(a, sq, p, sl) : 0xFFFFu};
+    f32x16 c[1];
+    scores<HD, MASKED>(c[0], k, q, vis[0]);
+    k.load(a, next, h, np);
+    weigh<HD, 1, MASKED>(s, c, a.scale, vis);
+    collect<HD, MASKED>(s, c[0], v, vis[0], total - p);
+    v.load(a, next, h, np);
   };
   while (p0 + kTile <= full) step(std::false_type{});
   while (p0 < end) step(std::true_type{});
