@@ -275,10 +275,10 @@ typedef enum { SJD_F32 = 0, SJD_BF16 = 1, SJD_E4M3 = 2 } sjd_dtype;
 
 /* Rotary positions with several axes (an image token's time, row and column).
  * Pair i of a head (dims i and pairs + i) turns by
- *   phi = pos[t][axis[i]] * freq[i]   (formed in 64 bits)
+ *   phi = pos[t][h_axis[i]] * h_freq[i]   (formed in 64 bits)
  * so (a, b) becomes (a cos - b sin, b cos + a sin); dims from 2 * pairs on pass
  * through. `inverse` turns back. Sections of pairs per axis, interleaved axes, and
- * frequencies that start anew on each axis are all choices of axis and freq. */
+ * frequencies that start anew on each axis are all choices of h_axis and h_freq. */
 typedef struct {
   int32_t T;        /* rows, 0 .. 2^24                                              */
   int32_t H, Hkv;   /* heads of q and of k, >= 0; 0: that tensor is not there        */
@@ -289,8 +289,8 @@ typedef struct {
   int32_t inverse;  /* 0 or 1                                                       */
   int64_t q_row, k_row, out_q_row, out_k_row; /* elements between rows (heads lie one
                        behind the other), >= heads * head_dim                        */
-  double freq[128];
-  uint8_t axis[128]; /* < axes                                                       */
+  const double* h_freq;  /* [pairs] finite; host arrays, read during the call           */
+  const uint8_t* h_axis; /* [pairs] < axes                                              */
 } sjd_rope_params;
 
 typedef struct {

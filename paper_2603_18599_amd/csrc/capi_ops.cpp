@@ -36,8 +36,9 @@ int check_rope(const sjd_rope_params* p, const sjd_rope_io* io) {
     return SJD_EINVAL;
   if (p->axes < 1 || p->axes > 4 || (p->inverse != 0 && p->inverse != 1)) return SJD_EINVAL;
   if (p->dtype != SJD_F32 && p->dtype != SJD_BF16) return SJD_EINVAL;
+  if (!p->h_freq || !p->h_axis) return SJD_EINVAL;
   for (int i = 0; i < p->pairs; ++i)
-    if (p->axis[i] >= p->axes || !std::isfinite(p->freq[i])) return SJD_EINVAL;
+    if (p->h_axis[i] >= p->axes || !std::isfinite(p->h_freq[i])) return SJD_EINVAL;
   if (p->T == 0) return SJD_OK;
   const uintptr_t es = p->dtype == SJD_F32 ? 4 : 2;
   if (!io->d_pos || !aligned(io->d_pos, 4)) return SJD_EINVAL;

@@ -76,6 +76,8 @@ struct Ctx {
   uint16_t *qkv_rows = nullptr, *att_rows = nullptr;  // [Mpad][q, k, v], [Mpad][q]
   void* attn_ws = nullptr;
   sjd_rope_params rp{};
+  double rope_freq[64];
+  uint8_t rope_axis[64];
   float2* rope = nullptr;
   float* logits[2] = {nullptr, nullptr};
   // target-row statistics of the step that wrote logits[i] ([B][L]); the
@@ -597,9 +599,11 @@ int page_buffers(Ctx& x, hipStream_t s) {
   x.rp.H = c.n_heads; x.rp.Hkv = c.n_kv_heads; x.rp.head_dim = hd; x.rp.pairs = P;
   x.rp.axes = x.grid ? 3 : 1; x.rp.dtype = SJD_BF16;
   x.rp.q_row = x.rp.k_row = x.rp.out_q_row = x.rp.out_k_row = N;
+  x.rp.h_freq = x.rope_freq;
+  x.rp.h_axis = x.rope_axis;
   for (int i = 0; i < P; ++i) {
-    x.rp.freq[i] = std::pow((double)c.rope_theta, -2.0 * i / hd);
-    x.rp.axis[i] = (uint8_t)(!x.grid || i < P / 4 ? 0 : 1 + (i & 1));
+    x.rope_freq[i] = std::pow((double)c.rope_theta, -2.0 * i / hd);
+    x.rope_axis[i] = (uint8_t)(!x.grid || i < P / 4 ? 0 : 1 + (i & 1));
   }
   return SJD_OK;
 }

@@ -98,8 +98,8 @@ hipError_t launch_rope_axes(const sjd_rope_params& p, const sjd_rope_io& io, hip
   a.T = p.T; a.H = p.H; a.Hkv = p.Hkv; a.hd = p.head_dim; a.pairs = p.pairs; a.axes = p.axes;
   a.sign = p.inverse ? -1.0f : 1.0f;
   for (int i = 0; i < p.pairs; ++i) {
-    a.rev[i] = p.freq[i] / 6.283185307179586476925286766559;
-    a.axis[i] = p.axis[i];
+    a.rev[i] = p.h_freq[i] / 6.283185307179586476925286766559;
+    a.axis[i] = p.h_axis[i];
   }
   // rows per workgroup: as many as give each thread one angle, unless that
   // leaves compute units without rows

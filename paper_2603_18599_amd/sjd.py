@@ -77,7 +77,7 @@ class RopeParams(C.Structure):
     _fields_ = [("T", C.c_int32), ("H", C.c_int32), ("Hkv", C.c_int32), ("head_dim", C.c_int32),
                 ("pairs", C.c_int32), ("axes", C.c_int32), ("dtype", C.c_int32), ("inverse", C.c_int32),
                 ("q_row", C.c_int64), ("k_row", C.c_int64), ("out_q_row", C.c_int64), ("out_k_row", C.c_int64),
-                ("freq", C.c_double * 128), ("axis", C.c_uint8 * 128)]
+                ("h_freq", C.c_void_p), ("h_axis", C.c_char_p)]
 
 
 class RopeIO(C.Structure):
@@ -307,26 +307,26 @@ def sjd_rope_axes(q, k, pos, freq, axis, *, out_q=None, out_k=None, inverse=Fals
     fn = "sjd_rope_axes"
     torch, types = _types()
     x = q if q is not None else k
-    P = len(freq)
-    _expect(fn, x is not None and x.dim() == 3 and pos.dim() == 2 and 1 <= P <= 128 and len(axis) == P)
+    _expect(fn, x is not None and x.dim() == 3 and pos.dim() == 2 and len(axis) == len(freq))
     (T, _, hd), dt, dev, axes = x.shape, x.dtype, x.get_device(), pos.shape[1]
-    par = RopeParams(T, 0, 0, hd, P, axes, types.get(dt, -1), 1 if inverse else 0)
-    C.memmove(C.byref(par, RopeParams.freq.offset), array("d", freq).tobytes(), 8 * P)
-    C.memmove(C.byref(par, RopeParams.axis.offset), bytes(axis), P)
-    io = RopeIO(None, None, _dense(fn, pos, (T, axes), torch.int32, dev))
-    if q is not None:
-        o = q if out_q is None else out_q
-        _expect(fn, o.dtype is dt and o.get_device() == dev)
-        par.H = H = q.shape[1]
-        par.q_row, par.out_q_row = _row_stride(fn, q, T, H, hd), _row_stride(fn, o, T, H, hd)
-        io.d_q, io.d_out_q = q.data_ptr(), o.data_ptr()
-    if k is not None:
-        o = k if out_k is None else out_k
-        _expect(fn, k.dim() == 3 and k.dtype is dt and k.get_device() == dev and o.dtype is dt and
-                o.get_device() == dev)
-        par.Hkv = H = k.shape[1]
-        par.k_row, par.out_k_row = _row_stride(fn, k, T, H, hd), _row_stride(fn, o, T, H, hd)
-        io.d_k, io.d_out_k = k.data_ptr(), o.data_ptr()
+    f, ax = array("d", freq), bytes(axis)
+
+    def rows(t, out):  # heads, strides and addresses of a tensor and of what it becomes
+        if t is None:
+            return 0, 0, 0, None, None
+        _expect(fn, t.dim() == 3 and t.dtype is dt and t.get_device() == dev)
+        H = t.shape[1]
+        stride, at = _row_stride(fn, t, T, H, hd), t.data_ptr()
+        if out is None or out is t:
+            return H, stride, stride, at, at
+        _expect(fn, out.dtype is dt and out.get_device() == dev)
+        return H, stride, _row_stride(fn, out, T, H, hd), at, out.data_ptr()
+
+    H, q_row, out_q_row, qp, out_qp = rows(q, out_q)
+    Hkv, k_row, out_k_row, kp, out_kp = rows(k, out_k)
+    par = RopeParams(T, H, Hkv, hd, len(f), axes, types.get(dt, -1), 1 if inverse else 0, q_row, k_row, out_q_row,
+                     out_k_row, f.buffer_info()[0], ax)
+    io = RopeIO(qp, kp, _dense(fn, pos, (T, axes), torch.int32, dev), out_qp, out_kp)
     _launch(fn, stream, dev, C.byref(par), C.byref(io))
 
 

@@ -46,12 +46,15 @@ def rope(par=None, io=None, axis=None, freq=None):
     i = dict(d_q=P, d_k=P, d_pos=P, d_out_q=2 * P, d_out_k=2 * P)
     p.update(par or {})
     i.update(io or {})
-    s = sjd.RopeParams(**p)
+    n = max(p["pairs"], 1)
+    f, a = (C.c_double * n)(*[1.0] * n), (C.c_uint8 * n)()
     for k, v in (axis or {}).items():
-        s.axis[k] = v
+        a[k] = v
     for k, v in (freq or {}).items():
-        s.freq[k] = v
-    return call("sjd_rope_axes", C.byref(s), C.byref(sjd.RopeIO(**i)), None)
+        f[k] = v
+    p.setdefault("h_freq", C.addressof(f))
+    p.setdefault("h_axis", C.cast(a, C.c_char_p))
+    return call("sjd_rope_axes", C.byref(sjd.RopeParams(**p)), C.byref(sjd.RopeIO(**i)), None)
 
 
 @pytest.mark.parametrize("par", [dict(T=-1), dict(T=(1 << 24) + 1), dict(H=-1), dict(H=0, Hkv=0), dict(H=2000),
@@ -65,6 +68,7 @@ def test_rope_refuses_parameters(par):
 def test_rope_refuses_tables_and_buffers():
     assert rope(axis={31: 3}) == -1
     assert rope(freq={0: float("inf")}) == -1
+    assert rope(dict(h_freq=None)) == -1 and rope(dict(h_axis=None)) == -1
     for io in (dict(d_q=None), dict(d_k=None), dict(d_pos=None), dict(d_out_q=None), dict(d_out_k=None),
                dict(d_q=P + 1), dict(d_out_k=P + 1), dict(d_pos=P + 2)):
         assert rope(None, io) == -1, io
