@@ -644,34 +644,40 @@ __global__ __launch_bounds__(256) void k_paged_join(PagedArgs a) {
   const int hh = i % a.H;
   const int n = (sq.cached + sq.rows + a.chunk - 1) / a.chunk;
   const int64_t at = t * a.H + hh, step = (int64_t)a.w.T * a.H;
-  // 64 splits at a time: a lane reads one split's statistics, then every lane its
-  // dims of each of them
-  constexpr int W = HD / 64;
+  // 64 splits at a time: a lane reads one split's statistics and every lane its dims of
+  // each of them, the first 8 before anything waits for the statistics
+  constexpr int W = HD / 64, kBatch = 8;
   float m = -INFINITY, l = 0.0f, v[W] = {};
   for (int k0 = 0; k0 < n; k0 += kWave) {
-    const float2 ml = k0 + lane < n ? *(const float2*)(a.ws_ml + (at + (k0 + lane) * step) * 2) : make_float2(-INFINITY, 0.0f);
-    const float mx = fmaxf(m, wave_max_dpp(ml.x));
-    const float f = mx == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ml.x - mx);
-    const float old = mx == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - mx);
-    l = l * old + wave_sum(k0 + lane < n ? ml.y * f : 0.0f);
-#pragma unroll
-    for (int e = 0; e < W; ++e) v[e] *= old;
-    m = mx;
     const int c = min(kWave, n - k0);
-    for (int k = 0; k < c; k += 8) {
-      float x[8][W];
+    const float2 ml = lane < c ? *(const float2*)(a.ws_ml + (at + (k0 + lane) * step) * 2) : make_float2(-INFINITY, 0.0f);
+    float x[kBatch][W];
+    auto read = [&](int k) {
 #pragma unroll
-      for (int u = 0; u < 8; ++u)
+      for (int u = 0; u < kBatch; ++u)
 #pragma unroll
         for (int e = 0; e < W; ++e)
           x[u][e] = k + u < c ? a.ws_o[(at + (k0 + k + u) * step) * HD + lane * W + e] : 0.0f;
+    };
+    read(0);
+    const float mx = fmaxf(m, wave_max_dpp(ml.x));
+    const float f = mx == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ml.x - mx);
+    const float old = mx == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - mx);
+    l = l * old + wave_sum(lane < c ? ml.y * f : 0.0f);
 #pragma unroll
-      for (int u = 0; u < 8; ++u)
+    for (int e = 0; e < W; ++e) v[e] *= old;
+    m = mx;
+    for (int k = 0;;) {
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u)
         if (k + u < c) {
           const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), k + u));
 #pragma unroll
           for (int e = 0; e < W; ++e) v[e] += x[u][e] * w;
         }
+      k += kBatch;
+      if (k >= c) break;
+      read(k);
     }
   }
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
