@@ -104,6 +104,9 @@ SJD_DEV int val_byte(int i, int j) {
   return FP8 ? (64 * (j >> 5) + lane) * 16 + 8 * (i >> 4) + (i & 7)
              : (((j >> 5) * 2 + (i >> 4)) * 64 + lane) * 16 + (i & 7) * 2;
 }
+// Its place in LDS: 16 bytes more every 256, which spreads the 8 threads of a row (256
+// and 1024 bytes apart) over the banks
+SJD_DEV int pad(int b) { return b + ((b >> 8) << 4); }
 template <bool FP8>
 SJD_DEV int piece_pos(int u) {
   const int hi = ((u & 63) >> 5) * 8;
@@ -126,7 +129,7 @@ struct CacheArgs {
 template <int HD, bool FP8, bool F32>
 __global__ __launch_bounds__(256) void k_kv_append(CacheArgs a) {
   constexpr int ES = FP8 ? 1 : 2, N = HD / 8;
-  __shared__ __align__(16) char vs[32 * HD * ES];
+  __shared__ __align__(16) char vs[32 * HD * ES * 17 / 16];
   const int z = blockIdx.z, h = blockIdx.y;
   const Seq sq = load_seq(a.w, a.pv, z);
   const int p0 = ((sq.cached >> 5) + (int)blockIdx.x) << 5;
@@ -158,7 +161,7 @@ __global__ __launch_bounds__(256) void k_kv_append(CacheArgs a) {
       }
     }
 #pragma unroll
-    for (int e = 0; e < N; ++e) vs[val_byte<true>(i, c * N + e)] = (char)(vc[e / 4] >> (8 * (e & 3)));
+    for (int e = 0; e < N; ++e) vs[pad(val_byte<true>(i, c * N + e))] = (char)(vc[e / 4] >> (8 * (e & 3)));
   } else {
 #pragma unroll
     for (int g = 0; g < N / 8; ++g) {
@@ -168,11 +171,11 @@ __global__ __launch_bounds__(256) void k_kv_append(CacheArgs a) {
       if (ok) store_row<false, 8>(kt + 1024 * g, 0, x);
     }
 #pragma unroll
-    for (int e = 0; e < N; ++e) *(uint16_t*)(vs + val_byte<false>(i, c * N + e)) = f32_to_bf16(vf[e]);
+    for (int e = 0; e < N; ++e) *(uint16_t*)(vs + pad(val_byte<false>(i, c * N + e))) = f32_to_bf16(vf[e]);
   }
   __syncthreads();
   for (int u = threadIdx.x; u < 2 * HD * ES; u += 256) {
-    const uint4 x = *(const uint4*)(vs + 16 * u);
+    const uint4 x = *(const uint4*)(vs + pad(16 * u));
     const int p = piece_pos<FP8>(u);
     char* d = vt + 16 * u;
     if (lo == 0 && hi == 32) {
@@ -193,7 +196,7 @@ __global__ __launch_bounds__(256) void k_kv_append(CacheArgs a) {
 template <int HD, bool FP8, bool F32>
 __global__ __launch_bounds__(256) void k_kv_read(CacheArgs a) {
   constexpr int ES = FP8 ? 1 : 2, N = HD / 8;
-  __shared__ __align__(16) char vs[32 * HD * ES];
+  __shared__ __align__(16) char vs[32 * HD * ES * 17 / 16];
   const int z = blockIdx.z, h = blockIdx.y;
   const Seq sq = load_seq(a.w, a.pv, z);
   const int p0 = ((sq.cached >> 5) + (int)blockIdx.x) << 5;
@@ -208,7 +211,7 @@ __global__ __launch_bounds__(256) void k_kv_read(CacheArgs a) {
   if (page) {
     const char* kt = page + tile_off<HD, ES>(a.pv, h, in, 0) + key_byte<HD, FP8>(i, c);
     const char* vt = page + tile_off<HD, ES>(a.pv, h, in, 1);
-    for (int u = threadIdx.x; u < 2 * HD * ES; u += 256) *(uint4*)(vs + 16 * u) = *(const uint4*)(vt + 16 * u);
+    for (int u = threadIdx.x; u < 2 * HD * ES; u += 256) *(uint4*)(vs + pad(16 * u)) = *(const uint4*)(vt + 16 * u);
     if constexpr (FP8) {
       const float ks = exp_scale((uint8_t)page[exp_off<HD>(a.pv, h, 0) + in + i]);
       const float vsc = exp_scale((uint8_t)page[exp_off<HD>(a.pv, h, 1) + in + i]);
@@ -223,7 +226,7 @@ __global__ __launch_bounds__(256) void k_kv_read(CacheArgs a) {
       for (int e = 0; e < N; e += 4) {
         uint32_t w = 0;
 #pragma unroll
-        for (int b = 0; b < 4; ++b) w |= (uint32_t)(uint8_t)vs[val_byte<true>(i, c * N + e + b)] << (8 * b);
+        for (int b = 0; b < 4; ++b) w |= (uint32_t)(uint8_t)vs[pad(val_byte<true>(i, c * N + e + b))] << (8 * b);
         decode4(w, vsc, vf + e);
       }
     } else {
@@ -236,7 +239,7 @@ __global__ __launch_bounds__(256) void k_kv_read(CacheArgs a) {
       }
       __syncthreads();
 #pragma unroll
-      for (int e = 0; e < N; ++e) vf[e] = bf16_to_f32(*(const uint16_t*)(vs + val_byte<false>(i, c * N + e)));
+      for (int e = 0; e < N; ++e) vf[e] = bf16_to_f32(*(const uint16_t*)(vs + pad(val_byte<false>(i, c * N + e))));
     }
   }
   if (!ok) return;
