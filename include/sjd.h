@@ -375,7 +375,10 @@ SJD_API int sjd_kv_read(const sjd_pages* pages, const sjd_windows* win, const sj
  * max_rows <= 64). A row that attends to nothing gives zeros. Query head h uses
  * key / value head h / (H / n_kv_heads). Scores, statistics and sums are held in 32
  * bits; probabilities enter the value product as bf16, relative to the row's
- * running maximum. Non-finite keys and values reach only rows that attend to them.
+ * reference maximum; the sums are divided at the end, so values within a factor of
+ * the number of keys of the largest float overflow. Non-finite keys and values reach
+ * only rows that attend to them. SJD_ENOTSUP for windows of more than 65535 * 128
+ * query slots (max_rows * H / n_kv_heads).
  * d_ws: sjd_paged_attention_workspace() bytes of scratch, 256-byte aligned (NULL
  * when that is 0); it holds nothing between calls, and calls that overlap in time
  * need one each. */

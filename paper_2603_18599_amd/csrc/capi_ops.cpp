@@ -100,8 +100,10 @@ int check_rows(const sjd_pages* p, const sjd_windows* w, const sjd_kv_rows* r) {
     if (_rc != SJD_OK) return _rc; \
   } while (0)
 
-int check_heads(const sjd_pages* p, int32_t H) {
-  return H >= 1 && H <= 1024 && H % p->n_kv_heads == 0 ? SJD_OK : SJD_EINVAL;
+int check_heads(const sjd_pages* p, const sjd_windows* w, int32_t H) {
+  if (H < 1 || H > 1024 || H % p->n_kv_heads) return SJD_EINVAL;
+  // query slots of a window: a launch has 65535 blocks of 128 of them
+  return (int64_t)w->max_rows * (H / p->n_kv_heads) <= 65535LL * 128 ? SJD_OK : SJD_ENOTSUP;
 }
 
 }  // namespace
@@ -138,7 +140,7 @@ extern "C" int sjd_kv_read(const sjd_pages* p, const sjd_windows* w, const sjd_k
 }
 
 extern "C" int64_t sjd_paged_attention_workspace(const sjd_pages* p, const sjd_windows* w, int32_t H) {
-  if (check_page_shape(p) != SJD_OK || check_windows_shape(p, w) != SJD_OK || check_heads(p, H) != SJD_OK) return 0;
+  if (check_page_shape(p) != SJD_OK || check_windows_shape(p, w) != SJD_OK || check_heads(p, w, H) != SJD_OK) return 0;
   return nothing(w) ? 0 : sjd::paged_attention_ws(*p, *w, H);
 }
 
@@ -147,7 +149,7 @@ extern "C" int sjd_paged_attention(const sjd_pages* p, const sjd_windows* w, con
   TRY(check_pages(p));
   TRY(check_windows(p, w));
   if (!io || !std::isfinite(io->scale)) return SJD_EINVAL;
-  TRY(check_heads(p, io->H));
+  TRY(check_heads(p, w, io->H));
   if (nothing(w)) return SJD_OK;
   const int64_t n = (int64_t)io->H * p->head_dim;
   if (!io->d_q || !io->d_out || !aligned(io->d_q, 16) || !aligned(io->d_out, 16) || io->q_row < n || io->out_row < n ||

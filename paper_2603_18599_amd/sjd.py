@@ -264,8 +264,15 @@ def _row_stride(fn, t, T, heads, hd):
     return s[0] if T > 1 else max(s[0], heads * hd)
 
 
+def _two_strides(fn, t, u, T, heads, hd):
+    """_row_stride of two tensors (laid out alike as a rule)."""
+    s = _row_stride(fn, t, T, heads, hd)
+    return s, s if u is t or (u.shape == t.shape and u.stride() == t.stride()) else _row_stride(fn, u, T, heads, hd)
+
+
 def _dense(fn, t, shape, dtype, device):
-    _expect(fn, t.shape == shape and t.dtype is dtype and t.is_contiguous() and t.get_device() == device)
+    if t.shape != shape or t.dtype is not dtype or not t.is_contiguous() or t.get_device() != device:
+        raise SjdError(fn, -1)
     return t.data_ptr()
 
 
@@ -315,12 +322,10 @@ def sjd_rope_axes(q, k, pos, freq, axis, *, out_q=None, out_k=None, inverse=Fals
         if t is None:
             return 0, 0, 0, None, None
         _expect(fn, t.dim() == 3 and t.dtype is dt and t.get_device() == dev)
+        out = t if out is None else out
+        _expect(fn, out is t or (out.dtype is dt and out.get_device() == dev))
         H = t.shape[1]
-        stride, at = _row_stride(fn, t, T, H, hd), t.data_ptr()
-        if out is None or out is t:
-            return H, stride, stride, at, at
-        _expect(fn, out.dtype is dt and out.get_device() == dev)
-        return H, stride, _row_stride(fn, out, T, H, hd), at, out.data_ptr()
+        return (H, *_two_strides(fn, t, out, T, H, hd), t.data_ptr(), out.data_ptr())
 
     H, q_row, out_q_row, qp, out_qp = rows(q, out_q)
     Hkv, k_row, out_k_row, kp, out_kp = rows(k, out_k)
@@ -363,8 +368,7 @@ class Windows:
 def _kv_call(fn, pages, win, k, v, stream):
     T, H, hd, dev = win.T, pages.n_kv_heads, pages.head_dim, pages.device
     _expect(fn, k.dtype is v.dtype and win.device == dev and k.get_device() == dev and v.get_device() == dev)
-    rows = KvRows(k.data_ptr(), v.data_ptr(), _row_stride(fn, k, T, H, hd), _row_stride(fn, v, T, H, hd),
-                  _types()[1].get(k.dtype, -1))
+    rows = KvRows(k.data_ptr(), v.data_ptr(), *_two_strides(fn, k, v, T, H, hd), _types()[1].get(k.dtype, -1))
     _launch(fn, stream, dev, C.byref(pages.desc), C.byref(win.desc), C.byref(rows))
 
 
@@ -398,7 +402,7 @@ def sjd_paged_attention(pages, win, q, out, ws, *, scale, anc=None, stream=None)
             q.get_device() == dev and out.get_device() == dev)
     H, size = q.shape[1], ws.numel()
     _expect(fn, ws.dtype is torch.uint8 and ws.is_contiguous() and (size == 0 or ws.get_device() == dev))
-    io = AttentionIO(H, scale, q.data_ptr(), out.data_ptr(), _row_stride(fn, q, T, H, hd), _row_stride(fn, out, T, H, hd),
+    io = AttentionIO(H, scale, q.data_ptr(), out.data_ptr(), *_two_strides(fn, q, out, T, H, hd),
                      None if anc is None else _dense(fn, anc, (T,), torch.int64, dev))
     _launch(fn, stream, dev, C.byref(pages.desc), C.byref(win.desc), C.byref(io), ws.data_ptr(), size)
 

@@ -139,6 +139,78 @@ def test_long_cache_is_split():
         c.check(c.run())
 
 
+@pytest.mark.parametrize("many", [False, True])
+@pytest.mark.parametrize("scale", [-0.3, 0.0])
+def test_negative_and_zero_scale(scale, many):
+    c = Case([(40, 200), (3, 0)], 32, 2, 2, 64, "e4m3", many=many)
+    c.scale = scale
+    c.check(c.run())
+
+
+def test_offsets_past_32_bits():
+    """Pages behind the first 4 GiB of a pool, and rows behind element 2^31 of
+    tensors with wide rows: the same bits as from small ones."""
+    small = Case([(40, 130), (1, 300)], 64, 2, 2, 128, "e4m3")
+    want = small.run()
+    n = (1 << 32) // small.pool.size + small.pool.n_pages + 1
+    pool = torch.empty(n * small.pool.size, dtype=torch.uint8, device="cuda")
+    pages = sjd.Pages(pool, n, 64, 2, 128, "e4m3")
+    shift = n - small.pool.n_pages
+    assert shift * small.pool.size > 1 << 32
+    table = torch.where(small.tt >= 0, small.tt + shift, small.tt)
+    wide, T = 1 << 20, 2049 + small.T
+    rows = torch.empty(T, wide, dtype=torch.bfloat16, device="cuda")
+    q = rows[:, :small.H * 128].view(T, small.H, 128)
+    q[2049:] = small.q.cuda()
+    seq = small.st.clone()
+    seq[:, 0] += 2049
+    win = sjd.Windows(seq, table, T, 40, 300)
+    # all keys and values through rows of the same wide tensor
+    both = [r + m for r, m in small.seqs]
+    k, v = (rows[:, a:a + 256].view(T, 2, 128) for a in (1024, 2048))
+    at = T - sum(both)
+    k[at:], v[at:] = torch.cat(small.k).cuda(), torch.cat(small.v).cuda()
+    whole = torch.tensor([[at, both[0], 0, 0], [at + both[0], both[1], 0, 0]], dtype=torch.int32).cuda()
+    every = sjd.Windows(whole, table, T, max(both), 0)
+    sjd.sjd_kv_append(pages, every, k, v)
+    out = rows[:, 4096:4096 + small.H * 128].view(T, small.H, 128)
+    out[2049:] = 3.0
+    ws = sjd.attention_workspace(pages, win, small.H)
+    sjd.sjd_paged_attention(pages, win, q, out, ws, scale=small.scale)
+    assert torch.equal(out[2049:], want)
+    kb, vb = (rows[:, a:a + 256].view(T, 2, 128) for a in (8192, 9216))
+    sjd.sjd_kv_read(pages, every, kb, vb)
+    got = torch.cat([kb[at:], vb[at:]]).double().cpu().numpy()
+    assert np.array_equal(got, np.concatenate([quantise(torch.cat(x).double().numpy())[0] for x in (small.k, small.v)]))
+    pos = torch.arange(T, dtype=torch.int32, device="cuda")[:, None].contiguous()
+    freq, axis = [1e4 ** (-i / 64) for i in range(64)], [0] * 64
+    alone = q[2049:].contiguous()
+    sjd.sjd_rope_axes(q, None, pos, freq, axis)
+    sjd.sjd_rope_axes(alone, None, pos[2049:].contiguous(), freq, axis)
+    assert torch.equal(q[2049:], alone)
+
+
+def test_two_calls_at_once():
+    """Two streams with a workspace each, and one stream twice with one."""
+    c, d = (Case([(8, 900), (1, 2000)], 64, 2, 4, 128, "e4m3", seed=s) for s in (0, 5))
+    want = [c.run(), d.run()]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    state = []
+    for x in (c, d):
+        win = x.windows()
+        state.append((x, win, x.q.cuda(), torch.full_like(want[0], 3.0), sjd.attention_workspace(x.pool.pages, win, x.H)))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for (x, win, q, out, ws), s in zip(state, streams):
+            sjd.sjd_paged_attention(x.pool.pages, win, q, out, ws, scale=x.scale, stream=s)
+    torch.cuda.synchronize()
+    assert all(torch.equal(s[3], w) for s, w in zip(state, want))
+    for x, win, q, out, _ in state:
+        out.fill_(3.0)
+        sjd.sjd_paged_attention(x.pool.pages, win, q, out, state[0][4], scale=x.scale)
+    assert all(torch.equal(s[3], w) for s, w in zip(state, want))
+
+
 def test_bounds_larger_than_the_data():
     c = Case([(3, 77), (1, 200)], 64, 2, 4, 128, "e4m3")
     a, b = c.run(), c.run(slack=5000)

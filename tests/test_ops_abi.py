@@ -128,6 +128,8 @@ def test_attention_refusals():
         assert attend(io=b) == -1, b
     assert attend(win=dict(max_rows=65, T=80), io=dict(d_anc=P)) == -1  # a mask has 64 bits
     assert attend(pages=dict(head_dim=32)) == -5
+    big = dict(T=1 << 24, max_rows=1 << 24, table_len=1 << 20)
+    assert attend(win=big, io=dict(H=128, q_row=1 << 20, out_row=1 << 20)) == -5  # query slots of a window
     assert attend(win=dict(B=0)) == 0
     assert call("sjd_paged_attention", None, None, None, None, 0, None) == -1
 
