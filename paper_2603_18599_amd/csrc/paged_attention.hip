@@ -24,6 +24,8 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
+constexpr int kMostSplits = 32;
+
 struct PagedArgs {
   PoolView pv;
   sjd_windows w;
@@ -644,41 +646,33 @@ __global__ __launch_bounds__(256) void k_paged_join(PagedArgs a) {
   const int hh = i % a.H;
   const int n = (sq.cached + sq.rows + a.chunk - 1) / a.chunk;
   const int64_t at = t * a.H + hh, step = (int64_t)a.w.T * a.H;
-  // 64 splits at a time: a lane reads one split's statistics and every lane its dims of
-  // each of them, the first 8 before anything waits for the statistics
+  // A lane reads one split's statistics and every lane its dims of each split, the
+  // first 8 before anything waits for the statistics
   constexpr int W = HD / 64, kBatch = 8;
-  float m = -INFINITY, l = 0.0f, v[W] = {};
-  for (int k0 = 0; k0 < n; k0 += kWave) {
-    const int c = min(kWave, n - k0);
-    const float2 ml = lane < c ? *(const float2*)(a.ws_ml + (at + (k0 + lane) * step) * 2) : make_float2(-INFINITY, 0.0f);
-    float x[kBatch][W];
-    auto read = [&](int k) {
+  static_assert(kMostSplits <= kWave, "one lane per split");
+  const float2 ml = lane < n ? *(const float2*)(a.ws_ml + (at + lane * step) * 2) : make_float2(-INFINITY, 0.0f);
+  float x[kBatch][W], v[W] = {};
+  auto read = [&](int k) {
 #pragma unroll
-      for (int u = 0; u < kBatch; ++u)
+    for (int u = 0; u < kBatch; ++u)
 #pragma unroll
-        for (int e = 0; e < W; ++e)
-          x[u][e] = k + u < c ? a.ws_o[(at + (k0 + k + u) * step) * HD + lane * W + e] : 0.0f;
-    };
-    read(0);
-    const float mx = fmaxf(m, wave_max_dpp(ml.x));
-    const float f = mx == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ml.x - mx);
-    const float old = mx == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m - mx);
-    l = l * old + wave_sum(lane < c ? ml.y * f : 0.0f);
+      for (int e = 0; e < W; ++e) x[u][e] = k + u < n ? a.ws_o[(at + (k + u) * step) * HD + lane * W + e] : 0.0f;
+  };
+  read(0);
+  const float mx = wave_max_dpp(ml.x);
+  const float f = mx == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ml.x - mx);
+  const float l = wave_sum(lane < n ? ml.y * f : 0.0f);
+  for (int k = 0;;) {
 #pragma unroll
-    for (int e = 0; e < W; ++e) v[e] *= old;
-    m = mx;
-    for (int k = 0;;) {
+    for (int u = 0; u < kBatch; ++u)
+      if (k + u < n) {
+        const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), k + u));
 #pragma unroll
-      for (int u = 0; u < kBatch; ++u)
-        if (k + u < c) {
-          const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), k + u));
-#pragma unroll
-          for (int e = 0; e < W; ++e) v[e] += x[u][e] * w;
-        }
-      k += kBatch;
-      if (k >= c) break;
-      read(k);
-    }
+        for (int e = 0; e < W; ++e) v[e] += x[u][e] * w;
+      }
+    k += kBatch;
+    if (k >= n) break;
+    read(k);
   }
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
   uint16_t* o = a.out + t * a.out_row + hh * HD + lane * (HD / 64);
@@ -706,8 +700,10 @@ void launch_head(const PagedArgs& a, const AttnPlan& pl, dim3 grid, hipStream_t 
 constexpr int kFewTiles = 1536;
 // Splits: as many as give two workgroups to each of 256 compute units, of one tile
 // per wave at least. More even out ragged sequences, but their partial outputs and
-// the second launch cost more: 64 single tokens over up to 8190 keys, 512 / 1024 /
-// 2048 workgroups: 140 / 148 / 156 us; 4 of them 18 / 23 / 31.
+// the second launch cost more: 64 single tokens over up to 8190 keys, 512 / 1024
+// workgroups: 127 / 131 us; 8 windows of 64 rows over 2000, 23 / 38. Past 32 the join's
+// rounds cost more than the splits save (a token of one key / value head over 8190
+// keys, 64 splits -> 32: 13.2 -> 11.3 us; over 30000, 235 -> 32: 29.7 -> 15.4).
 constexpr int kSplitWgs = 512;
 AttnPlan paged_attention_plan(const sjd_pages& p, const sjd_windows& w, int H) {
   const int64_t most = (int64_t)w.max_cached + w.max_rows;
@@ -716,6 +712,7 @@ AttnPlan paged_attention_plan(const sjd_pages& p, const sjd_windows& w, int H) {
   const bool few = slots <= 64 || tiles <= kFewTiles;
   int64_t S = few ? (kSplitWgs + tiles - 1) / tiles : 1;
   if (S > (most + kRound - 1) / kRound) S = (most + kRound - 1) / kRound;
+  if (S > kMostSplits) S = kMostSplits;
   const int64_t chunk = ((most + S - 1) / S + kRound - 1) / kRound * kRound;
   return AttnPlan{(int)chunk, (int)((most + chunk - 1) / chunk), few};
 }
