@@ -5,7 +5,9 @@
 // and hd codes and an exponent out. A workgroup takes one tile, 32 positions of
 // one head (whose part of a page is contiguous), 8 threads to a row. Keys go from
 // a thread's registers to their place; values lie transposed, so they cross LDS
-// in the tile's own order and move to and from memory in 16-byte pieces.
+// in the tile's own order and move to and from memory in 16-byte pieces. 10432 rows of
+// 32 heads of 128 written and 15363 read back (636 MB): 62 + 88 us, 4.2 TB/s; a copy
+// runs at 4.9.
 #include "device.h"
 #include "forward.h"
 #include "ops.h"
@@ -14,7 +16,7 @@ namespace sjd {
 
 namespace {
 
-// N consecutive elements as floats (16-byte aligned, or 8 bytes for N = 4 ...)
+// N consecutive elements as floats (16-byte aligned)
 template <bool F32, int N>
 SJD_DEV void load_row(const void* base, int64_t at, float (&v)[N]) {
   if constexpr (F32) {

@@ -6,7 +6,8 @@
 // instructions with the reduction to one revolution in 64 bits, and every head of
 // a row shares it, so a workgroup first fills a table in LDS with the (cos, sin)
 // of its rows' pairs, one entry per thread, and then streams the heads in 16-byte
-// pieces.
+// pieces. 8190 rows of 32 + 8 heads of 128 (168 MB): 35 us, 4.8 TB/s, a copy's rate; one
+// row 4.1 us.
 #include "device.h"
 #include "ops.h"
 
