@@ -23,7 +23,7 @@ int check_given(const sjd_given_params* p, const sjd_given_io* io) {
                         (const void*)io->d_u, (const void*)io->d_r, (const void*)io->d_tok, (const void*)io->d_next})
     if (!aligned(b, 4)) return SJD_EINVAL;
   if (!aligned(io->d_meta, 16)) return SJD_EINVAL;
-  // (a window's rows may lie in any order; windows of one row need no row stride)
+  // (windows may overlap or share their rows: any stride between them but a negative one)
   if (p->p_row < p->V || p->p_win < 0 || (io->d_q && (p->q_row < p->V || p->q_win < 0))) return SJD_EINVAL;
   return SJD_OK;
 }

@@ -265,8 +265,7 @@ __global__ __launch_bounds__(W * kWave) void k_given_chain(GivenArgs a) {
 template <int W>
 __global__ __launch_bounds__(W * kWave) void k_given_rows(GivenArgs a) {
   __shared__ DrawSmem<W> sm;
-  const int rows = a.p.L + (a.p.flags & SJD_BONUS ? 1 : 0);
-  const int b = blockIdx.x / rows, j = blockIdx.x % rows, n = drafts_of(a, b);
+  const int rows = gridDim.x, b = blockIdx.y, j = blockIdx.x, n = drafts_of(a, b);
   if (j > n || (j == n && rows == a.p.L)) return;
   int x = -1, t;
   if (j < n && accepts(a, b, j, &x)) t = a.io.d_draft[(int64_t)b * a.p.L + j];
@@ -305,7 +304,8 @@ template <int W>
 void launch(const GivenArgs& a, hipStream_t s) {
   if (a.p.flags & SJD_AC) {
     const int rows = a.p.L + (a.p.flags & SJD_BONUS ? 1 : 0);
-    hipLaunchKernelGGL(k_given_rows<W>, dim3(a.p.B * rows), dim3(W * kWave), 0, s, a);
+    // (in two dimensions: all rows' threads in one may pass 2^32)
+    hipLaunchKernelGGL(k_given_rows<W>, dim3(rows, a.p.B), dim3(W * kWave), 0, s, a);
     hipLaunchKernelGGL(k_given_end, dim3(a.p.B), dim3(128), 0, s, a);
   } else {
     hipLaunchKernelGGL(k_given_chain<W>, dim3(a.p.B), dim3(W * kWave), 0, s, a);

@@ -127,3 +127,18 @@ def test_given_law():
     _, tok, _ = call(p, q, draft, None, u, r, 0)
     seen = np.bincount(tok[:, 0], minlength=V)
     assert ((seen - B * p1) ** 2 / (B * p1)).sum() < 29.9
+
+
+def test_given_largest_batch():
+    """65535 windows of 64 drafts and a bonus row, 16 waves to a row: more threads
+    than 32 bits count. All windows share their probabilities."""
+    B, L, V = 65535, 64, 12289
+    p, _, _, _, _, _ = inputs(1, L, V, 8, True)
+    g = np.random.RandomState(9)
+    draft, n = g.randint(0, V, (B, L)).astype(np.int32), g.randint(0, L + 1, B).astype(np.int32)
+    u, r = (np.minimum(g.rand(B, k).astype(np.float32), 0.9999999) for k in (L, L + 1))
+    u[:, ::3] = 0.0  # (accepted)
+    meta, tok, nxt = call(torch.from_numpy(p).cuda().expand(B, L + 1, V), None, draft, n, u, r, sjd.SJD_AC | sjd.SJD_BONUS)
+    for b in (0, 1, 40000, 64526, 64527, 64528, 65533, 65534):
+        want = given(p[0], None, draft[b], n[b], u[b], r[b], True, True)
+        assert (list(meta[b]), list(tok[b]), list(nxt[b])) == tuple(want), b
