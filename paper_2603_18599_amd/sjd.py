@@ -261,7 +261,7 @@ def _row_stride(fn, t, T, heads, hd):
     _expect(fn, t.shape == (T, heads, hd))
     s = t.stride()
     _expect(fn, T == 0 or (s[2] == 1 and (heads == 1 or s[1] == hd)))
-    return s[0] if T > 1 else max(s[0], heads * hd)
+    return s[0] if T > 1 else heads * hd  # (a stride that separates nothing may be anything)
 
 
 def _two_strides(fn, t, u, T, heads, hd):

@@ -77,6 +77,24 @@ def test_rope_on_rows_of_a_wider_tensor(dtype):
             assert torch.equal(rows[:, part], before[:, part])
 
 
+def test_one_row_of_any_stride():
+    """The stride of a single row separates nothing: any value of it is taken."""
+    H, hd = 2, 64
+    odd = [torch.randn(1, H * hd + 5, device="cuda").bfloat16() for _ in range(4)]
+    k, v, k2, v2 = (x[:, :H * hd].unflatten(1, (H, hd)) for x in odd)
+    pages = sjd.Pages(torch.zeros(sjd.page_bytes(32, H, hd, "bf16"), dtype=torch.uint8, device="cuda"), 1, 32, H, hd, "bf16")
+    seq, table = torch.tensor([[0, 1, 0, 0]], dtype=torch.int32, device="cuda"), torch.zeros(1, 1, dtype=torch.int32, device="cuda")
+    win = sjd.Windows(seq, table, 1, 1, 0)
+    sjd.sjd_kv_append(pages, win, k, v)
+    sjd.sjd_kv_read(pages, win, k2, v2)
+    assert torch.equal(k2, k) and torch.equal(v2, v)
+    ws, out = sjd.attention_workspace(pages, win, H), torch.zeros(1, H * hd + 3, device="cuda").bfloat16()
+    sjd.sjd_paged_attention(pages, win, k, out[:, :H * hd].unflatten(1, (H, hd)), ws, scale=0.125)
+    assert torch.equal(out[:, :H * hd], v.flatten(1)) and not out[:, H * hd:].any()
+    sjd.sjd_rope_axes(k, None, torch.zeros(1, 1, dtype=torch.int32, device="cuda"), [1.0], [0])
+    assert torch.equal(k, k2)
+
+
 def rows_for(seqs, gap=3):
     """Sequence descriptions with rows nobody owns between them."""
     seq, at = [], gap
