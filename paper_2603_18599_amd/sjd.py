@@ -258,16 +258,13 @@ def _launch(fn, stream, device, *args):
 
 def _row_stride(fn, t, T, heads, hd):
     """Row stride of [T, heads, hd] rows whose heads lie one behind the other."""
-    _expect(fn, t.shape == (T, heads, hd))
+    if t.shape != (T, heads, hd):
+        raise SjdError(fn, -1)
+    if t.is_contiguous():  # (a single row whatever its stride, which separates nothing)
+        return heads * hd
     s = t.stride()
-    _expect(fn, T == 0 or (s[2] == 1 and (heads == 1 or s[1] == hd)))
-    return s[0] if T > 1 else heads * hd  # (a stride that separates nothing may be anything)
-
-
-def _two_strides(fn, t, u, T, heads, hd):
-    """_row_stride of two tensors (laid out alike as a rule)."""
-    s = _row_stride(fn, t, T, heads, hd)
-    return s, s if u is t or (u.shape == t.shape and u.stride() == t.stride()) else _row_stride(fn, u, T, heads, hd)
+    _expect(fn, T > 1 and s[2] == 1 and (heads == 1 or s[1] == hd))
+    return s[0]
 
 
 def _dense(fn, t, shape, dtype, device):
@@ -321,11 +318,15 @@ def sjd_rope_axes(q, k, pos, freq, axis, *, out_q=None, out_k=None, inverse=Fals
     def rows(t, out):  # heads, strides and addresses of a tensor and of what it becomes
         if t is None:
             return 0, 0, 0, None, None
-        _expect(fn, t.dim() == 3 and t.dtype is dt and t.get_device() == dev)
-        out = t if out is None else out
-        _expect(fn, out is t or (out.dtype is dt and out.get_device() == dev))
-        H = t.shape[1]
-        return (H, *_two_strides(fn, t, out, T, H, hd), t.data_ptr(), out.data_ptr())
+        if t.dim() != 3 or t.dtype is not dt or t.get_device() != dev:
+            raise SjdError(fn, -1)
+        H, at = t.shape[1], t.data_ptr()
+        row = _row_stride(fn, t, T, H, hd)
+        if out is None or out is t:
+            return H, row, row, at, at
+        if out.dtype is not dt or out.get_device() != dev:
+            raise SjdError(fn, -1)
+        return H, row, _row_stride(fn, out, T, H, hd), at, out.data_ptr()
 
     H, q_row, out_q_row, qp, out_qp = rows(q, out_q)
     Hkv, k_row, out_k_row, kp, out_kp = rows(k, out_k)
@@ -368,7 +369,8 @@ class Windows:
 def _kv_call(fn, pages, win, k, v, stream):
     T, H, hd, dev = win.T, pages.n_kv_heads, pages.head_dim, pages.device
     _expect(fn, k.dtype is v.dtype and win.device == dev and k.get_device() == dev and v.get_device() == dev)
-    rows = KvRows(k.data_ptr(), v.data_ptr(), *_two_strides(fn, k, v, T, H, hd), _types()[1].get(k.dtype, -1))
+    rows = KvRows(k.data_ptr(), v.data_ptr(), _row_stride(fn, k, T, H, hd), _row_stride(fn, v, T, H, hd),
+                  _types()[1].get(k.dtype, -1))
     _launch(fn, stream, dev, C.byref(pages.desc), C.byref(win.desc), C.byref(rows))
 
 
@@ -402,7 +404,7 @@ def sjd_paged_attention(pages, win, q, out, ws, *, scale, anc=None, stream=None)
             q.get_device() == dev and out.get_device() == dev)
     H, size = q.shape[1], ws.numel()
     _expect(fn, ws.dtype is torch.uint8 and ws.is_contiguous() and (size == 0 or ws.get_device() == dev))
-    io = AttentionIO(H, scale, q.data_ptr(), out.data_ptr(), *_two_strides(fn, q, out, T, H, hd),
+    io = AttentionIO(H, scale, q.data_ptr(), out.data_ptr(), _row_stride(fn, q, T, H, hd), _row_stride(fn, out, T, H, hd),
                      None if anc is None else _dense(fn, anc, (T,), torch.int64, dev))
     _launch(fn, stream, dev, C.byref(pages.desc), C.byref(win.desc), C.byref(io), ws.data_ptr(), size)
 
