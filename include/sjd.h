@@ -307,7 +307,9 @@ SJD_API int sjd_rope_axes(const sjd_rope_params* params, const sjd_rope_io* io, 
  * [Hkv][K, V] parts of page_len * head_dim elements, then (e4m3) [Hkv][K, V] parts
  * of page_len exponent bytes, padded to a multiple of 256 bytes.
  * An e4m3 row of a head carries one exponent byte E (1..254): the values are code *
- * 2^(E - 127). Rows that sjd_kv_append writes have the smallest E with max |x| <= 448 *
+ * 2^(E - 127), none of them past the largest float. (In sjd_paged_attention value rows
+ * with E < 27 lose bits: products with their power of two fall below the smallest
+ * normal bf16.) Rows that sjd_kv_append writes have the smallest E with max |x| <= 448 *
  * 2^(E - 127), kept within [27, 246] (E = 127 for a row of zeros); the maximum is taken
  * over finite values, larger ones and infinities become +-448, NaN stays. Powers of
  * two lose nothing in a floating type, make the quotient exact and are a shift to

@@ -175,9 +175,13 @@ SJD_DEV void scores(f32x16& c, const Keys& k, const Q& q, uint32_t vis) {
     for (int i = 0; i < 16; ++i) c[i] = (vis >> i) & 1 ? c[i] : -INFINITY;
 }
 
-// The reference moves only when a score exceeds it by kLag: probabilities up to 2^8
-// lose nothing (bf16 and float are relative), and most tiles skip the rescaling
-// of HD / 2 output registers.
+// The reference lies kLag above the largest score of the time when it was last moved,
+// and moves when a score passes it. Most tiles so skip the rescaling of HD / 2 output
+// registers, and probabilities stay between 2^-8 (a slot's largest) and 1: bf16 and
+// float are relative, so a factor loses nothing, and neither a probability times an
+// e4m3 row's power of two (up to 2^127) nor the sum of N of them, each times its
+// value, passes N of the largest value. (A reference kLag below its ceiling let
+// probabilities reach 2^8, and values 256 times smaller overflow.)
 constexpr float kLag = 8.0f;
 
 // Moves the reference if these scores ask for it, makes them probabilities and adds
@@ -191,11 +195,11 @@ SJD_DEV void weigh(WaveState<HD>& s, f32x16 (&c)[N], float scale, const uint32_t
     for (int i = 0; i < 16; ++i) mx = fmaxf(mx, c[n][i]);
   mx = max_of_halves(mx);
   mx = mx == -INFINITY ? mx : mx * scale;
-  const bool move = mx > s.m + kLag;
+  const bool move = mx > s.m;
   if (__any(move)) {
     // (each slot by itself: what its wave's other slots hold changes no bit of it)
-    const float alpha = move ? __builtin_amdgcn_exp2f(s.m - mx) : 1.0f;
-    s.m = move ? mx : s.m;
+    const float m = mx + kLag, alpha = move ? __builtin_amdgcn_exp2f(s.m - m) : 1.0f;
+    s.m = move ? m : s.m;
     s.l *= alpha;
 #pragma unroll
     for (int d = 0; d < HD / 32; ++d)

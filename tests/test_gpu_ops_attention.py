@@ -5,7 +5,7 @@ import pytest
 import torch
 
 import paper_2603_18599_amd as sjd
-from ops_util import Pool, attention, attention_tolerance, quantise, table_for
+from ops_util import Pool, attention, attention_tolerance, quantise, table_for, val_elem
 
 pytestmark = pytest.mark.gpu
 
@@ -392,3 +392,59 @@ def test_the_operators_together_and_captured():
                     assert (np.abs(io[1]["out"][r, h].double().cpu().numpy() - want) <= tol).all(), (i, z, h)
             for e in range(2):
                 io[e]["win"].seq[:, 2] += rows
+
+
+HOW = ["split", "whole", "shared"]  # keys split over workgroups, or not; keys shared by 128 slots
+
+
+def stepped(cache, how, later, cached=8100):
+    """Keys whose scores (log2 domain) are 0 in one half of every 256 positions and
+    `later` in the other, which a wave that takes more than one tile meets after the
+    first; one dim of a key differs from zero, so the scores are exact in 32 bits up to
+    their scaling."""
+    rows = 65 if how == "shared" else 3
+    c = Case([(rows, cached)] + [(0, 0)] * (0 if how == "split" else 600), 64, 1, 1, 64, cache, many=how == "shared")
+    assert (sjd.attention_workspace(c.pool.pages, c.windows(), 1).numel() > 0) == (how == "split")
+    n = cached + rows
+    c.k[0].zero_()
+    c.k[0][:, 0, 0] = (torch.arange(n) // 128 % 2).to(torch.bfloat16)
+    c.q.zero_()
+    c.q[:, 0, 0] = later / (1.4426950408889634 * c.scale)
+    return c, n
+
+
+@pytest.mark.parametrize("how", HOW)
+@pytest.mark.parametrize("cache", ["e4m3", "bf16"])
+def test_values_up_to_the_number_of_keys_below_the_largest_float(cache, how):
+    """Values of up to 2^127 / (number of keys), most of them behind scores that are
+    2^7.9 times as likely as the first ones'."""
+    c, n = stepped(cache, how, 7.9)
+    assert n <= 1 << 13
+    c.v[0] = torch.sign(c.v[0].float()).to(torch.bfloat16) * 2.0 ** (127 - 13)
+    c.v[0][:, 0, ::2] = 2.0 ** (127 - 13)  # (all of one sign: the largest sums)
+    c.fill_pages()
+    out = c.run()
+    assert bool(torch.isfinite(out.float()).all())
+    c.check(out)
+
+
+@pytest.mark.parametrize("how", HOW)
+def test_value_rows_with_the_largest_exponents(how):
+    """Rows that the caller wrote with exponent byte 254: codes of at most 2^-8
+    (values of 2^119 at most), zeros among them."""
+    c, n = stepped("e4m3", how, 7.9, cached=180)
+    assert n <= 1 << 8
+    c.fill_pages()
+    code = np.random.RandomState(2).randint(0, 3, (n, 64)).astype(np.uint8)  # 0, 2^-9, 2^-8
+    raw = c.pool.t.cpu().numpy().reshape(c.pool.n_pages, -1)
+    for p in range(n):
+        page, i = raw[c.table[0][p // 64]], p % 64
+        page[[64 * 64 + i // 32 * 32 * 64 + val_elem(i % 32, j, 64, True) for j in range(64)]] = code[p]
+        page[2 * 64 * 64 + 64 + i] = 254
+    c.pool.t.copy_(torch.from_numpy(raw.reshape(-1)))
+    c.v[0] = torch.from_numpy(code * 2.0 ** (127 - 9)).to(torch.bfloat16)[:, None]
+    c.pool.sync()
+    assert np.array_equal(c.pool.decode(c.table[0][2], 3)[1], c.v[0][131].double().numpy())
+    out = c.run()
+    assert bool(torch.isfinite(out.float()).all())
+    c.check(out)
