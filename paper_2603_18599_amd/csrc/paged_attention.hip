@@ -183,6 +183,9 @@ SJD_DEV void scores(f32x16& c, const Keys& k, const Q& q, uint32_t vis) {
 // value, passes N of the largest value. (A reference kLag below its ceiling let
 // probabilities reach 2^8, and values 256 times smaller overflow.)
 constexpr float kLag = 8.0f;
+// A reference of this size is rounded to 2^-4 and larger ones to more, which the
+// exact product under an exponent would show: past 2^31 as infinity or as zero.
+constexpr float kHuge = 0x1p20f;
 
 // Moves the reference if these scores ask for it, makes them probabilities and adds
 // them to the sum.
@@ -207,6 +210,14 @@ SJD_DEV void weigh(WaveState<HD>& s, f32x16 (&c)[N], float scale, const uint32_t
       for (int i = 0; i < 16; ++i) s.o[d][i] *= alpha;
   }
   const float base = s.m == -INFINITY ? 0.0f : s.m;
+  const bool huge = fabsf(base) >= kHuge;
+  if (__any(huge)) {  // (products rounded as the reference's was)
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) c[n][i] = huge ? c[n][i] * scale : c[n][i];
+    scale = huge ? 1.0f : scale;
+  }
   float sum[4] = {};
 #pragma unroll
   for (int n = 0; n < N; ++n)

@@ -448,3 +448,28 @@ def test_value_rows_with_the_largest_exponents(how):
     out = c.run()
     assert bool(torch.isfinite(out.float()).all())
     c.check(out)
+
+
+@pytest.mark.parametrize("how", HOW)
+@pytest.mark.parametrize("cache", ["e4m3", "bf16"])
+@pytest.mark.parametrize("top", [2.0 ** 26, 3e9, 1e20, 1e35])
+def test_huge_finite_scores(top, cache, how):
+    """The largest score is far past what its own rounding leaves of a power of two:
+    the keys that have it share the row, the others have nothing."""
+    c, n = stepped(cache, how, 1.0, cached=1000)
+    # products that are no floats times the scale, of either sign by the row
+    c.q[:, 0, 0] = (torch.tensor(top).log2().div(2).exp2() * torch.tensor([1.37, -1.11, 1.93]).repeat(c.T)[:c.T]).to(torch.bfloat16)
+    c.k[0][:, 0, 0] *= torch.tensor(top).sqrt().to(torch.bfloat16) * 1.21
+    c.scale = 0.3
+    c.fill_pages()
+    out = c.run()
+    assert bool(torch.isfinite(out.float()).all())
+    got = out.double().cpu().numpy()
+    k, v = c.value(c.k[0])[:, 0, 0], c.value(c.v[0])[:, 0]
+    first = c.seq[0][0]
+    for i in range(c.seqs[0][0]):
+        s = float(c.q[first + i, 0, 0]) * k[:1000 + i + 1]
+        share = v[:1000 + i + 1][s == s.max()]
+        want, mag = share.mean(0), np.abs(share).mean(0)
+        # (bf16 weights and output, a sum over the keys in 32 bits)
+        assert (np.abs(got[first + i, 0] - want) <= (2.0 ** -8 + n * 2.0 ** -22) * mag + 2.0 ** -8 * np.abs(want)).all()
