@@ -382,7 +382,7 @@ SJD_API int sjd_kv_read(const sjd_pages* pages, const sjd_windows* win, const sj
  * only rows that attend to them. SJD_ENOTSUP for windows of more than 65535 * 128
  * query slots (max_rows * H / n_kv_heads).
  * d_ws: sjd_paged_attention_workspace() bytes of scratch, 256-byte aligned (NULL
- * when that is 0); it holds nothing between calls, and calls that overlap in time
+ * when that is 0; it grows with the smaller of T and B * max_rows); it holds nothing between calls, and calls that overlap in time
  * need one each. */
 typedef struct {
   int32_t H;             /* query heads, a multiple of n_kv_heads                      */

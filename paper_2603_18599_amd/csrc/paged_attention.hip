@@ -40,9 +40,18 @@ struct PagedArgs {
   float scale;  // |scale| * log2(e);
   int negate;   // scale < 0: q changes sign
   int chunk, splits;
-  float* ws_o;  // [splits][T][H][HD] unnormalised outputs (splits > 1)
-  float* ws_ml; // [splits][T][H][2] maximum (log2 domain), sum
+  int ws_rows;  // rows of a split in the workspace, see split_rows
+  int ws_seq;   // .. of a sequence of them, or 0: rows of the tensors
+  float* ws_o;  // [splits][ws_rows][H][HD] unnormalised outputs (splits > 1)
+  float* ws_ml; // [splits][ws_rows][H][2] reference (log2 domain), sum
 };
+// The workspace has a place for each row of the tensors, or, where that is less, for
+// each row that the windows can have: a few of them may lie anywhere in large tensors.
+inline int split_rows(const sjd_windows& w) {
+  const int64_t n = (int64_t)w.B * w.max_rows;
+  return n < w.T ? (int)n : w.T;
+}
+SJD_DEV int split_row0(const PagedArgs& a, const Seq& sq, int z) { return a.ws_seq ? z * a.ws_seq : sq.row0; }
 
 SJD_DEV uint32_t pk_bf16(float a, float b) {
   const f32x2 v = {a, b};
@@ -459,7 +468,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_attn(PagedArgs a) {
                         pk_bf16(y[8 * i + 4] * inv, y[8 * i + 5] * inv), pk_bf16(y[8 * i + 6] * inv, y[8 * i + 7] * inv));
     return;
   }
-  const int64_t at = ((int64_t)sp * a.w.T + tt) * a.H + hh;
+  const int64_t at = ((int64_t)sp * a.ws_rows + split_row0(a, sq, z) + g / a.G) * a.H + hh;
 #pragma unroll
   for (int i = 0; i < DPT; i += 4)
     *(float4*)(a.ws_o + at * HD + d0 + i) = make_float4(y[i], y[i + 1], y[i + 2], y[i + 3]);
@@ -663,7 +672,8 @@ __global__ __launch_bounds__(256) void k_paged_join(PagedArgs a) {
   const int64_t t = sq.row0 + i / a.H;
   const int hh = i % a.H;
   const int n = (sq.cached + sq.rows + a.chunk - 1) / a.chunk;
-  const int64_t at = t * a.H + hh, step = (int64_t)a.w.T * a.H;
+  // (place i of the sequence's (row, head) pairs)
+  const int64_t at = (int64_t)split_row0(a, sq, z) * a.H + i, step = (int64_t)a.ws_rows * a.H;
   // A lane reads one split's statistics and every lane its dims of each split, the
   // first 8 before anything waits for the statistics
   constexpr int W = HD / 64, kBatch = 8;
@@ -738,7 +748,7 @@ AttnPlan paged_attention_plan(const sjd_pages& p, const sjd_windows& w, int H) {
 int64_t paged_attention_ws(const sjd_pages& p, const sjd_windows& w, int H) {
   const AttnPlan pl = paged_attention_plan(p, w, H);
   if (pl.splits <= 1) return 0;
-  return (int64_t)pl.splits * w.T * H * (p.head_dim + 2) * 4;
+  return (int64_t)pl.splits * split_rows(w) * H * (p.head_dim + 2) * 4;
 }
 
 hipError_t launch_paged_attention(const sjd_pages& p, const sjd_windows& w, const sjd_attention_io& io, void* ws,
@@ -750,8 +760,10 @@ hipError_t launch_paged_attention(const sjd_pages& p, const sjd_windows& w, cons
   a.scale = (float)(1.4426950408889634 * std::fabs((double)io.scale));
   a.negate = io.scale < 0.0f ? 1 : 0;
   a.chunk = pl.chunk; a.splits = pl.splits;
+  a.ws_rows = split_rows(w);
+  a.ws_seq = a.ws_rows < w.T ? w.max_rows : 0;
   a.ws_o = (float*)ws;
-  a.ws_ml = ws ? (float*)ws + (int64_t)pl.splits * w.T * io.H * p.head_dim : nullptr;
+  a.ws_ml = ws ? (float*)ws + (int64_t)pl.splits * a.ws_rows * io.H * p.head_dim : nullptr;
   const int slots = w.max_rows * a.G, per = pl.few ? 32 : 128;
   const dim3 grid(p.n_kv_heads * pl.splits, (slots + per - 1) / per, w.B);
   const bool f8 = p.dtype == SJD_E4M3;

@@ -473,3 +473,25 @@ def test_huge_finite_scores(top, cache, how):
         want, mag = share.mean(0), np.abs(share).mean(0)
         # (bf16 weights and output, a sum over the keys in 32 bits)
         assert (np.abs(got[first + i, 0] - want) <= (2.0 ** -8 + n * 2.0 ** -22) * mag + 2.0 ** -8 * np.abs(want)).all()
+
+
+def test_few_rows_of_large_tensors():
+    """Windows far apart in row tensors of a million rows: the bits, and the workspace, of
+    the same ones in small tensors."""
+    c = Case([(2, 5000), (3, 900)], 64, 1, 2, 64, "e4m3")
+    want, T = c.run(), 1 << 20
+    q = torch.zeros(T, 2, 64, dtype=torch.bfloat16, device="cuda")
+    out = torch.full_like(q, 3.0)
+    seq, at = c.st.clone(), [70000, T - 3]
+    for z, (first, r, _, _) in enumerate(c.seq):
+        q[at[z]:at[z] + r] = c.q[first:first + r].cuda()
+        seq[z, 0] = at[z]
+    win = sjd.Windows(seq, c.tt, T, 3, 5000)
+    ws = sjd.attention_workspace(c.pool.pages, win, 2)
+    assert 0 < ws.numel() <= sjd.attention_workspace(c.pool.pages, c.windows(), 2).numel()
+    ws.fill_(0xFF)
+    sjd.sjd_paged_attention(c.pool.pages, win, q, out, ws, scale=c.scale)
+    for z, (first, r, _, _) in enumerate(c.seq):
+        assert torch.equal(out[at[z]:at[z] + r], want[first:first + r])
+        out[at[z]:at[z] + r] = 3.0
+    assert bool((out == 3.0).all())

@@ -163,3 +163,16 @@ def test_python_side_refuses_tensors_that_do_not_fit():
         sjd.Pages(torch.zeros(100, dtype=torch.uint8), 1, 32, 1, 64, "e4m3")  # too small
     with pytest.raises(sjd.SjdError):
         sjd.Windows(torch.zeros(2, 3, dtype=torch.int32), torch.zeros(2, 2, dtype=torch.int32), 4, 1, 1)
+
+
+def test_attention_workspace_follows_the_windows():
+    """A window of few rows needs no more scratch in large row tensors than in small ones,
+    ragged windows no more than their tensors' rows."""
+    def need(**w):
+        return sjd.load_library().sjd_paged_attention_workspace(C.byref(sjd.PagesDesc(**PAGES)),
+                                                                C.byref(sjd.WindowsDesc(**{**WIN, **w})), 4)
+
+    one = dict(B=1, max_rows=1, max_cached=8000, table_len=200)
+    assert 0 < need(T=1, **one) == need(T=1 << 20, **one) == need(T=1 << 24, **one)
+    few = dict(B=3, max_rows=16, max_cached=8000, table_len=200)
+    assert 0 < need(T=20, **few) < need(T=48, **few) == need(T=49, **few)
