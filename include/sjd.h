@@ -91,19 +91,20 @@ typedef enum {
  * changed, if one is found. sjd_verify: in sjd_verify_params.flags;
  * decoder contexts: in sjd_config.flags. */
 #define SJD_CHECK_FINITE 32u
-/* decoder contexts only: caches in pages (see sjd_pages) instead of two bf16
- * planes, and attention by sjd_paged_attention. SJD_KV_E4M3 holds keys and values
- * in 8 bits with a power of two per row and head, a quarter of the default's
- * memory; with SJD_ROPE_GRID alone the pages are bf16. Rows of q, k and v are rounded
- * to bf16 before they are placed. SJD_EINVAL together with SJD_TUNE, whose
- * timings are those of the default path. */
+/* decoder contexts only: caches in pages (see sjd_pages) of 8 bits with a power of
+ * two per row and head instead of two bf16 planes, a quarter of the default's memory,
+ * and attention by sjd_paged_attention. Rows of q, k and v are rounded to bf16 before
+ * they are placed. SJD_EINVAL together with SJD_TUNE, whose timings are those of the
+ * default path. */
 #define SJD_KV_E4M3 128u
 /* decoder contexts only: image tokens are placed by time, row and column
  * (sjd_rope_axes) instead of along one axis. The prompt's tokens take their
  * position on all three; generated token g, with a prompt of n_p tokens, takes n_p,
  * n_p + g / (row_len + 1) and n_p + g % (row_len + 1). Of a head's pairs of dims (by
  * falling frequency rope_theta^(-2i / head_dim)) the first quarter turns by time, of
- * the others those with even i by row and those with odd i by column. Needs row_len >= 1 (SJD_EINVAL otherwise). */
+ * the others those with even i by row and those with odd i by column. The caches and
+ * their precision are the default's unless SJD_KV_E4M3 is set too. Needs row_len >= 1,
+ * and not SJD_TUNE (SJD_EINVAL otherwise). */
 #define SJD_ROPE_GRID 256u
 /* sjd_verify_given only: the row behind a window's last draft holds the
  * target's probabilities too, and a window whose drafts are all accepted

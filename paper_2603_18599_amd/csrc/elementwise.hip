@@ -220,7 +220,7 @@ hipError_t launch_window_in(const WindowIn& a, hipStream_t s) {
 }
 
 // Rotate-half rotary embedding (pair i with i + hd/2 at angle pos * theta^(-2i/hd),
-// table rope[pos][i] = (cos, sin)), then: q -> q planes, k and v -> cache
+// table rope[pos][i] = (cos, sin); pos: the row's position, or one of its place), then: q -> q planes, k and v -> cache
 // position n + m (tiled layout), all as hi / lo bf16 planes. Two-stream
 // windows: row m is slot m & 31 of stream m >> 5, cached at that stream's
 // own position in its own cache; padding rows get a zero q and no cache write.
@@ -230,9 +230,12 @@ hipError_t launch_window_in(const WindowIn& a, hipStream_t s) {
 // of 8 positions in each 16-byte chunk, and its lines then fill in one L2
 // instead of leaving as partial lines from eight (the row-major grid wrote
 // 5.8 MB per launch for about 1.5 MB of data, and the step took 60 us longer).
-template <int SMAX>
-__global__ void k_rope_kv(const float* qkv, int S, size_t plane, const Window* win, const int32_t* n_dev, int n_host,
-                          int H, int Hkv, int hd, const float2* rope, KvPlanes o, int cap, Streams sm) {
+// (GRID is a template argument: a branch around the position's load, which then no
+// longer runs beside the planes', cost a step of four images 0.3%)
+template <int SMAX, bool GRID>
+__global__ void k_rope_kv(const float* qkv, int S, size_t plane, const Window* win, const int32_t* places,
+                          const int32_t* n_dev, int n_host, int H, int Hkv, int hd, const float2* rope, KvPlanes o,
+                          int cap, Streams sm) {
   const int m = blockIdx.y, hh = blockIdx.x, i = threadIdx.x;
   const int half = hd / 2;
   const bool two = sm.mode != kStreamsOne;
@@ -271,7 +274,8 @@ __global__ void k_rope_kv(const float* qkv, int S, size_t plane, const Window* w
       b += pb[s];
     }
   if (hh < H + Hkv) {
-    const float2 cs = rope[(size_t)win->pos[m] * half + i];
+    const int pos = GRID ? places[3 * m + grid_axis(i, half)] : win->pos[m];
+    const float2 cs = rope[(size_t)pos * half + i];
     float o0, o1;
     rotate_pair(a, b, cs, o0, o1);
     if (hh < H) {
@@ -292,23 +296,21 @@ __global__ void k_rope_kv(const float* qkv, int S, size_t plane, const Window* w
   }
 }
 
-hipError_t launch_rope_kv(const float* qkv, int S, size_t plane, const Window* win, const int32_t* n_dev, int n_host,
-                          int M, int H, int Hkv, int hd, const float2* rope, const KvPlanes& o, int cap,
-                          const Streams& sm, hipStream_t s) {
+hipError_t launch_rope_kv(const float* qkv, int S, size_t plane, const Window* win, const int32_t* places,
+                          const int32_t* n_dev, int n_host, int M, int H, int Hkv, int hd, const float2* rope,
+                          const KvPlanes& o, int cap, const Streams& sm, hipStream_t s) {
   const dim3 grid(H + 2 * Hkv, M), block(hd / 2);
-  if (S < 1) return hipErrorInvalidValue;
-  if (S <= 4)
-    hipLaunchKernelGGL(k_rope_kv<4>, grid, block, 0, s, qkv, S, plane, win, n_dev, n_host, H, Hkv, hd, rope, o, cap, sm);
-  else if (S <= 8)
-    hipLaunchKernelGGL(k_rope_kv<8>, grid, block, 0, s, qkv, S, plane, win, n_dev, n_host, H, Hkv, hd, rope, o, cap, sm);
-  else if (S <= 16)
-    hipLaunchKernelGGL(k_rope_kv<16>, grid, block, 0, s, qkv, S, plane, win, n_dev, n_host, H, Hkv, hd, rope, o, cap,
-                       sm);
-  else if (S <= kGemmMaxSplits)
-    hipLaunchKernelGGL(k_rope_kv<kGemmMaxSplits>, grid, block, 0, s, qkv, S, plane, win, n_dev, n_host, H, Hkv, hd,
-                       rope, o, cap, sm);
-  else
-    return hipErrorInvalidValue;
+  if (S < 1 || S > kGemmMaxSplits) return hipErrorInvalidValue;
+  auto go = [&](auto g) {
+    constexpr bool G = decltype(g)::value;
+    const auto k = S <= 4    ? k_rope_kv<4, G>
+                   : S <= 8  ? k_rope_kv<8, G>
+                   : S <= 16 ? k_rope_kv<16, G>
+                             : k_rope_kv<kGemmMaxSplits, G>;
+    hipLaunchKernelGGL(k, grid, block, 0, s, qkv, S, plane, win, places, n_dev, n_host, H, Hkv, hd, rope, o, cap, sm);
+  };
+  if (places) go(std::true_type{});
+  else go(std::false_type{});
   return hipGetLastError();
 }
 

@@ -65,8 +65,9 @@ struct Ctx {
   int nstreams = 1;
   size_t kv_elems = 0;
   int delta[sjd::kMaxStreams] = {0, 0, 0, 0};  // per image (host copy, for the cache-fill bound)
-  // caches in pages (SJD_KV_E4M3, SJD_ROPE_GRID) instead of the planes above: one
-  // pool per layer, every stream's pages in it under one table
+  // caches in e4m3 pages (SJD_KV_E4M3) instead of the planes above: one pool per
+  // layer, every stream's pages in it under one table. With a grid (SJD_ROPE_GRID)
+  // rows have places of time, row and column, over either kind of cache.
   bool paged = false, grid = false;
   sjd_pages pages{};        // layer 0's; layer l's pool lies l * pool_bytes behind it
   int64_t pool_bytes = 0;
@@ -230,8 +231,11 @@ sjd_windows page_windows(const Ctx& x, int M, bool prompt, int cache) {
   return w;
 }
 
-// Attention of a context with paged caches, from QKV partial planes to activation
-// tiles: rows, their places, the cache, the attention over it.
+// Attention of a context with e4m3 pages, from QKV partial planes to activation
+// tiles: rows, their places, the cache, the attention over it. Rows are bf16: q has to
+// be for the attention's matrix operands, and beside 8 bits of k and v the rounding
+// before the rotation is small (logits of two to four layers off by 0.0260, 0.0197, 0.0494 rms from
+// those without any rounding, by 0.0251, 0.0189, 0.0477 with one rounding less).
 int paged_layer(Ctx& x, int l, int S, size_t plane, int M, int mt, bool prompt, int cache, hipStream_t s) {
   const sjd_config& c = x.c;
   const int hd = c.head_dim, Nq = c.n_heads * hd, Nkv = c.n_kv_heads * hd, N = Nq + 2 * Nkv;
@@ -275,7 +279,7 @@ int forward(Ctx& x, int M, const int32_t* prompt, const int32_t* n_dev, int n_ho
   in.vis_lo = c.vis_lo; in.sm = sm; in.win = x.win; in.E = x.embed; in.d = d; in.vocab = c.vocab_size; in.x = x.x;
   in.g = x.lw[0][0]; in.y = x.xn; in.mtiles = mt; in.ss = x.ss; in.fours = x.fours;
   HIPTRY(sjd::launch_window_in(in, s));
-  if (x.paged) {
+  if (x.paged || x.grid) {
     const sjd::PageWindow pw{x.win, in.st, n_host, M, c.L, x.grid ? 1 : 0, c.row_len, sm, x.pseq, x.ppos};
     HIPTRY(sjd::launch_page_window(pw, s));
   }
@@ -341,8 +345,8 @@ int forward(Ctx& x, int M, const int32_t* prompt, const int32_t* n_dev, int n_ho
     if (x.paged) {
       TRY(paged_layer(x, l, P[kProjQkv].S, qplane, M, mt, prompt != nullptr, cache, s));
     } else {
-      HIPTRY(sjd::launch_rope_kv(x.qkv, P[kProjQkv].S, qplane, x.win, n_dev, n_host, M, H, Hkv, hd, x.rope, kv,
-                                 x.cap_pad, sm, s));
+      HIPTRY(sjd::launch_rope_kv(x.qkv, P[kProjQkv].S, qplane, x.win, x.grid ? x.ppos : nullptr, n_dev, n_host, M, H,
+                                 Hkv, hd, x.rope, kv, x.cap_pad, sm, s));
       HIPTRY(sjd::launch_attention(a, hd, s));
     }
     g = plain;
@@ -477,7 +481,8 @@ Ctx::Plan tune_projection(Ctx& x, int proj, const std::vector<Ctx::Plan>& cand, 
         g.W = w[1]; g.N = Nqkv; g.out = x.qkv; g.plane = qplane; g.ldo = Nqkv;
         if ((e = sjd::launch_gemm(g, s)) != hipSuccess) return e;
         const sjd::KvPlanes kv{x.q, x.q_lo, x.kc, x.kc_lo, x.vt, x.vt_lo, x.kv_elems};
-        return sjd::launch_rope_kv(x.qkv, S, qplane, x.win, nullptr, 0, M, H, Hkv, hd, x.rope, kv, x.cap_pad, one, s);
+        return sjd::launch_rope_kv(x.qkv, S, qplane, x.win, nullptr, nullptr, 0, M, H, Hkv, hd, x.rope, kv, x.cap_pad,
+                                   one, s);
       }
       case kProjO:
         g.A = x.att; g.mtiles = mt; g.W = w[4]; g.N = d; g.K = Nq;
@@ -561,14 +566,14 @@ int cache_check(Ctx& x) {
   return SJD_OK;
 }
 
-// Pools, tables and row buffers of a context with paged caches.
+// Pools, tables and row buffers of a context with e4m3 pages.
 int page_buffers(Ctx& x, hipStream_t s) {
   const sjd_config& c = x.c;
   const int hd = c.head_dim, Nq = c.n_heads * hd, N = Nq + 2 * c.n_kv_heads * hd, P = hd / 2;
   constexpr int kPageLen = 64;
   x.page_cols = x.cap_pad / kPageLen;
   const int n_pages = x.page_cols * x.nstreams;
-  x.pages = sjd_pages{nullptr, n_pages, kPageLen, c.n_kv_heads, hd, c.flags & SJD_KV_E4M3 ? SJD_E4M3 : SJD_BF16};
+  x.pages = sjd_pages{nullptr, n_pages, kPageLen, c.n_kv_heads, hd, SJD_E4M3};
   x.pool_bytes = sjd::page_bytes(x.pages) * n_pages;
   char* pool = nullptr;
   // scratch of the largest launch: a step's, or a prompt's window of any length
@@ -581,8 +586,6 @@ int page_buffers(Ctx& x, hipStream_t s) {
   TRY(dalloc(x, &pool, (size_t)x.pool_bytes * c.n_layers));
   TRY(dalloc(x, &w, (size_t)ws));
   TRY(dalloc(x, &x.ptable, (size_t)n_pages));
-  TRY(dalloc(x, &x.pseq, 4 * sjd::kMaxStreams));
-  TRY(dalloc(x, &x.ppos, 3 * (size_t)x.Mpad));
   TRY(dalloc(x, &x.qkv_rows, (size_t)x.Mpad * N));
   TRY(dalloc(x, &x.att_rows, (size_t)x.Mpad * Nq));
   x.pages.d_pool = pool;
@@ -591,11 +594,8 @@ int page_buffers(Ctx& x, hipStream_t s) {
   for (int i = 0; i < n_pages; ++i) table[i] = i;
   // (rows between two streams are read, and never matter: they stay finite)
   if (hipMemcpyAsync(x.ptable, table.data(), table.size() * 4, hipMemcpyHostToDevice, s) != hipSuccess ||
-      hipMemsetAsync(x.ppos, 0, 12 * (size_t)x.Mpad, s) != hipSuccess ||
       hipMemsetAsync(x.att_rows, 0, (size_t)x.Mpad * Nq * 2, s) != hipSuccess || hipStreamSynchronize(s) != hipSuccess)
     return SJD_EHIP;
-  // places: pairs by frequency; with a grid the highest quarter turns by time, the
-  // rest by row and column in turn
   x.rp.H = c.n_heads; x.rp.Hkv = c.n_kv_heads; x.rp.head_dim = hd; x.rp.pairs = P;
   x.rp.axes = x.grid ? 3 : 1; x.rp.dtype = SJD_BF16;
   x.rp.q_row = x.rp.k_row = x.rp.out_q_row = x.rp.out_k_row = N;
@@ -603,7 +603,7 @@ int page_buffers(Ctx& x, hipStream_t s) {
   x.rp.h_axis = x.rope_axis;
   for (int i = 0; i < P; ++i) {
     x.rope_freq[i] = std::pow((double)c.rope_theta, -2.0 * i / hd);
-    x.rope_axis[i] = (uint8_t)(!x.grid || i < P / 4 ? 0 : 1 + (i & 1));
+    x.rope_axis[i] = (uint8_t)(x.grid ? sjd::grid_axis(i, P) : 0);
   }
   return SJD_OK;
 }
@@ -644,9 +644,9 @@ extern "C" int sjd_init(const sjd_config* cfg, const sjd_weights* w, void* strea
   // weights: copied into library memory; matrices repacked into the GEMM
   // tile layout (bf16), fp32 inputs rounded to nearest even
   const int f32 = c.weights_f32 ? 1 : 0;
-  x.paged = (c.flags & (SJD_KV_E4M3 | SJD_ROPE_GRID)) != 0;
+  x.paged = (c.flags & SJD_KV_E4M3) != 0;
   x.grid = (c.flags & SJD_ROPE_GRID) != 0;
-  x.fused = fused_shape(c) && !(c.flags & SJD_TUNE) && !x.paged;
+  x.fused = fused_shape(c) && !(c.flags & SJD_TUNE) && !x.paged && !x.grid;
   auto copy_rows = [&](const void* p, size_t count, const uint16_t** dst) -> int {
     uint16_t* b = nullptr;
     int rc = dalloc(x, &b, count);
@@ -721,6 +721,10 @@ extern "C" int sjd_init(const sjd_config* cfg, const sjd_weights* w, void* strea
       (rc = dalloc(x, &x.win, 1)) || (rc = dalloc(x, &x.rec, (size_t)x.B * c.L * sjd::kRecInts)) ||
       (rc = dalloc(x, &x.nonfinite, 16)))
     return fail(rc);
+  if (x.paged || x.grid) {  // (rows between two streams are read, and never matter: they stay finite)
+    if ((rc = dalloc(x, &x.pseq, 4 * sjd::kMaxStreams)) || (rc = dalloc(x, &x.ppos, 3 * (size_t)Mp))) return fail(rc);
+    if (hipMemsetAsync(x.ppos, 0, 12 * (size_t)Mp, s) != hipSuccess) return fail(SJD_EHIP);
+  }
   if (x.paged && (rc = page_buffers(x, s))) return fail(rc);
   x.att = x.xn + xnsz;
   x.hbuf = x.att + attsz;

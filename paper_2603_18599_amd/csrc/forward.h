@@ -224,10 +224,15 @@ struct KvPlanes {
   uint16_t *q, *q_lo, *kc, *kc_lo, *vt, *vt_lo;
   size_t sstride;  // multi-stream windows: stream z's caches are kc.. + z * sstride
 };
-// qkv: S fp32 partial planes [S][plane] summed in order
-hipError_t launch_rope_kv(const float* qkv, int S, size_t plane, const Window* win, const int32_t* n_dev, int n_host,
-                          int M, int H, int Hkv, int hd, const float2* rope, const KvPlanes& o, int cap,
-                          const Streams& st, hipStream_t s);
+// qkv: S fp32 partial planes [S][plane] summed in order. places: { time, row, column }
+// of each window row (SJD_ROPE_GRID), pair i turning by grid_axis(i)'s, or NULL: all of
+// them by the row's position
+hipError_t launch_rope_kv(const float* qkv, int S, size_t plane, const Window* win, const int32_t* places,
+                          const int32_t* n_dev, int n_host, int M, int H, int Hkv, int hd, const float2* rope,
+                          const KvPlanes& o, int cap, const Streams& st, hipStream_t s);
+// Which of a place's three a pair of dims turns by: the quarter of the highest
+// frequencies by time, the rest by row and column in turn
+__host__ __device__ inline int grid_axis(int pair, int pairs) { return pair < pairs / 4 ? 0 : 1 + (pair & 1); }
 // h = silu(gate) * up as tiled activations, gate = sum of the S fp32 partial
 // planes at columns [0, F), up = at columns [F, 2F) (row stride 2F)
 hipError_t launch_swiglu(const float* P, int S, size_t plane, int M, int F, uint16_t* h, int mtiles, hipStream_t s);

@@ -87,8 +87,8 @@ int64_t paged_attention_ws(const sjd_pages& p, const sjd_windows& w, int H);
 hipError_t launch_paged_attention(const sjd_pages& p, const sjd_windows& w, const sjd_attention_io& io, void* ws,
                                   hipStream_t s);
 
-// ---- decoder contexts whose caches are pages (paged_step.hip)
-// A window's sequences and places: seq[z] = { row0, rows, cached, 0 } of stream z,
+// ---- decoder contexts with e4m3 pages or a grid (paged_step.hip)
+// A window's sequences (of pages) and places: seq[z] = { row0, rows, cached, 0 } of stream z,
 // pos[m] = the row's position, or with grid { time, row, column } of it: a text
 // token's position three times; image token g (the first one at position n_p): n_p,
 // n_p + g / (row_len + 1), n_p + g % (row_len + 1).

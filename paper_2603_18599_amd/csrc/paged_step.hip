@@ -1,7 +1,7 @@
-// What a decoder context with paged caches runs around the standalone operators:
-// its window's sequences and places, rows from GEMM planes and back into activation
-// tiles, and the move of an accepted sibling's cache row. All of it small beside the
-// projections (a window is at most 128 rows).
+// What a decoder context with e4m3 pages runs around the standalone operators: its
+// window's sequences and places (these with a grid, too), rows from GEMM planes and
+// back into activation tiles, and the move of an accepted sibling's cache row. All of
+// it small beside the projections (a window is at most 128 rows).
 #include "device.h"
 #include "ops.h"
 
@@ -63,24 +63,21 @@ __global__ __launch_bounds__(256) void k_row_tiles(const uint16_t* rows, int K, 
   *(uint4*)(d + kActLo) = make_uint4(0, 0, 0, 0);
 }
 
-// Element of position i (of 32) and dim j in a key and in a value tile (sjd.h)
-template <bool FP8>
+// Byte of position i (of 32) and dim j in a key and in a value tile (sjd.h)
 SJD_DEV int key_elem(int i, int j, int hd) {
   const int h2 = hd / 2, lane = swap23(i) + 32 * (j / h2), t = j % h2 / 8;
-  return FP8 ? (64 * (t / 2) + lane) * 16 + 8 * (t % 2) + j % 8 : (64 * t + lane) * 8 + j % 8;
+  return (64 * (t / 2) + lane) * 16 + 8 * (t % 2) + j % 8;
 }
-template <bool FP8>
 SJD_DEV int val_elem(int i, int j) {
   const int lane = j % 32 + 32 * (i / 8 % 2);
-  return FP8 ? (64 * (j / 32) + lane) * 16 + 8 * (i / 16) + i % 8 : ((j / 32 * 2 + i / 16) * 64 + lane) * 8 + i % 8;
+  return (64 * (j / 32) + lane) * 16 + 8 * (i / 16) + i % 8;
 }
 
 // grid (layer, key / value head, stream), one thread per dim
-template <int HD, bool FP8>
+template <int HD>
 __global__ __launch_bounds__(HD) void k_page_commit(const DevState* st, const Window* win, PoolView pv,
                                                     int64_t pool_bytes, const int32_t* table, int table_len, int K,
                                                     int guided) {
-  constexpr int ES = FP8 ? 1 : 2;
   const int z = blockIdx.z, h = blockIdx.y, j = threadIdx.x, b = guided ? z >> 1 : z;
   const DevState* s = st + b;
   const int acc_k = s->meta[5];
@@ -93,16 +90,10 @@ __global__ __launch_bounds__(HD) void k_page_commit(const DevState* st, const Wi
   const int mask = (1 << pv.plen_log2) - 1, is = src & mask, id = dst & mask;
 #pragma unroll
   for (int kv = 0; kv < 2; ++kv) {
-    const int es = kv ? val_elem<FP8>(is & 31, j) : key_elem<FP8>(is & 31, j, HD);
-    const int ed = kv ? val_elem<FP8>(id & 31, j) : key_elem<FP8>(id & 31, j, HD);
-    const char* from = ps + tile_off<HD, ES>(pv, h, is, kv);
-    char* to = pd + tile_off<HD, ES>(pv, h, id, kv);
-    if constexpr (FP8) {
-      to[ed] = from[es];
-      if (j == 0) pd[exp_off<HD>(pv, h, kv) + id] = ps[exp_off<HD>(pv, h, kv) + is];
-    } else {
-      ((uint16_t*)to)[ed] = ((const uint16_t*)from)[es];
-    }
+    const int es = kv ? val_elem(is & 31, j) : key_elem(is & 31, j, HD);
+    const int ed = kv ? val_elem(id & 31, j) : key_elem(id & 31, j, HD);
+    pd[tile_off<HD, 1>(pv, h, id, kv) + ed] = ps[tile_off<HD, 1>(pv, h, is, kv) + es];
+    if (j == 0) pd[exp_off<HD>(pv, h, kv) + id] = ps[exp_off<HD>(pv, h, kv) + is];
   }
 }
 
@@ -128,14 +119,10 @@ hipError_t launch_row_tiles(const uint16_t* rows, int M, int K, uint16_t* y, int
 
 hipError_t launch_page_commit(const DevState* st, const Window* win, const sjd_pages& p, int64_t pool_bytes, int layers,
                               const int32_t* table, int table_len, int K, int nstreams, bool guided, hipStream_t s) {
-  const PoolView pv = pool_view(p);
-  const dim3 grid(layers, p.n_kv_heads, nstreams);
-  const bool f8 = p.dtype == SJD_E4M3;
-  auto go = [&](auto kernel, int hd) {
-    hipLaunchKernelGGL(kernel, grid, dim3(hd), 0, s, st, win, pv, pool_bytes, table, table_len, K, guided ? 1 : 0);
-  };
-  if (p.head_dim == 128) f8 ? go(k_page_commit<128, true>, 128) : go(k_page_commit<128, false>, 128);
-  else f8 ? go(k_page_commit<64, true>, 64) : go(k_page_commit<64, false>, 64);
+  if (p.dtype != SJD_E4M3) return hipErrorInvalidValue;
+  const auto k = p.head_dim == 128 ? k_page_commit<128> : k_page_commit<64>;
+  hipLaunchKernelGGL(k, dim3(layers, p.n_kv_heads, nstreams), dim3(p.head_dim), 0, s, st, win, pool_view(p), pool_bytes,
+                     table, table_len, K, guided ? 1 : 0);
   return hipGetLastError();
 }
 

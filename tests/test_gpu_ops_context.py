@@ -231,3 +231,33 @@ def test_flags_refused_on_host():
                  dict(flags=sjd.SJD_KV_E4M3 | 16), dict(flags=512)):
         c = b.Config(**{**good, **over})
         assert lib.sjd_init(C.byref(c), C.byref(w), None, C.byref(h)) == -1, over
+
+
+# A context without e4m3 pages rounds activations, keys and values to pairs of bf16 (16
+# bits, half a step of 2^-17), 2^-8 of what a single bf16 rounding does. Rounding q, k, v
+# and the attention's output to bf16 moves these cases' logits by 0.0051 to 0.0193 (plain
+# decoder, CPU); the GEMM inputs and probabilities are as many rounding points again, and
+# more: 4 * 0.0193 * 2^-8 = 3e-4. Three times that is the bound, a fifth of what bf16 does.
+PAIRS = 1e-3
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("flags", [0, sjd.SJD_ROPE_GRID])
+@pytest.mark.parametrize("over", CASES, ids=[str(i) for i in range(len(CASES))])
+def test_a_grid_alone_keeps_the_default_precision(over, flags):
+    """Where tokens are placed says nothing about the bits of the caches and of the
+    attention."""
+    cfg = config(flags, **over)
+    w = model_weights(cfg, 3, std=STD)
+    prompt, drafts = tokens(cfg, cfg["n_prompt"], 4), tokens(cfg, cfg["L"], 5, vis=True)
+    eng = make_engine(cfg, weights_device(w))
+    eng.prefill(prompt.cuda(), 1)
+    eng.set_drafts(drafts.cuda())
+    out = torch.empty(cfg["L"], cfg["V"], device="cuda")
+    eng.forward_window(out)
+    toks = prompt.tolist() + drafts.tolist()[:-1]
+    ref = reference(cfg, w, toks, places(cfg, len(prompt), range(len(toks))), causal(len(toks)), rounds=False)
+    err = (out.cpu().double() - ref[len(prompt) - 1:]).abs().max().item()
+    print("max error", err)
+    assert err < PAIRS
+    eng.close()
