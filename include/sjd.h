@@ -530,7 +530,9 @@ SJD_API int sjd_step(sjd_ctx* ctx, const int32_t* d_draft_tok, const float* d_dr
  * so the caller may reuse them once the stream passes this call). A draft
  * outside [vis_lo, vis_lo + V) is verified as no draft (its row draws from
  * p and counts as rejected); one outside [0, vocab_size) (e.g. the -1 that
- * pads d_out_next) is fed to the model as token vis_lo.
+ * pads d_out_next) is fed to the model as token vis_lo. Row end positions
+ * take eol_id and count as accepted whatever was fed, so eol_id is the draft
+ * to give there: the cache keeps the row of the token that was fed.
  * SJD_ESTATE before the image is prefilled. */
 SJD_API int sjd_set_drafts(sjd_ctx* ctx, int32_t image, const int32_t* d_draft_tok, const float* d_draft_logits,
                            void* stream);
