@@ -375,19 +375,20 @@ SJD_API int sjd_kv_read(const sjd_pages* pages, const sjd_windows* win, const sj
  * rows' own keys and values already (sjd_kv_append): out = softmax(scale * q . k) v
  * over every cached position and, of the window, over the rows up to itself or
  * (d_anc) the rows i whose bit i is set in the row's ancestor mask (tree windows;
- * max_rows <= 64). A row that attends to nothing gives zeros. Query head h uses
- * key / value head h / (H / n_kv_heads). Scores, statistics and sums are held in 32
- * bits; probabilities enter the value product as bf16, relative to the row's
- * reference maximum; the sums are divided at the end, so values within a factor of
- * the number of keys of the largest float overflow. Non-finite keys and values reach
- * only rows that attend to them. SJD_ENOTSUP for windows of more than 65535 * 128
- * query slots (max_rows * H / n_kv_heads).
+ * max_rows <= 64). A row that attends to nothing, or only to keys whose score is
+ * -infinity, gives zeros. Query head h uses key / value head h / (H / n_kv_heads).
+ * Scores (times log2(e), infinite where that passes the largest float), statistics and
+ * sums are held in 32 bits; probabilities enter the value product as bf16, relative to
+ * the row's reference maximum; the sums are divided at the end, so values within a
+ * factor of the number of keys of the largest float overflow. Non-finite keys and
+ * values reach only rows that attend to them. SJD_ENOTSUP for windows of more than
+ * 65535 * 128 query slots (max_rows * H / n_kv_heads).
  * d_ws: sjd_paged_attention_workspace() bytes of scratch, 256-byte aligned (NULL
- * when that is 0; it grows with the smaller of T and B * max_rows); it holds nothing between calls, and calls that overlap in time
- * need one each. */
+ * when that is 0; it grows with the smaller of T and B * max_rows); it holds nothing
+ * between calls, and calls that overlap in time need one each. */
 typedef struct {
   int32_t H;             /* query heads, a multiple of n_kv_heads                      */
-  float scale;           /* finite                                                    */
+  float scale;           /* scale * log2(e) is a finite float                          */
   const void* d_q;       /* [T][H][head_dim] bf16, 16-byte aligned                      */
   void* d_out;           /* [T][H][head_dim] bf16, 16-byte aligned; must not overlap q   */
   int64_t q_row, out_row; /* elements between rows, multiples of 8                       */

@@ -148,7 +148,7 @@ extern "C" int sjd_paged_attention(const sjd_pages* p, const sjd_windows* w, con
                                    int64_t ws_bytes, void* stream) {
   TRY(check_pages(p));
   TRY(check_windows(p, w));
-  if (!io || !std::isfinite(io->scale)) return SJD_EINVAL;
+  if (!io || !std::isfinite(sjd::log2_scale(io->scale))) return SJD_EINVAL;
   TRY(check_heads(p, w, io->H));
   if (nothing(w)) return SJD_OK;
   const int64_t n = (int64_t)io->H * p->head_dim;

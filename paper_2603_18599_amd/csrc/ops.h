@@ -4,6 +4,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <cmath>
+
 #include "forward.h"
 #include "sjd.h"
 
@@ -77,6 +79,8 @@ hipError_t launch_kv_append(const sjd_pages& p, const sjd_windows& w, const sjd_
 hipError_t launch_kv_read(const sjd_pages& p, const sjd_windows& w, const sjd_kv_rows& r, hipStream_t s);
 
 // ---- attention over pages
+// Scores are formed in the log2 domain: |scale| * log2(e)
+inline float log2_scale(float scale) { return (float)(1.4426950408889634 * std::fabs((double)scale)); }
 struct AttnPlan {
   int chunk;   // keys per split, a multiple of the workgroup's keys per round
   int splits;  // most splits of a sequence

@@ -757,7 +757,7 @@ hipError_t launch_paged_attention(const sjd_pages& p, const sjd_windows& w, cons
   PagedArgs a{};
   a.pv = pool_view(p); a.w = w; a.q = (const uint16_t*)io.d_q; a.out = (uint16_t*)io.d_out;
   a.q_row = io.q_row; a.out_row = io.out_row; a.anc = io.d_anc; a.H = io.H; a.G = io.H / p.n_kv_heads;
-  a.scale = (float)(1.4426950408889634 * std::fabs((double)io.scale));
+  a.scale = log2_scale(io.scale);
   a.negate = io.scale < 0.0f ? 1 : 0;
   a.chunk = pl.chunk; a.splits = pl.splits;
   a.ws_rows = split_rows(w);

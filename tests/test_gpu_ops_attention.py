@@ -495,3 +495,22 @@ def test_few_rows_of_large_tensors():
         assert torch.equal(out[at[z]:at[z] + r], want[first:first + r])
         out[at[z]:at[z] + r] = 3.0
     assert bool((out == 3.0).all())
+
+
+@pytest.mark.parametrize("how", HOW)
+def test_scores_of_minus_infinity(how):
+    """Keys with such scores have no weight; a row with no others gives zeros."""
+    c, n = stepped("bf16", how, 1.0, cached=1000)
+    c.k[0][300:, 0, 5], c.k[0][:40, 0, 5] = -float("inf"), -float("inf")
+    c.q[:, 0, 5] = 0.5
+    c.q[c.seq[0][0], 0, 5] = 2.0
+    c.fill_pages()
+    out, rows = c.run(), c.seqs[0][0]
+    keep = c.k[0].clone()
+    c.k[0][300:, 0, 5], c.k[0][:40, 0, 5] = 0, 0  # (the plain form leaves them out)
+    c.check(out, left_out=[(0, 40), (300, n)])
+    c.k[0] = keep
+    c.k[0][:, 0, 5] = -float("inf")
+    c.fill_pages()
+    out = c.run()
+    assert not out[c.seq[0][0]:c.seq[0][0] + rows].any()

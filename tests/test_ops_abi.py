@@ -134,6 +134,15 @@ def test_attention_refusals():
     assert call("sjd_paged_attention", None, None, None, None, 0, None) == -1
 
 
+def test_attention_refuses_a_scale_that_overflows_as_a_power_of_two():
+    import math
+    most = 3.4028234e38 / math.log2(math.e)
+    for s in (3.4e38, -3.4e38, most * 1.000001):
+        assert attend(io=dict(scale=s)) == -1, s
+    for s in (most * 0.999999, -0.0, 1e-45):
+        assert attend(win=dict(B=0), io=dict(scale=s)) == 0, s
+
+
 def test_attention_needs_its_workspace():
     w = dict(B=1, T=1, max_rows=1, max_cached=8000, table_len=200)
     lib = sjd.load_library()
