@@ -9,8 +9,11 @@
 // e4m3 codes become bf16 without rounding, times the key's power of two (an operand
 // of the conversion); a value row's power multiplies its probability.
 // 64 tokens over up to 8190 keys (8 heads, e4m3, 647 MB): 127 us, 5.1 TB/s, bound by
-// memory. A prompt of 4096 rows over 4172 keys (bf16, 417 GFLOP): 434 us, 960 TFLOP/s,
-// bound by the matrix rate that the card sustains (a library product: 1207).
+// memory (bf16 pages: 235). A prompt of 4096 rows over 4172 keys (bf16, 417 GFLOP): 434 to
+// 463 us on several cards, 900 to 960 TFLOP/s (a library product: 1207). MFMAs keep the
+// matrix units busy for 44% of its cycles and the softmax the vector units for about 40%;
+// two waves per SIMD overlap them in part (waves wait 32% of their cycles, LDS is active
+// in 22%).
 #include <cmath>
 #include <type_traits>
 
