@@ -73,6 +73,19 @@ template <int HD>
 __device__ __forceinline__ int64_t exp_off(const PoolView& pv, int h, int kv) {
   return ((int64_t)2 * pv.Hkv * HD + 2 * h + kv) << pv.plen_log2;
 }
+// Byte of position i (of 32) and dim j inside a key tile and inside a value tile: the
+// layout of sjd.h, which the attention reads as its matrix operands without these
+template <int HD, bool FP8>
+__device__ __forceinline__ int key_byte(uint32_t i, uint32_t j) {
+  const uint32_t lane = swap23(i) + 32 * (j / (HD / 2)), t = j % (HD / 2) / 8;
+  return FP8 ? (64 * (t / 2) + lane) * 16 + 8 * (t % 2) + j % 8 : (64 * t + lane) * 16 + 2 * (j % 8);
+}
+template <bool FP8>
+__device__ __forceinline__ int val_byte(uint32_t i, uint32_t j) {
+  const uint32_t lane = j % 32 + 32 * (i / 8 % 2);
+  return FP8 ? (64 * (j / 32) + lane) * 16 + 8 * (i / 16) + i % 8
+             : ((j / 32 * 2 + i / 16) * 64 + lane) * 16 + 2 * (i % 8);
+}
 #endif
 
 hipError_t launch_kv_append(const sjd_pages& p, const sjd_windows& w, const sjd_kv_rows& r, hipStream_t s);

@@ -98,28 +98,15 @@ SJD_DEV void decode4(uint32_t w, float f, float* v) {
   v[0] = a[0] * f; v[1] = a[1] * f; v[2] = b[0] * f; v[3] = b[1] * f;
 }
 
-// Byte offset in a value tile of position i, dim j; and the first position of the
-// 16-byte piece u of a tile (half 0, and 8 positions on in e4m3's half 1: 16 on)
-template <bool FP8>
-SJD_DEV int val_byte(int i, int j) {
-  const int lane = (j & 31) + 32 * ((i >> 3) & 1);
-  return FP8 ? (64 * (j >> 5) + lane) * 16 + 8 * (i >> 4) + (i & 7)
-             : (((j >> 5) * 2 + (i >> 4)) * 64 + lane) * 16 + (i & 7) * 2;
-}
-// Its place in LDS: 16 bytes more every 256, which spreads the 8 threads of a row (256
-// and 1024 bytes apart) over the banks
+// A value tile's place in LDS: 16 bytes more every 256, which spreads the 8 threads of a
+// row (256 and 1024 bytes apart) over the banks
 SJD_DEV int pad(int b) { return b + ((b >> 8) << 4); }
+// The first position (see val_byte) of the 16-byte piece u of a value tile; e4m3's second
+// 8 bytes are 16 positions on
 template <bool FP8>
 SJD_DEV int piece_pos(int u) {
   const int hi = ((u & 63) >> 5) * 8;
   return FP8 ? hi : hi + 16 * ((u >> 6) & 1);
-}
-// Byte offset in a key tile of the thread's first chunk of 8 dims (row i, part c
-// of 8; a second chunk, 128-dim heads: 8 bytes on in e4m3, 1024 in bf16)
-template <int HD, bool FP8>
-SJD_DEV int key_byte(int i, int c) {
-  const int lane = swap23(i) + 32 * (c >> 2), t = (c & 3) * (HD / 64);
-  return FP8 ? ((t >> 1) * 64 + lane) * 16 + (t & 1) * 8 : (t * 64 + lane) * 16;
 }
 
 struct CacheArgs {
@@ -149,7 +136,8 @@ __global__ __launch_bounds__(256) void k_kv_append(CacheArgs a) {
     load_row<F32, N>(a.r.d_k, t * a.r.k_row + h * HD + c * N, kf);
     load_row<F32, N>(a.r.d_v, t * a.r.v_row + h * HD + c * N, vf);
   }
-  char* kt = page + tile_off<HD, ES>(a.pv, h, in, 0) + key_byte<HD, FP8>(i, c);
+  // (of the row's first 8 dims; a second chunk, 128-dim heads: 8 bytes on in e4m3, 1024 in bf16)
+  char* kt = page + tile_off<HD, ES>(a.pv, h, in, 0) + key_byte<HD, FP8>(i, c * N);
   char* vt = page + tile_off<HD, ES>(a.pv, h, in, 1);
   if constexpr (FP8) {
     uint32_t kc[N / 4], vc[N / 4];
@@ -211,7 +199,7 @@ __global__ __launch_bounds__(256) void k_kv_read(CacheArgs a) {
   const int64_t t = sq.row0 + r;
   float kf[N] = {}, vf[N] = {};
   if (page) {
-    const char* kt = page + tile_off<HD, ES>(a.pv, h, in, 0) + key_byte<HD, FP8>(i, c);
+    const char* kt = page + tile_off<HD, ES>(a.pv, h, in, 0) + key_byte<HD, FP8>(i, c * N);
     const char* vt = page + tile_off<HD, ES>(a.pv, h, in, 1);
     for (int u = threadIdx.x; u < 2 * HD * ES; u += 256) *(uint4*)(vs + pad(16 * u)) = *(const uint4*)(vt + 16 * u);
     if constexpr (FP8) {

@@ -63,16 +63,6 @@ __global__ __launch_bounds__(256) void k_row_tiles(const uint16_t* rows, int K, 
   *(uint4*)(d + kActLo) = make_uint4(0, 0, 0, 0);
 }
 
-// Byte of position i (of 32) and dim j in a key and in a value tile (sjd.h)
-SJD_DEV int key_elem(int i, int j, int hd) {
-  const int h2 = hd / 2, lane = swap23(i) + 32 * (j / h2), t = j % h2 / 8;
-  return (64 * (t / 2) + lane) * 16 + 8 * (t % 2) + j % 8;
-}
-SJD_DEV int val_elem(int i, int j) {
-  const int lane = j % 32 + 32 * (i / 8 % 2);
-  return (64 * (j / 32) + lane) * 16 + 8 * (i / 16) + i % 8;
-}
-
 // grid (layer, key / value head, stream), one thread per dim
 template <int HD>
 __global__ __launch_bounds__(HD) void k_page_commit(const DevState* st, const Window* win, PoolView pv,
@@ -90,8 +80,8 @@ __global__ __launch_bounds__(HD) void k_page_commit(const DevState* st, const Wi
   const int mask = (1 << pv.plen_log2) - 1, is = src & mask, id = dst & mask;
 #pragma unroll
   for (int kv = 0; kv < 2; ++kv) {
-    const int es = kv ? val_elem(is & 31, j) : key_elem(is & 31, j, HD);
-    const int ed = kv ? val_elem(id & 31, j) : key_elem(id & 31, j, HD);
+    const int es = kv ? val_byte<true>(is & 31, j) : key_byte<HD, true>(is & 31, j);
+    const int ed = kv ? val_byte<true>(id & 31, j) : key_byte<HD, true>(id & 31, j);
     pd[tile_off<HD, 1>(pv, h, id, kv) + ed] = ps[tile_off<HD, 1>(pv, h, is, kv) + es];
     if (j == 0) pd[exp_off<HD>(pv, h, kv) + id] = ps[exp_off<HD>(pv, h, kv) + is];
   }
