@@ -704,20 +704,21 @@ extern "C" int sjd_init(const sjd_config* cfg, const sjd_weights* w, void* strea
   // work buffers
   const int Mp = x.Mpad;
   x.kv_elems = (size_t)c.n_layers * Hkv * x.cap_pad * hd;
-  const size_t kv = x.paged ? 0 : x.kv_elems * x.nstreams;  // every stream's caches
+  // every stream's caches, and what the attention over them needs beside them
+  const size_t kv = x.paged ? 0 : x.kv_elems * x.nstreams;
+  const size_t qsz = x.paged ? 0 : (size_t)Mp * Nq, nsp = x.paged ? 0 : (size_t)H * x.nsplit_max * sjd::kWinRows;
   const size_t xnsz = sjd::act_elems(d, x.mtiles), attsz = sjd::act_elems(Nq, x.mtiles),
                hsz = sjd::act_elems(F, x.mtiles);
   if ((rc = dalloc(x, &x.x, (size_t)Mp * d)) ||
       (rc = dalloc(x, &x.xn, xnsz + attsz + hsz + sjd::kZeroTile)) ||
-      (rc = dalloc(x, &x.q, (size_t)Mp * Nq)) ||
-      (rc = dalloc(x, &x.q_lo, (size_t)Mp * Nq)) || (rc = dalloc(x, &x.kc, kv)) || (rc = dalloc(x, &x.kc_lo, kv)) ||
+      (rc = dalloc(x, &x.q, qsz)) ||
+      (rc = dalloc(x, &x.q_lo, qsz)) || (rc = dalloc(x, &x.kc, kv)) || (rc = dalloc(x, &x.kc_lo, kv)) ||
       (rc = dalloc(x, &x.vt, kv)) || (rc = dalloc(x, &x.vt_lo, kv)) ||
       (rc = dalloc(x, &x.rope, (size_t)x.cap_pad * (hd / 2))) ||
       (rc = dalloc(x, &x.logits[0], (size_t)logit_rows(x) * c.V)) ||
       (rc = dalloc(x, &x.logits[1], (size_t)logit_rows(x) * c.V)) ||
       (rc = dalloc(x, &x.stats[0], (size_t)x.B * c.L)) || (rc = dalloc(x, &x.stats[1], (size_t)x.B * c.L)) ||
-      (rc = dalloc(x, &x.attn_o, (size_t)H * x.nsplit_max * sjd::kWinRows * hd)) ||
-      (rc = dalloc(x, &x.attn_ml, (size_t)H * x.nsplit_max * sjd::kWinRows * 2)) || (rc = dalloc(x, &x.st, x.B)) ||
+      (rc = dalloc(x, &x.attn_o, nsp * hd)) || (rc = dalloc(x, &x.attn_ml, nsp * 2)) || (rc = dalloc(x, &x.st, x.B)) ||
       (rc = dalloc(x, &x.win, 1)) || (rc = dalloc(x, &x.rec, (size_t)x.B * c.L * sjd::kRecInts)) ||
       (rc = dalloc(x, &x.nonfinite, 16)))
     return fail(rc);
@@ -840,7 +841,7 @@ extern "C" int sjd_init(const sjd_config* cfg, const sjd_weights* w, void* strea
   for (void* p : zero) ok = ok && hipMemsetAsync(p, 0, kv * 2, s) == hipSuccess;
   ok = ok && hipMemsetAsync(x.xn, 0, (xnsz + attsz + hsz + sjd::kZeroTile) * 2, s) == hipSuccess;
   void* zero5[] = {x.q, x.q_lo};
-  for (void* p : zero5) ok = ok && hipMemsetAsync(p, 0, (size_t)Mp * Nq * 2, s) == hipSuccess;
+  for (void* p : zero5) ok = ok && hipMemsetAsync(p, 0, qsz * 2, s) == hipSuccess;
   if (!ok) return fail(SJD_EHIP);
   // rotary table in double precision: rope[pos][i] = (cos, sin)(pos * theta^(-2i/hd))
   {
@@ -882,7 +883,7 @@ extern "C" int sjd_init(const sjd_config* cfg, const sjd_weights* w, void* strea
     bool okz = hipMemsetAsync(x.x, 0, (size_t)Mp * d * sizeof(float), s) == hipSuccess;
     for (void* p : zero) okz = okz && hipMemsetAsync(p, 0, kv * 2, s) == hipSuccess;
     okz = okz && hipMemsetAsync(x.xn, 0, xnsz * 2, s) == hipSuccess;
-    for (void* p : zero5) okz = okz && hipMemsetAsync(p, 0, (size_t)Mp * Nq * 2, s) == hipSuccess;
+    for (void* p : zero5) okz = okz && hipMemsetAsync(p, 0, qsz * 2, s) == hipSuccess;
     okz = okz && hipMemsetAsync(x.hbuf, 0, hsz * 2, s) == hipSuccess;
     if (!okz || hipStreamSynchronize(s) != hipSuccess) return fail(SJD_EHIP);
   }

@@ -261,3 +261,25 @@ def test_a_grid_alone_keeps_the_default_precision(over, flags):
     print("max error", err)
     assert err < PAIRS
     eng.close()
+
+
+@pytest.mark.gpu
+def test_pages_instead_of_the_default_buffers():
+    """Device memory of a context of 60000 positions: e4m3 pages are a quarter of the
+    default's caches, and what its attention alone needs is not there."""
+    over = dict(L=16, n_layers=4, n_heads=4, n_kv_heads=4, head_dim=64, d_model=256, ffn_dim=256, max_seq=60000)
+    used = []
+    for flags in (0, sjd.SJD_KV_E4M3):
+        cfg = config(flags, **over)
+        w = weights_device(model_weights(cfg, 3, std=STD))
+        torch.cuda.synchronize()
+        free = torch.cuda.mem_get_info()[0]
+        eng = make_engine(cfg, w)
+        used.append(free - torch.cuda.mem_get_info()[0])
+        eng.close()
+    positions = -(-60000 // 128) * 128
+    planes = 4 * 4 * positions * 64 * 8  # layers, heads, positions, dims; two planes of k and of v
+    splits = 4 * (positions // 128) * 128 * (64 + 2) * 4  # the default attention's partial outputs
+    # (allocations are rounded up: 2 MB each, some 40 of them)
+    assert used[0] >= planes + splits
+    assert used[1] <= planes // 4 * 1.04 + (used[0] - planes - splits) + (16 << 20), used
