@@ -234,7 +234,7 @@ sjd_windows page_windows(const Ctx& x, int M, bool prompt, int cache) {
 // Attention of a context with e4m3 pages, from QKV partial planes to activation
 // tiles: rows, their places, the cache, the attention over it. Rows are bf16: q has to
 // be for the attention's matrix operands, and beside 8 bits of k and v the rounding
-// before the rotation is small (logits of two to four layers off by 0.0260, 0.0197, 0.0494 rms from
+// before the rotation is small (logits of two layers off by 0.0260, 0.0197, 0.0494 rms from
 // those without any rounding, by 0.0251, 0.0189, 0.0477 with one rounding less).
 int paged_layer(Ctx& x, int l, int S, size_t plane, int M, int mt, bool prompt, int cache, hipStream_t s) {
   const sjd_config& c = x.c;
