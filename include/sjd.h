@@ -272,7 +272,7 @@ SJD_API int sjd_verify_given(const sjd_given_params* params, const sjd_given_io*
  * over them (sjd_paged_attention). They allocate nothing and keep nothing from
  * one call to the next, so calls on different streams and captured calls are
  * independent as long as their buffers are. */
-typedef enum { SJD_F32 = 0, SJD_BF16 = 1, SJD_E4M3 = 2 } sjd_dtype;
+typedef enum { SJD_F32 = 0, SJD_BF16 = 1, SJD_E4M3 = 2, SJD_I8 = 3 } sjd_dtype;
 
 /* Rotary positions with several axes (an image token's time, row and column).
  * Pair i of a head (dims i and pairs + i) turns by
@@ -371,6 +371,27 @@ SJD_API int sjd_kv_append(const sjd_pages* pages, const sjd_windows* win, const 
  * (rounded to their type). Positions outside the pool read as zeros. */
 SJD_API int sjd_kv_read(const sjd_pages* pages, const sjd_windows* win, const sjd_kv_rows* rows, void* stream);
 
+/* sjd_rope_axes and sjd_kv_append in one call: the windows' key rows are placed on
+ * their axes and go into the pages with the value rows, rounded once (to the pages'
+ * type), and their query rows are placed in d_out_q. The rows of sequences that are
+ * left out keep their bytes; a window's queries are placed whatever its pages are. */
+typedef struct {
+  int32_t H;         /* query heads, 0..1024; 0: no query rows                          */
+  int32_t pairs;     /* 1 .. head_dim / 2                                            */
+  int32_t axes;      /* 1..4                                                         */
+  int32_t out_dtype; /* of d_out_q: SJD_BF16 or SJD_F32. d_q has the key rows' type     */
+  const double* h_freq;  /* [pairs] finite; host arrays, read during the call           */
+  const uint8_t* h_axis; /* [pairs] < axes                                              */
+  const int32_t* d_pos;  /* [T][axes]                                                 */
+  const void* d_q;       /* [T][H][head_dim], 16-byte aligned                          */
+  void* d_out_q;         /* [T][H][head_dim], 16-byte aligned; may be d_q itself (same type
+                            and stride), else must not overlap the inputs               */
+  int64_t q_row, out_q_row; /* elements between rows, multiples of 8                    */
+} sjd_append_rope;
+
+SJD_API int sjd_kv_append_rope(const sjd_pages* pages, const sjd_windows* win, const sjd_kv_rows* rows,
+                               const sjd_append_rope* rope, void* stream);
+
 /* Attention of the windows' rows over their sequences' pages, which hold the
  * rows' own keys and values already (sjd_kv_append): out = softmax(scale * q . k) v
  * over every cached position and, of the window, over the rows up to itself or
@@ -398,6 +419,81 @@ typedef struct {
 SJD_API int64_t sjd_paged_attention_workspace(const sjd_pages* pages, const sjd_windows* win, int32_t H);
 SJD_API int sjd_paged_attention(const sjd_pages* pages, const sjd_windows* win, const sjd_attention_io* io, void* d_ws,
                                 int64_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* Projections in 8-bit integers, for programs that run their own around this
+ * library's step: rows are quantised with a scale each (sjd_quantise_rows), weights
+ * with a scale per output channel, once (sjd_pack_i8), and the product is exact in
+ * 32-bit integers before the scales (sjd_matmul_i8): a row's result depends on its own
+ * codes alone, not on the rows beside it nor on the launch. Like the operators above
+ * they allocate and keep nothing.
+ *
+ * Rows of codes hold K rounded up to a multiple of 16 of them; those behind K are
+ * multiplied by zeros. */
+
+/* Row t as codes and a scale: y = x, or with d_norm x * norm / sqrt(mean of x^2 + eps)
+ * (RMSNorm), or with d_gate gate / (1 + e^-gate) * x (the input of a gated layer's last
+ * projection); scale[t] = max |y| / 127, code = y * (127 / max |y|) to the nearest, ties
+ * to even. A row with max |y| below 2^-100 counts as zeros (scale 0). A row for which a
+ * y is not finite, or the sum of the x^2 is not, has zeros for codes and NaN for its
+ * scale, so that the products of that row, and of no other, are NaN. Computed in 32
+ * bits. The codes behind K become zero. */
+typedef struct {
+  int32_t T;          /* rows, 0 .. 2^24                                               */
+  int32_t K;          /* 1..65536                                                     */
+  int32_t dtype;      /* of d_x and d_gate: SJD_F32 or SJD_BF16                         */
+  int32_t norm_dtype; /* of d_norm (not looked at without it)                          */
+  float eps;          /* with d_norm: a positive normal number                         */
+  int64_t x_row, gate_row; /* elements between rows, >= K                               */
+  int64_t code_row;   /* bytes between rows, a multiple of 16, >= K rounded up to one    */
+} sjd_quantise_params;
+
+typedef struct {
+  const void* d_x;    /* [T][K]                                                       */
+  const void* d_norm; /* [K], or NULL                                                 */
+  const void* d_gate; /* [T][K], or NULL; not together with d_norm                      */
+  int8_t* d_code;     /* [T][K up to a multiple of 16], 16-byte aligned; must not overlap
+                         the inputs                                                     */
+  float* d_scale;     /* [T]                                                          */
+} sjd_quantise_io;
+
+SJD_API int sjd_quantise_rows(const sjd_quantise_params* params, const sjd_quantise_io* io, void* stream);
+
+/* Weights [N][K] of a projection in the product's layout (32 channels by 32 inputs, in
+ * the order of the matrix operands; made by sjd_pack_i8), and their channels' scales. */
+typedef struct {
+  int32_t N;      /* output channels, 1 .. 2^20                                         */
+  int32_t K;      /* inputs, 1..65536                                                  */
+  void* d_w;      /* sjd_i8_weight_bytes() bytes, 256-byte aligned                      */
+  float* d_scale; /* [N]                                                              */
+} sjd_i8_weights;
+
+/* Bytes of d_w (0 for sizes out of range). */
+SJD_API int64_t sjd_i8_weight_bytes(int32_t N, int32_t K);
+
+/* Lays out d_src [N][K], `row` elements between channels: SJD_I8 codes as they are
+ * (d_scale is the caller's and not touched), or SJD_F32 / SJD_BF16 weights, quantised
+ * by channel as sjd_quantise_rows quantises rows (d_scale is written). */
+SJD_API int sjd_pack_i8(const sjd_i8_weights* weights, const void* d_src, int32_t dtype, int64_t row, void* stream);
+
+/* out[t][n] = code_scale[t] * scale[n] * sum over k of code[t][k] * w[n][k] (+ add[t][n]),
+ * rounded once to out's type behind 32-bit arithmetic. d_ws:
+ * sjd_matmul_i8_workspace() bytes of scratch, 256-byte aligned (NULL when that is 0); it
+ * holds nothing between calls, and calls that overlap in time need one each. */
+typedef struct {
+  int32_t T;                 /* rows, 0 .. 2^24                                        */
+  int32_t dtype;             /* of d_out and d_add: SJD_F32 or SJD_BF16                 */
+  const int8_t* d_code;      /* [T][K up to a multiple of 16], 16-byte aligned          */
+  const float* d_code_scale; /* [T]                                                   */
+  void* d_out;               /* [T][N]; must not overlap the inputs                     */
+  const void* d_add;         /* [T][N] or NULL; may be d_out itself (same stride)        */
+  int64_t code_row;          /* bytes between rows, a multiple of 16                     */
+  int64_t out_row, add_row;  /* elements between rows, >= N                              */
+} sjd_matmul_io;
+
+SJD_API int64_t sjd_matmul_i8_workspace(const sjd_i8_weights* weights, int32_t T);
+SJD_API int sjd_matmul_i8(const sjd_i8_weights* weights, const sjd_matmul_io* io, void* d_ws, int64_t ws_bytes,
+                          void* stream);
 
 /* ------------------------------------------------------------------------ */
 /* Decoder context: weights, KV cache and window state of one generation.

@@ -5,6 +5,7 @@
 #include <cmath>
 
 #include "ops.h"
+#include "rows_i8.h"
 #include "sjd.h"
 
 namespace {
@@ -100,6 +101,61 @@ int check_rows(const sjd_pages* p, const sjd_windows* w, const sjd_kv_rows* r) {
     if (_rc != SJD_OK) return _rc; \
   } while (0)
 
+int check_append_rope(const sjd_pages* p, const sjd_windows* w, const sjd_kv_rows* r, const sjd_append_rope* o) {
+  if (!o || o->H < 0 || o->H > 1024 || o->pairs < 1 || o->pairs > p->head_dim / 2 || o->axes < 1 || o->axes > 4)
+    return SJD_EINVAL;
+  if (!o->h_freq || !o->h_axis) return SJD_EINVAL;
+  for (int i = 0; i < o->pairs; ++i)
+    if (o->h_axis[i] >= o->axes || !std::isfinite(o->h_freq[i])) return SJD_EINVAL;
+  if (o->H && o->out_dtype != SJD_F32 && o->out_dtype != SJD_BF16) return SJD_EINVAL;
+  if (nothing(w)) return SJD_OK;
+  if (!o->d_pos || !aligned(o->d_pos, 4)) return SJD_EINVAL;
+  const int64_t n = (int64_t)o->H * p->head_dim;
+  if (o->H && (!o->d_q || !o->d_out_q || !aligned(o->d_q, 16) || !aligned(o->d_out_q, 16) || o->q_row < n ||
+               o->out_q_row < n || (o->q_row & 7) || (o->out_q_row & 7) ||
+               (o->d_q == o->d_out_q && (o->q_row != o->out_q_row || o->out_dtype != r->dtype))))
+    return SJD_EINVAL;
+  return SJD_OK;
+}
+
+int check_quantise(const sjd_quantise_params* p, const sjd_quantise_io* io) {
+  if (!p || !io || p->T < 0 || p->T > (1 << 24) || p->K < 1 || p->K > sjd::kMaxK) return SJD_EINVAL;
+  if (p->dtype != SJD_F32 && p->dtype != SJD_BF16) return SJD_EINVAL;
+  if (io->d_norm && (io->d_gate || (p->norm_dtype != SJD_F32 && p->norm_dtype != SJD_BF16) || !std::isnormal(p->eps) ||
+                     p->eps < 0))
+    return SJD_EINVAL;
+  const int64_t cols = (p->K + 15) & ~15;
+  if (p->x_row < p->K || (io->d_gate && p->gate_row < p->K) || p->code_row < cols || (p->code_row & 15)) return SJD_EINVAL;
+  if (p->T == 0) return SJD_OK;
+  const uintptr_t es = p->dtype == SJD_F32 ? 4 : 2;
+  if (!io->d_x || !aligned(io->d_x, es) || (io->d_gate && !aligned(io->d_gate, es)) || !io->d_code ||
+      !aligned(io->d_code, 16) || !io->d_scale || !aligned(io->d_scale, 4))
+    return SJD_EINVAL;
+  return !io->d_norm || aligned(io->d_norm, p->norm_dtype == SJD_F32 ? 4 : 2) ? SJD_OK : SJD_EINVAL;
+}
+
+bool i8_sizes(int32_t N, int32_t K) { return N >= 1 && N <= (1 << 20) && K >= 1 && K <= sjd::kMaxK; }
+
+int check_i8_weights(const sjd_i8_weights* w) {
+  if (!w || !i8_sizes(w->N, w->K) || !w->d_w || !aligned(w->d_w, 256) || !w->d_scale || !aligned(w->d_scale, 4))
+    return SJD_EINVAL;
+  return SJD_OK;
+}
+
+int check_matmul(const sjd_i8_weights* w, const sjd_matmul_io* io) {
+  const int st = check_i8_weights(w);
+  if (st != SJD_OK) return st;
+  if (!io || io->T < 0 || io->T > (1 << 24) || (io->dtype != SJD_F32 && io->dtype != SJD_BF16)) return SJD_EINVAL;
+  if (io->code_row < ((w->K + 15) & ~15) || (io->code_row & 15) || io->out_row < w->N || (io->d_add && io->add_row < w->N))
+    return SJD_EINVAL;
+  if (io->T == 0) return SJD_OK;
+  const uintptr_t es = io->dtype == SJD_F32 ? 4 : 2;
+  if (!io->d_code || !aligned(io->d_code, 16) || !io->d_code_scale || !aligned(io->d_code_scale, 4) || !io->d_out ||
+      !aligned(io->d_out, es) || !aligned(io->d_add, es) || (io->d_add == io->d_out && io->add_row != io->out_row))
+    return SJD_EINVAL;
+  return SJD_OK;
+}
+
 int check_heads(const sjd_pages* p, const sjd_windows* w, int32_t H) {
   if (H < 1 || H > 1024 || H % p->n_kv_heads) return SJD_EINVAL;
   // query slots of a window: a launch has 65535 blocks of 128 of them
@@ -137,6 +193,48 @@ extern "C" int sjd_kv_read(const sjd_pages* p, const sjd_windows* w, const sjd_k
   TRY(check_rows(p, w, r));
   if (nothing(w)) return SJD_OK;
   return status(sjd::launch_kv_read(*p, *w, *r, (hipStream_t)stream));
+}
+
+extern "C" int sjd_kv_append_rope(const sjd_pages* p, const sjd_windows* w, const sjd_kv_rows* r, const sjd_append_rope* o,
+                                  void* stream) {
+  TRY(check_pages(p));
+  TRY(check_windows(p, w));
+  TRY(check_rows(p, w, r));
+  TRY(check_append_rope(p, w, r, o));
+  if (nothing(w)) return SJD_OK;
+  return status(sjd::launch_kv_append_rope(*p, *w, *r, *o, (hipStream_t)stream));
+}
+
+extern "C" int sjd_quantise_rows(const sjd_quantise_params* p, const sjd_quantise_io* io, void* stream) {
+  TRY(check_quantise(p, io));
+  if (p->T == 0) return SJD_OK;
+  return status(sjd::launch_quantise_rows(*p, *io, (hipStream_t)stream));
+}
+
+extern "C" int64_t sjd_i8_weight_bytes(int32_t N, int32_t K) {
+  if (!i8_sizes(N, K)) return 0;
+  const sjd::I8Shape s = sjd::i8_shape(N, K);
+  return (int64_t)s.nb * s.ks * 1024;
+}
+
+extern "C" int sjd_pack_i8(const sjd_i8_weights* w, const void* src, int32_t dtype, int64_t row, void* stream) {
+  TRY(check_i8_weights(w));
+  if (dtype != SJD_I8 && dtype != SJD_F32 && dtype != SJD_BF16) return SJD_EINVAL;
+  if (!src || !aligned(src, dtype == SJD_F32 ? 4 : dtype == SJD_BF16 ? 2 : 1) || row < w->K) return SJD_EINVAL;
+  return status(sjd::launch_pack_i8(*w, src, dtype, row, (hipStream_t)stream));
+}
+
+extern "C" int64_t sjd_matmul_i8_workspace(const sjd_i8_weights* w, int32_t T) {
+  if (!w || !i8_sizes(w->N, w->K) || T < 1 || T > (1 << 24)) return 0;
+  return sjd::matmul_i8_ws(*w, T);
+}
+
+extern "C" int sjd_matmul_i8(const sjd_i8_weights* w, const sjd_matmul_io* io, void* d_ws, int64_t ws_bytes, void* stream) {
+  TRY(check_matmul(w, io));
+  if (io->T == 0) return SJD_OK;
+  const int64_t need = sjd::matmul_i8_ws(*w, io->T);
+  if (need && (!d_ws || ws_bytes < need || !aligned(d_ws, 256))) return SJD_EINVAL;
+  return status(sjd::launch_matmul_i8(*w, *io, d_ws, (hipStream_t)stream));
 }
 
 extern "C" int64_t sjd_paged_attention_workspace(const sjd_pages* p, const sjd_windows* w, int32_t H) {

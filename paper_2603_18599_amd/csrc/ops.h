@@ -91,6 +91,9 @@ __device__ __forceinline__ int val_byte(uint32_t i, uint32_t j) {
 hipError_t launch_kv_append(const sjd_pages& p, const sjd_windows& w, const sjd_kv_rows& r, hipStream_t s);
 hipError_t launch_kv_read(const sjd_pages& p, const sjd_windows& w, const sjd_kv_rows& r, hipStream_t s);
 
+hipError_t launch_kv_append_rope(const sjd_pages& p, const sjd_windows& w, const sjd_kv_rows& r, const sjd_append_rope& o,
+                                 hipStream_t s);
+
 // ---- attention over pages
 // Scores are formed in the log2 domain: |scale| * log2(e)
 inline float log2_scale(float scale) { return (float)(1.4426950408889634 * std::fabs((double)scale)); }
@@ -128,6 +131,13 @@ hipError_t launch_page_commit(const DevState* st, const Window* win, const sjd_p
                               const int32_t* table, int table_len, int K, int nstreams, bool guided, hipStream_t s);
 
 hipError_t launch_rope_axes(const sjd_rope_params& p, const sjd_rope_io& io, hipStream_t s);
+
+// ---- projections in 8-bit integers
+hipError_t launch_quantise_rows(const sjd_quantise_params& p, const sjd_quantise_io& io, hipStream_t s);
+hipError_t launch_pack_i8(const sjd_i8_weights& w, const void* src, int dtype, int64_t row, hipStream_t s);
+int64_t matmul_i8_ws(const sjd_i8_weights& w, int T);
+hipError_t launch_matmul_i8(const sjd_i8_weights& w, const sjd_matmul_io& io, void* ws, hipStream_t s);
+
 hipError_t launch_verify_given(const sjd_given_params& p, const sjd_given_io& io, hipStream_t s);
 
 }  // namespace sjd

@@ -1,0 +1,59 @@
+// Rows of 8-bit integers with a scale: the rule that makes one, and the layout of
+// packed weights, shared by the quantiser, the packer and the product.
+#pragma once
+#include "device.h"
+
+namespace sjd {
+
+constexpr int kMaxK = 65536;      // 128 * 128 * kMaxK fits an int32
+constexpr float kLeastRow = 0x1p-100f;  // rows below it count as zeros (127 / max stays finite)
+
+SJD_DEV float elem_f32(uint16_t v) { return bf16_to_f32(v); }
+SJD_DEV float elem_f32(float v) { return v; }
+// (e^-x overflows to infinity below -88: the quotient is then -0, the limit)
+SJD_DEV float silu(float x) { return x / (1.0f + expf(-x)); }
+
+struct RowScale {
+  float scale, inv;  // inv 0: the codes are zeros
+};
+// bits: the largest |y| of the row, as bits
+SJD_DEV RowScale row_scale(uint32_t bits, bool bad) {
+  if (bad || bits >= 0x7F800000u) return {__uint_as_float(0x7FC00000u), 0.0f};
+  const float m = __uint_as_float(bits);
+  if (m < kLeastRow) return {0.0f, 0.0f};
+  return {m / 127.0f, 127.0f / m};
+}
+SJD_DEV int8_t code_of(float y, float inv) { return (int8_t)(int)fminf(fmaxf(rintf(y * inv), -127.0f), 127.0f); }
+
+// over a workgroup of N threads (scratch: a word per wave)
+template <int N>
+SJD_DEV float block_sum(float v, float* scratch) {
+  v = wave_sum(v);
+  if ((threadIdx.x & 63) == 0) scratch[threadIdx.x >> 6] = v;
+  __syncthreads();
+  v = 0.0f;
+#pragma unroll
+  for (int w = 0; w < N / kWave; ++w) v += scratch[w];
+  return v;
+}
+template <int N>
+SJD_DEV uint32_t block_max(uint32_t v, uint32_t* scratch) {
+  v = wave_reduce32(v, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
+  if ((threadIdx.x & 63) == 0) scratch[threadIdx.x >> 6] = v;
+  __syncthreads();
+  v = 0;
+#pragma unroll
+  for (int w = 0; w < N / kWave; ++w) v = max(v, scratch[w]);
+  return v;
+}
+
+// Packed weights: tiles of 32 channels x 32 inputs, 1 KB, channels and inputs (up to a
+// multiple of 128) padded with zeros. Channel n, input k of a tile: byte 16 * (n + 32 *
+// (k / 16)) + k % 16, so a wave reads a tile as an operand of the 32x32x32 MFMA with
+// one contiguous load. Tiles of a row block lie one behind the other.
+struct I8Shape {
+  int nb, ks;  // row blocks, tiles of a row block
+};
+__host__ __device__ inline I8Shape i8_shape(int N, int K) { return {(N + 31) / 32, (K + 127) / 128 * 4}; }
+
+}  // namespace sjd

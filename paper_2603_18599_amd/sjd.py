@@ -105,10 +105,37 @@ class AttentionIO(C.Structure):
                 ("q_row", C.c_int64), ("out_row", C.c_int64), ("d_anc", C.c_void_p)]
 
 
+class AppendRope(C.Structure):
+    _fields_ = [("H", C.c_int32), ("pairs", C.c_int32), ("axes", C.c_int32), ("out_dtype", C.c_int32),
+                ("h_freq", C.c_void_p), ("h_axis", C.c_char_p), ("d_pos", C.c_void_p), ("d_q", C.c_void_p),
+                ("d_out_q", C.c_void_p), ("q_row", C.c_int64), ("out_q_row", C.c_int64)]
+
+
+class QuantiseParams(C.Structure):
+    _fields_ = [("T", C.c_int32), ("K", C.c_int32), ("dtype", C.c_int32), ("norm_dtype", C.c_int32), ("eps", C.c_float),
+                ("x_row", C.c_int64), ("gate_row", C.c_int64), ("code_row", C.c_int64)]
+
+
+class QuantiseIO(C.Structure):
+    _fields_ = [("d_x", C.c_void_p), ("d_norm", C.c_void_p), ("d_gate", C.c_void_p), ("d_code", C.c_void_p),
+                ("d_scale", C.c_void_p)]
+
+
+class I8WeightsDesc(C.Structure):
+    _fields_ = [("N", C.c_int32), ("K", C.c_int32), ("d_w", C.c_void_p), ("d_scale", C.c_void_p)]
+
+
+class MatmulIO(C.Structure):
+    _fields_ = [("T", C.c_int32), ("dtype", C.c_int32), ("d_code", C.c_void_p), ("d_code_scale", C.c_void_p),
+                ("d_out", C.c_void_p), ("d_add", C.c_void_p), ("code_row", C.c_int64), ("out_row", C.c_int64),
+                ("add_row", C.c_int64)]
+
+
 EXPORTS = ["sjd_status_str", "sjd_verify", "sjd_verify_noalloc", "sjd_init", "sjd_prefill", "sjd_prefill_image",
            "sjd_prefill_cfg", "sjd_prefill_image_cfg", "sjd_set_drafts", "sjd_step", "sjd_forward_window",
            "sjd_get_plan", "sjd_destroy", "sjd_verify_given", "sjd_rope_axes", "sjd_page_bytes", "sjd_kv_append",
-           "sjd_kv_read", "sjd_paged_attention_workspace", "sjd_paged_attention"]
+           "sjd_kv_read", "sjd_paged_attention_workspace", "sjd_paged_attention", "sjd_kv_append_rope", "sjd_quantise_rows",
+           "sjd_i8_weight_bytes", "sjd_pack_i8", "sjd_matmul_i8_workspace", "sjd_matmul_i8"]
 
 _lib = None
 
@@ -173,6 +200,19 @@ def load_library():
     lib.sjd_paged_attention.restype = C.c_int
     lib.sjd_paged_attention.argtypes = [C.POINTER(PagesDesc), C.POINTER(WindowsDesc), C.POINTER(AttentionIO),
                                         C.c_void_p, C.c_int64, C.c_void_p]
+    lib.sjd_kv_append_rope.restype = C.c_int
+    lib.sjd_kv_append_rope.argtypes = [C.POINTER(PagesDesc), C.POINTER(WindowsDesc), C.POINTER(KvRows),
+                                       C.POINTER(AppendRope), C.c_void_p]
+    lib.sjd_quantise_rows.restype = C.c_int
+    lib.sjd_quantise_rows.argtypes = [C.POINTER(QuantiseParams), C.POINTER(QuantiseIO), C.c_void_p]
+    lib.sjd_i8_weight_bytes.restype = C.c_int64
+    lib.sjd_i8_weight_bytes.argtypes = [C.c_int32, C.c_int32]
+    lib.sjd_pack_i8.restype = C.c_int
+    lib.sjd_pack_i8.argtypes = [C.POINTER(I8WeightsDesc), C.c_void_p, C.c_int32, C.c_int64, C.c_void_p]
+    lib.sjd_matmul_i8_workspace.restype = C.c_int64
+    lib.sjd_matmul_i8_workspace.argtypes = [C.POINTER(I8WeightsDesc), C.c_int32]
+    lib.sjd_matmul_i8.restype = C.c_int
+    lib.sjd_matmul_i8.argtypes = [C.POINTER(I8WeightsDesc), C.POINTER(MatmulIO), C.c_void_p, C.c_int64, C.c_void_p]
     _lib = lib
     return lib
 
@@ -386,6 +426,29 @@ def sjd_kv_read(pages, win, k, v, stream=None):
     _kv_call("sjd_kv_read", pages, win, k, v, stream)
 
 
+def sjd_kv_append_rope(pages, win, k, v, pos, freq, axis, *, q=None, out_q=None, stream=None):
+    """Places rows k [T, Hkv, hd] on their axes and writes them with rows v into
+    the windows' pages, and places queries q [T, H, hd] in out_q (in place
+    unless given; bfloat16 or float32) (sjd_kv_append_rope in include/sjd.h).
+    k, v and q have one type, bfloat16 or float32. pos int32 [T, axes]; freq and
+    axis: one frequency and one axis for each pair of dims."""
+    fn = "sjd_kv_append_rope"
+    torch, types = _types()
+    T, hd, dev, dt = win.T, pages.head_dim, pages.device, k.dtype
+    _expect(fn, dt is v.dtype and win.device == dev and k.get_device() == dev and v.get_device() == dev and
+            pos.dim() == 2 and len(axis) == len(freq) and (q is not None or out_q is None))
+    axes, f, ax = pos.shape[1], array("d", freq), bytes(axis)
+    rows = KvRows(k.data_ptr(), v.data_ptr(), _row_stride(fn, k, T, pages.n_kv_heads, hd),
+                  _row_stride(fn, v, T, pages.n_kv_heads, hd), types.get(dt, -1))
+    par = AppendRope(0, len(f), axes, 1, f.buffer_info()[0], ax, _dense(fn, pos, (T, axes), torch.int32, dev))
+    if q is not None:
+        out = q if out_q is None else out_q
+        _expect(fn, q.dim() == 3 and q.dtype is dt and q.get_device() == dev and out.get_device() == dev)
+        par.H, par.out_dtype, par.d_q, par.d_out_q = q.shape[1], types.get(out.dtype, -1), q.data_ptr(), out.data_ptr()
+        par.q_row, par.out_q_row = _row_stride(fn, q, T, par.H, hd), _row_stride(fn, out, T, par.H, hd)
+    _launch(fn, stream, dev, C.byref(pages.desc), C.byref(win.desc), C.byref(rows), C.byref(par))
+
+
 def attention_workspace(pages, win, H):
     """Scratch for sjd_paged_attention with these pages and windows (calls that
     overlap in time need one each)."""
@@ -407,6 +470,98 @@ def sjd_paged_attention(pages, win, q, out, ws, *, scale, anc=None, stream=None)
     io = AttentionIO(H, scale, q.data_ptr(), out.data_ptr(), _row_stride(fn, q, T, H, hd), _row_stride(fn, out, T, H, hd),
                      None if anc is None else _dense(fn, anc, (T,), torch.int64, dev))
     _launch(fn, stream, dev, C.byref(pages.desc), C.byref(win.desc), C.byref(io), ws.data_ptr(), size)
+
+
+def _rows2(fn, t, T, cols, device):
+    """Address and row stride of [T, cols] rows whose elements lie one behind the other."""
+    if t.shape != (T, cols) or t.get_device() != device:
+        raise SjdError(fn, -1)
+    if t.is_contiguous():
+        return t.data_ptr(), cols
+    s = t.stride()
+    _expect(fn, T > 1 and (cols == 1 or s[1] == 1))
+    return t.data_ptr(), s[0]
+
+
+def code_columns(K):
+    """Columns of a row of K codes: a multiple of 16."""
+    return (K + 15) // 16 * 16
+
+
+def sjd_quantise_rows(x, code, scale, *, norm=None, gate=None, eps=1e-5, stream=None):
+    """Rows x [T, K] (bfloat16 or float32) as int8 codes [T, code_columns(K)] and
+    float32 scales [T] (sjd_quantise_rows in include/sjd.h), behind an RMSNorm of
+    gains norm [K] or times silu(gate) (gate [T, K] of x's type)."""
+    fn = "sjd_quantise_rows"
+    torch, types = _types()
+    _expect(fn, x.dim() == 2 and code.dtype is torch.int8)
+    (T, K), dt, dev = x.shape, x.dtype, x.get_device()
+    xp, x_row = _rows2(fn, x, T, K, dev)
+    cp, code_row = _rows2(fn, code, T, code_columns(K), dev)
+    npt, norm_type, gp, gate_row = None, 0, None, 0
+    if norm is not None:
+        npt, norm_type = _dense(fn, norm, (K,), norm.dtype, dev), types.get(norm.dtype, -1)
+    if gate is not None:
+        _expect(fn, gate.dtype is dt)
+        gp, gate_row = _rows2(fn, gate, T, K, dev)
+    par = QuantiseParams(T, K, types.get(dt, -1), norm_type, eps, x_row, gate_row, code_row)
+    io = QuantiseIO(xp, npt, gp, cp, _dense(fn, scale, (T,), torch.float32, dev))
+    _launch(fn, stream, dev, C.byref(par), C.byref(io))
+
+
+class I8Weights:
+    """Weights of a projection with N outputs and K inputs in 8 bits
+    (sjd_i8_weights); sjd_pack_i8 fills them. scale: float32 [N], the channels'
+    scales (codes: the caller's; None: made here for weights that are
+    quantised)."""
+
+    def __init__(self, N, K, scale=None, device="cuda"):
+        fn, torch = "sjd_i8_weights", _types()[0]
+        size = load_library().sjd_i8_weight_bytes(N, K)
+        _expect(fn, size > 0)
+        if scale is None:
+            scale = torch.empty(N, dtype=torch.float32, device=device)
+        self.N, self.K, self.scale, self.device = N, K, scale, scale.get_device()
+        self.w = torch.empty(size, dtype=torch.uint8, device=scale.device)
+        self.desc = I8WeightsDesc(N, K, self.w.data_ptr(), _dense(fn, scale, (N,), torch.float32, self.device))
+
+
+def sjd_pack_i8(weights, src, stream=None):
+    """Lays src [N, K] out as weights (sjd_pack_i8 in include/sjd.h): int8 codes,
+    or bfloat16 / float32 weights, which are quantised (weights.scale is
+    written)."""
+    fn = "sjd_pack_i8"
+    torch, types = _types()
+    p, row = _rows2(fn, src, weights.N, weights.K, weights.device)
+    _launch(fn, stream, weights.device, C.byref(weights.desc), p, 3 if src.dtype is torch.int8 else types.get(src.dtype, -1),
+            row)
+
+
+def matmul_workspace(weights, T):
+    """Scratch for sjd_matmul_i8 of T rows with these weights (calls that overlap in
+    time need one each)."""
+    n = load_library().sjd_matmul_i8_workspace(C.byref(weights.desc), T)
+    return _types()[0].empty(n, dtype=_types()[0].uint8, device=weights.w.device)
+
+
+def sjd_matmul_i8(weights, code, code_scale, out, ws, *, add=None, stream=None):
+    """Product of rows of codes [T, code_columns(K)] and scales [T] with weights
+    into out [T, N] (bfloat16 or float32), plus add (of out's type and shape, may
+    be out itself) (sjd_matmul_i8 in include/sjd.h). ws: matmul_workspace."""
+    fn = "sjd_matmul_i8"
+    torch, types = _types()
+    _expect(fn, out.dim() == 2 and code.dtype is torch.int8 and ws.dtype is torch.uint8 and ws.is_contiguous())
+    T, N, dev, size, dt = out.shape[0], weights.N, weights.device, ws.numel(), out.dtype
+    cp, code_row = _rows2(fn, code, T, code_columns(weights.K), dev)
+    op, out_row = _rows2(fn, out, T, N, dev)
+    ap, add_row = None, 0
+    if add is not None:
+        _expect(fn, add.dtype is dt)
+        ap, add_row = (op, out_row) if add is out else _rows2(fn, add, T, N, dev)
+    _expect(fn, size == 0 or ws.get_device() == dev)
+    io = MatmulIO(T, types.get(dt, -1), cp, _dense(fn, code_scale, (T,), torch.float32, dev), op, ap, code_row, out_row,
+                  add_row)
+    _launch(fn, stream, dev, C.byref(weights.desc), C.byref(io), ws.data_ptr(), size)
 
 
 class Engine:
