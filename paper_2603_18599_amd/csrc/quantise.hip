@@ -1,6 +1,8 @@
 // Rows as 8-bit integers with a scale each (definition: sjd.h), the input of the
 // products in matmul_i8.hip, with what stands in front of a projection: an RMSNorm or
 // the gate of a gated layer.
+#include <type_traits>
+
 #include "device.h"
 #include "ops.h"
 #include "rows_i8.h"
@@ -9,68 +11,132 @@ namespace sjd {
 
 namespace {
 
+template <int N>
+using Int = std::integral_constant<int, N>;
+
 struct QuantArgs {
   const void *x, *norm, *gate;
   int8_t* code;
   float* scale;
   int64_t x_row, gate_row, code_row;
-  int K;
+  int T, K;
+  int x_wide, gate_wide, norm_wide;  // 16-byte loads are aligned
   int norm_f32;
   float inv_k, eps;
 };
 
-constexpr int kThreads = 256;
+// Elements k .. k + 7 of a row, zeros behind K
+template <class E>
+SJD_DEV void load8(const E* row, int k, int K, bool wide, float (&v)[8]) {
+  if (wide && k + 8 <= K) {
+    constexpr int N = sizeof(E) / 2;  // 16-byte pieces
+    uint4 p[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) p[i] = ((const uint4*)(row + k))[i];
+    if constexpr (N == 2) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(((const uint32_t*)p)[e]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = bf16_to_f32((uint16_t)(((const uint32_t*)p)[e / 2] >> (16 * (e & 1))));
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = k + e < K ? elem_f32(row[k + e]) : 0.0f;
+  }
+}
 
-// E: element (uint16_t bf16, float)
-template <class E, bool NORM, bool GATE>
-__global__ __launch_bounds__(kThreads) void k_quantise(QuantArgs a) {
-  __shared__ float red[kThreads / kWave];
-  __shared__ uint32_t redu[kThreads / kWave];
-  const int64_t t = blockIdx.x;
+// NT threads hold a row in P pieces of 8 elements each; a wave per row (four to a
+// workgroup) needs no barrier. E: element (uint16_t bf16, float)
+template <class E, int NT, int P, bool NORM, bool GATE>
+__global__ __launch_bounds__(NT < 256 ? 256 : NT) void k_quantise(QuantArgs a) {
+  __shared__ float red[NT / kWave];
+  __shared__ uint32_t redu[NT / kWave];
+  const int64_t t = NT == kWave ? blockIdx.x * 4LL + (threadIdx.x >> 6) : blockIdx.x;
+  if (NT == kWave && t >= a.T) return;
+  const int tid = threadIdx.x % NT, cols = (a.K + 15) & ~15;
   const E* x = (const E*)a.x + t * a.x_row;
-  const E* gate = (const E*)a.gate + t * a.gate_row;
-  float rinv = 0.0f;
+  float y[P][8];
+#pragma unroll
+  for (int i = 0; i < P; ++i) load8(x, (tid + i * NT) * 8, a.K, a.x_wide, y[i]);
   bool bad = false;
   if constexpr (NORM) {
     float ss = 0.0f;
-    for (int k = threadIdx.x; k < a.K; k += kThreads) {
-      const float v = elem_f32(x[k]);
-      ss += v * v;
-    }
-    ss = block_sum<kThreads>(ss, red);
+#pragma unroll
+    for (int i = 0; i < P; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) ss = __builtin_fmaf(y[i][e], y[i][e], ss);
+    ss = NT == kWave ? wave_sum(ss) : block_sum<NT>(ss, red);
     bad = !(ss < INFINITY);
-    rinv = 1.0f / sqrtf(ss * a.inv_k + a.eps);
+    const float rinv = 1.0f / sqrtf(ss * a.inv_k + a.eps);
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      const int k = (tid + i * NT) * 8;
+      float g[8];
+      if (a.norm_f32) load8((const float*)a.norm, k, a.K, a.norm_wide, g);
+      else load8((const uint16_t*)a.norm, k, a.K, a.norm_wide, g);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[i][e] = y[i][e] * rinv * g[e];
+    }
   }
-  auto y = [&](int k) {
-    const float v = elem_f32(x[k]);
-    if constexpr (NORM) return v * rinv * (a.norm_f32 ? ((const float*)a.norm)[k] : bf16_to_f32(((const uint16_t*)a.norm)[k]));
-    if constexpr (GATE) return v * silu(elem_f32(gate[k]));
-    return v;
-  };
+  if constexpr (GATE) {
+    const E* gate = (const E*)a.gate + t * a.gate_row;
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      float g[8];
+      load8(gate, (tid + i * NT) * 8, a.K, a.gate_wide, g);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[i][e] *= silu(g[e]);
+    }
+  }
   uint32_t m = 0;  // (as bits: NaN is above infinity)
-  for (int k = threadIdx.x; k < a.K; k += kThreads) m = max(m, __float_as_uint(y(k)) & 0x7FFFFFFFu);
-  m = block_max<kThreads>(m, redu);
+#pragma unroll
+  for (int i = 0; i < P; ++i)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) m = max(m, __float_as_uint(y[i][e]) & 0x7FFFFFFFu);
+  m = NT == kWave ? wave_max_u32(m) : block_max<NT>(m, redu);
   const RowScale rs = row_scale(m, bad);
-  if (threadIdx.x == 0) a.scale[t] = rs.scale;
+  if (tid == 0) a.scale[t] = rs.scale;
   int8_t* code = a.code + t * a.code_row;
-  const int cols = (a.K + 15) & ~15;
-  for (int k = threadIdx.x; k < cols; k += kThreads) code[k] = k < a.K && rs.inv > 0.0f ? code_of(y(k), rs.inv) : 0;
+#pragma unroll
+  for (int i = 0; i < P; ++i) {
+    const int k = (tid + i * NT) * 8;
+    if (k >= cols) break;
+    uint32_t w[2] = {};
+    if (rs.inv > 0.0f)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w[e / 4] |= (uint32_t)(uint8_t)code_of(y[i][e], rs.inv) << (8 * (e & 3));
+    *(uint2*)(code + k) = make_uint2(w[0], w[1]);
+  }
 }
 
 }  // namespace
 
 hipError_t launch_quantise_rows(const sjd_quantise_params& p, const sjd_quantise_io& io, hipStream_t s) {
-  const QuantArgs a{io.d_x, io.d_norm, io.d_gate, io.d_code, io.d_scale, p.x_row, p.gate_row, p.code_row, p.K,
-                    p.norm_dtype == SJD_F32, (float)(1.0 / p.K), p.eps};
-  const dim3 grid(p.T), block(kThreads);
-  auto go = [&](auto e) {
-    using E = decltype(e);
-    if (io.d_norm) hipLaunchKernelGGL((k_quantise<E, true, false>), grid, block, 0, s, a);
-    else if (io.d_gate) hipLaunchKernelGGL((k_quantise<E, false, true>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((k_quantise<E, false, false>), grid, block, 0, s, a);
+  auto wide = [](const void* q, int64_t row, int dtype) {
+    return ((uintptr_t)q & 15) == 0 && row % (dtype == SJD_F32 ? 4 : 8) == 0;
   };
-  if (p.dtype == SJD_F32) go(float{});
-  else go(uint16_t{});
+  const QuantArgs a{io.d_x, io.d_norm, io.d_gate, io.d_code, io.d_scale, p.x_row, p.gate_row, p.code_row, p.T, p.K,
+                    wide(io.d_x, p.x_row, p.dtype), wide(io.d_gate, p.gate_row, p.dtype), wide(io.d_norm, 0, p.norm_dtype),
+                    p.norm_dtype == SJD_F32, (float)(1.0 / p.K), p.eps};
+  auto go = [&](auto e, auto nt, auto pieces) {
+    using E = decltype(e);
+    constexpr int NT = decltype(nt)::value, P = decltype(pieces)::value;
+    const dim3 grid(NT == kWave ? (p.T + 3) / 4 : p.T), block(NT < 256 ? 256 : NT);
+    if (io.d_norm) hipLaunchKernelGGL((k_quantise<E, NT, P, true, false>), grid, block, 0, s, a);
+    else if (io.d_gate) hipLaunchKernelGGL((k_quantise<E, NT, P, false, true>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((k_quantise<E, NT, P, false, false>), grid, block, 0, s, a);
+  };
+  // (by K alone: the order of a row's sum does not depend on the rows beside it)
+  auto pick = [&](auto e) {
+    if (p.K <= 512) go(e, Int<64>{}, Int<1>{});
+    else if (p.K <= 2048) go(e, Int<64>{}, Int<4>{});
+    else if (p.K <= 4096) go(e, Int<256>{}, Int<2>{});
+    else if (p.K <= 16384) go(e, Int<1024>{}, Int<2>{});
+    else go(e, Int<1024>{}, Int<8>{});
+  };
+  if (p.dtype == SJD_F32) pick(float{});
+  else pick(uint16_t{});
   return hipGetLastError();
 }
 

@@ -36,9 +36,12 @@ SJD_DEV float block_sum(float v, float* scratch) {
   for (int w = 0; w < N / kWave; ++w) v += scratch[w];
   return v;
 }
+SJD_DEV uint32_t wave_max_u32(uint32_t v) {
+  return wave_reduce32(v, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
+}
 template <int N>
 SJD_DEV uint32_t block_max(uint32_t v, uint32_t* scratch) {
-  v = wave_reduce32(v, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
+  v = wave_max_u32(v);
   if ((threadIdx.x & 63) == 0) scratch[threadIdx.x >> 6] = v;
   __syncthreads();
   v = 0;
