@@ -27,7 +27,9 @@ struct MatArgs {
   int T, N, cols;  // cols: codes of a row that are there
   int nb, ks;
   int f32;
-  int pair;  // bf16 outputs may be stored two channels at a time
+  int wide;  // four channels of a row are aligned for one access
+  int splits;      // of the inputs; with more than one
+  int32_t* sums;   // .. sums of their parts, [splits][T][32 nb]
 };
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -37,45 +39,42 @@ SJD_DEV uint32_t pk_bf16(float a, float b) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
 }
 
-SJD_DEV void put(const MatArgs& a, int t, int n, int sum, float ws, float cs) {
-  float v = (float)sum * ws * cs;
-  if (a.f32) {
-    if (a.add) v += ((const float*)a.add)[t * a.add_row + n];
-    ((float*)a.out)[t * a.out_row + n] = v;
-  } else {
-    if (a.add) v += bf16_to_f32(((const uint16_t*)a.add)[t * a.add_row + n]);
-    ((uint16_t*)a.out)[t * a.out_row + n] = f32_to_bf16(v);
+// Channels n .. n + 3 of row t, from their sums
+SJD_DEV void put(const MatArgs& a, int t, int n, const i32x4& sum, const float4& ws, float cs) {
+  float v[4] = {(float)sum[0] * ws.x * cs, (float)sum[1] * ws.y * cs, (float)sum[2] * ws.z * cs, (float)sum[3] * ws.w * cs};
+  const int64_t at = t * a.out_row + n, from = t * a.add_row + n;
+  if (a.wide && n + 4 <= a.N) {
+    if (a.f32) {
+      if (a.add) {
+        const float4 x = *(const float4*)((const float*)a.add + from);
+        v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
+      }
+      *(float4*)((float*)a.out + at) = make_float4(v[0], v[1], v[2], v[3]);
+    } else {
+      if (a.add) {
+        const uint2 x = *(const uint2*)((const uint16_t*)a.add + from);
+        v[0] += __uint_as_float(x.x << 16); v[1] += __uint_as_float(x.x & 0xFFFF0000u);
+        v[2] += __uint_as_float(x.y << 16); v[3] += __uint_as_float(x.y & 0xFFFF0000u);
+      }
+      *(uint2*)((uint16_t*)a.out + at) = make_uint2(pk_bf16(v[0], v[1]), pk_bf16(v[2], v[3]));
+    }
+    return;
   }
-}
-
-// C rows (channels) of register i: 8 (i / 4) + 4 half + i % 4; column (row of codes) lane % 32
-SJD_DEV void finish(const MatArgs& a, const i32x16& c, int n0, int t) {
-  if (t >= a.T) return;
-  const float cs = a.cscale[t];
-  const int half = (threadIdx.x & 63) >> 5;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const int n = n0 + 8 * (i >> 2) + 4 * half + (i & 3);
-    if (n < a.N) put(a, t, n, c[i], a.wscale[n], cs);
+  for (int e = 0; e < 4; ++e) {
+    if (n + e >= a.N) break;
+    if (a.f32) {
+      if (a.add) v[e] += ((const float*)a.add)[from + e];
+      ((float*)a.out)[at + e] = v[e];
+    } else {
+      if (a.add) v[e] += bf16_to_f32(((const uint16_t*)a.add)[from + e]);
+      ((uint16_t*)a.out)[at + e] = f32_to_bf16(v[e]);
+    }
   }
 }
-
-// A wave: 32 channels x 32 rows, operands straight from memory. Rows past T read the last
-// row, codes past the row's end its first ones (against weights of zero).
-__global__ __launch_bounds__(256) void k_matmul_i8(MatArgs a) {
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, half = lane >> 5;
-  const int nb = blockIdx.y * 4 + wave;
-  if (nb >= a.nb) return;
-  const int t = blockIdx.x * 32 + (lane & 31);
-  const int8_t* code = a.code + min(t, a.T - 1) * a.code_row;
-  const char* w = a.w + (int64_t)nb * a.ks * 1024 + lane * 16;
-  i32x16 c = {};
-  for (int ks = 0; ks < a.ks; ++ks) {
-    const int k = ks * 32 + 16 * half;
-    const i32x4 x = *(const i32x4*)(w + (int64_t)ks * 1024), y = *(const i32x4*)(code + (k < a.cols ? k : 0));
-    c = __builtin_amdgcn_mfma_i32_32x32x32_i8(x, y, c, 0, 0, 0);
-  }
-  finish(a, c, nb * 32, t);
+SJD_DEV float4 channel_scales(const MatArgs& a, int n) {
+  return make_float4(a.wscale[min(n, a.N - 1)], a.wscale[min(n + 1, a.N - 1)], a.wscale[min(n + 2, a.N - 1)],
+                     a.wscale[min(n + 3, a.N - 1)]);
 }
 
 // Few rows: the weights pass once. A workgroup has CH channels and TT tiles of CH rows;
@@ -103,11 +102,18 @@ struct FewMfma<16> {
   static SJD_DEV int n(int lane, int) { return 4 * (lane >> 4); }
 };
 
+// Where a row of P pieces of 16 bytes in LDS has piece p, and which piece lies at place p: the
+// 16 rows that a read takes at a time cover all 64 banks
+template <int P>
+SJD_DEV int swizzle(int row, int p) {
+  static_assert(P == 4 || P == 8, "16 rows of P pieces: P times all banks");
+  return p ^ (P == 8 ? row >> 1 & 7 : row >> 2 & 3);
+}
+
 constexpr int kFewWaves = 8;
 
 // STAGE: codes are loaded eight lanes to a row's 128 bytes and pass through the wave's own
-// part of LDS, 16-byte pieces exchanged so that rows eight apart share banks; else
-// each lane loads its operand, which touches a line per row.
+// part of LDS; else each lane loads its operand, which touches a line per row.
 template <int CH, int TT, int DEPTH, bool STAGE>
 __global__ __launch_bounds__(64 * kFewWaves, 2) void k_matmul_few(MatArgs a) {
   using M = FewMfma<CH>;
@@ -117,8 +123,8 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void k_matmul_few(MatArgs a) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int t0 = blockIdx.y * (CH * TT), n0 = blockIdx.x * CH;
   const char* w = a.w + (int64_t)(n0 >> 5) * a.ks * 1024 + M::w(lane, (n0 >> 4) & 1);
-  // STAGE: a load is rows 8 p .. + 7 of a tile, piece lane % 8 ^ row
-  const int k0 = STAGE ? 16 * ((lane & 7) ^ (lane >> 3)) : M::k(lane);
+  // STAGE: a load is rows 8 p .. + 7 of a tile
+  const int k0 = STAGE ? 0 : M::k(lane);
   constexpr int ROWS = STAGE ? TT * S : TT;
   const int8_t* code[ROWS];
 #pragma unroll
@@ -131,7 +137,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void k_matmul_few(MatArgs a) {
 #pragma unroll
     for (int s = 0; s < S; ++s) {
       x[d][s] = *(const i32x4*)(w + (int64_t)u * 4096 + s * (4096 / S));
-      const int k = u * 128 + (STAGE ? 0 : s * (128 / S)) + k0;
+      const int k = u * 128 + (STAGE ? 16 * swizzle<8>(8 * s + (lane >> 3), lane & 7) : s * (128 / S)) + k0;
 #pragma unroll
       for (int i = 0; i < TT; ++i) y[d][i][s] = *(const i32x4*)(code[STAGE ? i * S + s : i] + (k < a.cols ? k : 0));
     }
@@ -156,7 +162,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void k_matmul_few(MatArgs a) {
         for (int i = 0; i < TT; ++i) {
           if constexpr (STAGE) {
             const int row = lane % CH, piece = s * (8 / S) + lane / CH;
-            const i32x4 v = *(const i32x4*)(mine + i * (CH * 32) + row * 32 + 4 * (piece ^ (row & 7)));
+            const i32x4 v = *(const i32x4*)(mine + i * (CH * 32) + row * 32 + 4 * swizzle<8>(row, piece));
             c[i] = M::mma(x[d][s], v, c[i]);
           } else {
             c[i] = M::mma(x[d][s], y[d][i][s], c[i]);
@@ -172,83 +178,78 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void k_matmul_few(MatArgs a) {
     for (int r = 0; r < M::kRegs; r += 4)
       *(i32x4*)&sums[wave][(lane % CH) * ROW + M::n(lane, r / 4)] = i32x4{c[i][r], c[i][r + 1], c[i][r + 2], c[i][r + 3]};
     __syncthreads();
-    for (int e = threadIdx.x; e < CH * CH; e += 64 * kFewWaves) {
-      const int t = t0 + CH * i + e / CH, n = n0 + e % CH;
-      if (t >= a.T || n >= a.N) continue;
-      int sum = 0;
+    if (threadIdx.x >= CH * CH / 4) continue;
+    const int row = threadIdx.x / (CH / 4), col = threadIdx.x % (CH / 4) * 4, t = t0 + CH * i + row, n = n0 + col;
+    if (t >= a.T || n >= a.N) continue;
+    i32x4 sum = {};
 #pragma unroll
-      for (int v = 0; v < kFewWaves; ++v) sum += sums[v][e / CH * ROW + e % CH];
-      put(a, t, n, sum, a.wscale[n], a.cscale[t]);
-    }
+    for (int v = 0; v < kFewWaves; ++v) sum += *(const i32x4*)&sums[v][row * ROW + col];
+    put(a, t, n, sum, channel_scales(a, n), a.cscale[t]);
   }
 }
 
-// Scales, addend and stores of a wave's FT x FN blocks from row t0, channel n0. Register r of
-// a block: row 8 (r / 4) + 4 (lane / 32) + r % 4, channel lane % 32. bf16: two lanes
-// exchange halves of two rows, so that each stores two channels of one.
-template <bool F32, bool ADD, int FT, int FN>
-SJD_DEV void finish_many(const MatArgs& a, const i32x16 (&c)[FT][FN], int t0, int n0) {
-  using E = std::conditional_t<F32, float, uint16_t>;
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int i = 0; i < FT; ++i) {
-    const int tb = t0 + 32 * i + 4 * (lane >> 5);
-    float cs[16];
-#pragma unroll
-    for (int r = 0; r < 16; ++r) cs[r] = a.cscale[min(tb + 8 * (r >> 2) + (r & 3), a.T - 1)];
-#pragma unroll
-    for (int j = 0; j < FN; ++j) {
-      const int n = n0 + 32 * j + (lane & 31);
-      const float ws = a.wscale[min(n, a.N - 1)];
-      float v[16];
-      if constexpr (ADD) {
-        const E* add = (const E*)a.add + min(n, a.N - 1);
-        E x[16];
-#pragma unroll
-        for (int r = 0; r < 16; ++r) x[r] = add[min(tb + 8 * (r >> 2) + (r & 3), a.T - 1) * a.add_row];
-#pragma unroll
-        for (int r = 0; r < 16; ++r) v[r] = (float)c[i][j][r] * ws * cs[r] + elem_f32(x[r]);
-      } else {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) v[r] = (float)c[i][j][r] * ws * cs[r];
-      }
-      if constexpr (F32) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int t = tb + 8 * (r >> 2) + (r & 3);
-          if (t < a.T && n < a.N) ((float*)a.out)[t * a.out_row + n] = v[r];
-        }
-      } else {
-#pragma unroll
-        for (int r = 0; r < 16; r += 2) {
-          const uint32_t p = pk_bf16(v[r], v[r + 1]);
-          const int t = tb + 8 * (r >> 2) + (r & 3);
-          if (a.pair) {
-            const uint32_t o = dpp::mov<dpp::kXor1>(p);
-            const bool odd = lane & 1;
-            const uint32_t q = odd ? (o >> 16) | (p & 0xFFFF0000u) : (p & 0xFFFFu) | (o << 16);
-            const int tq = t + odd, nq = n & ~1;
-            if (tq < a.T && nq < a.N) *(uint32_t*)((uint16_t*)a.out + tq * a.out_row + nq) = q;
-          } else {
-            if (t < a.T && n < a.N) ((uint16_t*)a.out)[t * a.out_row + n] = (uint16_t)p;
-            if (t + 1 < a.T && n < a.N) ((uint16_t*)a.out)[(t + 1) * a.out_row + n] = (uint16_t)(p >> 16);
-          }
-        }
-      }
-    }
-  }
-}
-
-// Many rows: a workgroup of 2 x 2 waves has BT rows and BN channels, in steps of 128 inputs
-// through two buffers of LDS, filled from memory directly.
 typedef const void __attribute__((address_space(1)))* GlobalPtr;
 typedef void __attribute__((address_space(3)))* LdsPtr;
+SJD_DEV void load_lds(const void* src, char* lds) {
+  __builtin_amdgcn_global_load_lds((GlobalPtr)src, (LdsPtr)lds, 16, 0, 0);
+}
+// Waits until this wave's reads of LDS are done and at most N of its loads are outstanding, then
+// for the other waves. (A plain barrier: a fence would wait for every load.)
+template <int N>
+SJD_DEV void wait_barrier() {
+  __builtin_amdgcn_s_waitcnt(0x0070 | (N & 15) | (N >> 4) << 14);  // vmcnt(N) lgkmcnt(0)
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
 
+// Rows q0 + i * STEP (i < U) of a wave's block of sums in LDS, scaled and stored: four
+// channels a lane
+template <bool F32, bool ADD, int U, int STEP, int OUT>
+SJD_DEV void put_rows(const MatArgs& a, const int* sums, const float* scales, int t0, int q0, int n, const float4& ws) {
+  using P = std::conditional_t<F32, float4, uint2>;
+  constexpr int ES = F32 ? 4 : 2;
+  i32x4 c[U];
+  P add[U];
+  float cs[U];
+#pragma unroll
+  for (int i = 0; i < U; ++i) {
+    const int q = q0 + i * STEP;
+    c[i] = *(const i32x4*)(sums + q * OUT);
+    cs[i] = scales[q];
+    if constexpr (ADD) add[i] = *(const P*)((const char*)a.add + (min(t0 + q, a.T - 1) * a.add_row + n) * ES);
+  }
+#pragma unroll
+  for (int i = 0; i < U; ++i) {
+    const int t = t0 + q0 + i * STEP;
+    float v[4] = {(float)c[i][0] * ws.x * cs[i], (float)c[i][1] * ws.y * cs[i], (float)c[i][2] * ws.z * cs[i],
+                  (float)c[i][3] * ws.w * cs[i]};
+    P* const out = (P*)((char*)a.out + (t * a.out_row + n) * ES);
+    if constexpr (F32) {
+      if constexpr (ADD) v[0] += add[i].x, v[1] += add[i].y, v[2] += add[i].z, v[3] += add[i].w;
+      if (t < a.T) *out = make_float4(v[0], v[1], v[2], v[3]);
+    } else {
+      if constexpr (ADD) {
+        v[0] += __uint_as_float(add[i].x << 16), v[1] += __uint_as_float(add[i].x & 0xFFFF0000u);
+        v[2] += __uint_as_float(add[i].y << 16), v[3] += __uint_as_float(add[i].y & 0xFFFF0000u);
+      }
+      if (t < a.T) *out = make_uint2(pk_bf16(v[0], v[1]), pk_bf16(v[2], v[3]));
+    }
+  }
+}
+
+// Many rows: a workgroup of VT x VN waves has BT rows and BN channels, a wave FT x FN blocks of
+// 32 x 32. Steps of 64 inputs pass through four buffers of LDS, filled from memory directly.
+// Half-way through a step its operands are all in registers: its buffer is filled again, with
+// the step four on.
 template <int BT, int BN, int VT, int VN>
-__global__ __launch_bounds__(64 * VT * VN, VT * VN / 4) void k_matmul_many(MatArgs a, int nt, int nn) {
-  constexpr int WT = BT / VT, WN = BN / VN, FT = WT / 32, FN = WN / 32;
-  __shared__ __align__(16) char lds0[(BT + BN) * 128];
-  __shared__ __align__(16) char lds1[(BT + BN) * 128];
+__global__ __launch_bounds__(64 * VT * VN, BT * BN / (VT * VN) > 64 * 128 ? 1 : 2) void k_matmul_many(MatArgs a, int nt,
+                                                                                                   int nn) {
+  constexpr int WT = BT / VT, WN = BN / VN, FT = WT / 32, FN = WN / 32, WAVES = VT * VN;
+  constexpr int kBuf = (BT + BN) * 64;
+  __shared__ __align__(256) float scales[BT];
+  // (an object each: the compiler then knows that a step's reads do not touch what is being filled)
+  __shared__ __align__(16) char lds0[kBuf], lds1[kBuf], lds2[kBuf], lds3[kBuf];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   // eight dies take workgroups in turn: each has a run of tiles, four tiles of rows by all
   // the channels at a time
@@ -261,67 +262,147 @@ __global__ __launch_bounds__(64 * VT * VN, VT * VN / 4) void k_matmul_many(MatAr
     tn = r / rows;
   }
   const int t0 = tt * BT, b0 = tn * (BN / 32);
-  // this wave's loads of a step: rows of codes 8 at a time, tiles of weights
-  constexpr int LT = BT / 8 / (VT * VN), LN = BN / 8 / (VT * VN);
+  const int wt = wave % VT * WT, wn = wave / VT * FN;
+  const int units = a.ks >> 1, u0 = units * (int)blockIdx.y / a.splits, u1 = units * ((int)blockIdx.y + 1) / a.splits;
+  // this wave's loads of a step: rows of codes 16 at a time (64 bytes of each; rows past T read
+  // the last one), tiles of weights
+  constexpr int LT = BT / 16 / WAVES, LN = BN / 16 / WAVES, L = LT + LN, L0 = L / 2;
   const int8_t* code[LT];
   const char* w[LN];
-  const int kl = 16 * ((lane & 7) ^ (lane >> 3));
+  const int kl = 16 * swizzle<4>(lane >> 2, lane & 3);
 #pragma unroll
-  for (int i = 0; i < LT; ++i) code[i] = a.code + min(t0 + 8 * (wave * LT + i) + (lane >> 3), a.T - 1) * a.code_row;
+  for (int i = 0; i < LT; ++i)
+    code[i] = a.code + min(t0 + 16 * (wave * LT + i) + (lane >> 2), a.T - 1) * a.code_row + (int64_t)u0 * 64 + kl;
 #pragma unroll
   for (int i = 0; i < LN; ++i) {
-    const int q = wave * LN + i;  // row block q / 4, tile q % 4 of the step
-    w[i] = a.w + ((int64_t)min(b0 + q / 4, a.nb - 1) * a.ks + (q & 3)) * 1024 + lane * 16;
+    const int q = wave * LN + i;  // row block q / 2, tile q % 2 of the step
+    w[i] = a.w + ((int64_t)min(b0 + q / 2, a.nb - 1) * a.ks + 2 * u0 + q % 2) * 1024;
   }
-  auto fill = [&](char* lds, int u) {
-    const int k = u * 128 + kl;
-#pragma unroll
-    for (int i = 0; i < LT; ++i)
-      __builtin_amdgcn_global_load_lds((GlobalPtr)(code[i] + (k < a.cols ? k : 0)), (LdsPtr)(lds + (wave * LT + i) * 1024), 16,
-                                       0, 0);
-#pragma unroll
-    for (int i = 0; i < LN; ++i)
-      __builtin_amdgcn_global_load_lds((GlobalPtr)(w[i] + (int64_t)u * 4096),
-                                       (LdsPtr)(lds + BT * 128 + (wave * LN + i) * 1024), 16, 0, 0);
-  };
-  const int wt = wave % VT * WT, wn = wave / VT * FN;
-  i32x16 c[FT][FN] = {};
-  auto compute = [&](const char* lds) {
-    i32x4 x[2][FT], y[2][FN];
-    auto frags = [&](int s, int p) {
-#pragma unroll
-      for (int i = 0; i < FT; ++i) {
-        const int row = wt + 32 * i + (lane & 31);
-        x[p][i] = *(const i32x4*)(lds + row * 128 + 16 * ((2 * s + (lane >> 5)) ^ (row & 7)));
-      }
-#pragma unroll
-      for (int j = 0; j < FN; ++j) y[p][j] = *(const i32x4*)(lds + BT * 128 + ((wn + j) * 4 + s) * 1024 + lane * 16);
-    };
-    frags(0, 0);
-#pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      if (s < 3) frags(s + 1, (s + 1) & 1);
-#pragma unroll
-      for (int i = 0; i < FT; ++i)
-#pragma unroll
-        for (int j = 0; j < FN; ++j) c[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(x[s & 1][i], y[s & 1][j], c[i][j], 0, 0, 0);
+  // load p of step u (its pointer then is at the next step's). FULL: no code lies behind its row;
+  // else such a piece reads the row's first, against weights of zero
+  auto fill = [&](auto full, char* lds, int u, int p) __attribute__((always_inline)) {
+    if (p < LT) {
+      const int k = u * 64 + kl;
+      load_lds(decltype(full)::value || k < a.cols ? code[p] : code[p] - k, lds + (wave * LT + p) * 1024);
+      code[p] += 64;
+    } else {
+      load_lds(w[p - LT] + (uint32_t)(lane * 16), lds + BT * 64 + (wave * LN + p - LT) * 1024);
+      w[p - LT] += 2048;
     }
   };
-  const int units = a.ks >> 2;
-  auto step = [&](char* now, char* next, int u) {
-    __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): this wave's part of the step is in LDS
-    __syncthreads();                     // .. and the others'; nobody reads the other buffer
-    if (u + 1 < units) fill(next, u + 1);
-    compute(now);
+  i32x16 c[FT][FN] = {};
+  i32x4 x[2][FT], y[2][FN];
+  auto frags = [&](const char* lds, int s) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < FT; ++i) {
+      const int row = wt + 32 * i + (lane & 31);
+      x[s][i] = *(const i32x4*)(lds + row * 64 + 16 * swizzle<4>(row, 2 * s + (lane >> 5)));
+    }
+#pragma unroll
+    for (int j = 0; j < FN; ++j) y[s][j] = *(const i32x4*)(lds + BT * 64 + ((wn + j) * 2 + s) * 1024 + lane * 16);
   };
-  fill(lds0, 0);
-  for (int u = 0; u < units; u += 2) {
-    step(lds0, lds1, u);
-    if (u + 1 < units) step(lds1, lds0, u + 1);
+  // Products of half a step, `more`: with loads P0 .. P1 - 1 of step u between them. They go out one
+  // at a time, over a whole step: the waves' loads of half of it would wait for each other.
+  auto multiply = [&](auto full, int s, bool more, char* lds, int u, auto p0, auto p1) __attribute__((always_inline)) {
+    constexpr int P0 = decltype(p0)::value, N = decltype(p1)::value - P0;
+#pragma unroll
+    for (int i = 0; i < FT; ++i) {
+      if (more) {
+#pragma unroll
+        for (int p = 0; p < N; ++p)
+          if (p * FT / N == i) fill(full, lds, u, P0 + p);
+      }
+#pragma unroll
+      for (int j = 0; j < FN; ++j) c[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(y[s][j], x[s][i], c[i][j], 0, 0, 0);
+    }
+  };
+  // FULL: there are eight steps behind it
+  auto step = [&](auto full, char* now, const char* next, char* last, int u) __attribute__((always_inline)) {
+    constexpr bool FULL = decltype(full)::value;
+    if (!FULL && u >= u1) return;
+    frags(now, 1);
+    multiply(full, 0, FULL || u + 3 < u1, last, u + 3, Int<L0>{}, Int<L>{});
+    // the next step is there, and no wave reads this one's buffer any more
+    if (FULL || u + 3 < u1) wait_barrier<2 * L>();
+    else if (u + 2 < u1) wait_barrier<L>();
+    else wait_barrier<0>();
+    if (FULL || u + 1 < u1) frags(next, 0);
+    multiply(full, 1, FULL || u + 4 < u1, now, u + 4, Int<0>{}, Int<L0>{});
+  };
+  const float cs = threadIdx.x < BT ? a.cscale[min(t0 + (int)threadIdx.x, a.T - 1)] : 0.0f;
+  const std::false_type checked;
+#pragma unroll
+  for (int p = 0; p < 3 * L + L0; ++p) {
+    const int i = p / L;
+    if (i == 0 || u0 + i < u1) fill(checked, i == 0 ? lds0 : i == 1 ? lds1 : i == 2 ? lds2 : lds3, u0 + i, p % L);
   }
-  auto finish = [&](auto f32, auto add) { finish_many<decltype(f32)::value, decltype(add)::value, FT, FN>(a, c, t0 + wt, (b0 + wn) * 32); };
-  if (a.f32) a.add ? finish(std::true_type{}, std::true_type{}) : finish(std::true_type{}, std::false_type{});
-  else a.add ? finish(std::false_type{}, std::true_type{}) : finish(std::false_type{}, std::false_type{});
+  if (u0 + 3 < u1) wait_barrier<2 * L + L0>();
+  else wait_barrier<0>();
+  frags(lds0, 0);
+  int u = u0;
+  auto four = [&](auto full) __attribute__((always_inline)) {
+    step(full, lds0, lds1, lds3, u);
+    step(full, lds1, lds2, lds0, u + 1);
+    step(full, lds2, lds3, lds1, u + 2);
+    step(full, lds3, lds0, lds2, u + 3);
+  };
+  for (; u + 12 <= u1; u += 4) four(std::true_type{});
+  for (; u < u1; u += 4) four(checked);
+
+  // Blocks of 32 rows pass through a part of LDS of the wave's own, to leave in whole rows
+  // (register r of a block: channel 8 (r / 4) + 4 (lane / 32) + r % 4, row lane % 32)
+  constexpr int OUT = WN + 4, kParts = kBuf / (32 * OUT * 4), LPR = WN / 4, RPI = 64 / LPR, U = 32 / RPI < 8 ? 32 / RPI : 8;
+  static_assert(kParts * 4 >= WAVES && BT <= 64 * WAVES, "a part for each wave, a scale for each thread");
+  if (threadIdx.x < BT) scales[threadIdx.x] = cs;
+  __syncthreads();
+  const int part = wave / kParts;
+  int* const mine = (int*)(part == 0 ? lds0 : part == 1 ? lds1 : part == 2 ? lds2 : lds3) + wave % kParts * (32 * OUT);
+  const int col = lane % LPR * 4, n = (b0 + wn) * 32 + col, q0 = lane / LPR;
+  const float4 ws = channel_scales(a, n);
+  const int64_t row = a.nb * 32LL;
+  int32_t* const sums = a.sums + (int64_t)blockIdx.y * a.T * row + n;
+#pragma unroll
+  for (int i = 0; i < FT; ++i) {
+#pragma unroll
+    for (int j = 0; j < FN; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; r += 4)
+        *(i32x4*)(mine + (lane & 31) * OUT + 32 * j + 2 * r + 4 * (lane >> 5)) =
+            i32x4{c[i][j][r], c[i][j][r + 1], c[i][j][r + 2], c[i][j][r + 3]};
+    const int tb = t0 + wt + 32 * i;
+    const float* const sc = scales + wt + 32 * i;
+    if (a.splits > 1) {
+#pragma unroll
+      for (int q = 0; q < 32; q += RPI) {
+        const i32x4 v = *(const i32x4*)(mine + (q0 + q) * OUT + col);
+        if (tb + q0 + q < a.T && n < row) *(i32x4*)(sums + (tb + q0 + q) * row) = v;
+      }
+    } else if (a.wide && n + 4 <= a.N) {
+      for (int q = q0; q < 32; q += U * RPI) {
+        if (a.f32) {
+          if (a.add) put_rows<true, true, U, RPI, OUT>(a, mine + col, sc, tb, q, n, ws);
+          else put_rows<true, false, U, RPI, OUT>(a, mine + col, sc, tb, q, n, ws);
+        } else {
+          if (a.add) put_rows<false, true, U, RPI, OUT>(a, mine + col, sc, tb, q, n, ws);
+          else put_rows<false, false, U, RPI, OUT>(a, mine + col, sc, tb, q, n, ws);
+        }
+      }
+    } else if (n < a.N) {
+      for (int q = q0; q < 32; q += RPI)
+        if (tb + q < a.T) put(a, tb + q, n, *(const i32x4*)(mine + q * OUT + col), ws, sc[q]);
+    }
+  }
+}
+
+// Sums of the parts of split inputs, scaled: a thread has four channels of a row
+__global__ __launch_bounds__(256) void k_matmul_join(MatArgs a) {
+  const int n0 = (blockIdx.x * 256 + threadIdx.x) * 4, t = blockIdx.y;
+  if (n0 >= a.N) return;
+  const int64_t row = a.nb * 32LL;
+  const int32_t* p = a.sums + t * row + n0;
+  i32x4 c = *(const i32x4*)p;
+  for (int s = 1; s < a.splits; ++s) c += *(const i32x4*)(p + s * (a.T * row));
+  put(a, t, n0, c, channel_scales(a, n0), a.cscale[t]);
 }
 
 struct PackArgs {
@@ -374,14 +455,31 @@ __global__ __launch_bounds__(256) void k_pack_i8(PackArgs a) {
 
 }  // namespace
 
-int64_t matmul_i8_ws(const sjd_i8_weights& w, int T) { return 0; }
+// Which kernel, tile and split of the inputs a product takes
+struct MatPlan {
+  int bt, bn;  // rows and channels of a workgroup; bt 0: few rows
+  int splits;
+};
+static MatPlan matmul_plan(const sjd_i8_weights& w, int T) {
+  if (T <= 64) return {0, 0, 1};
+  MatPlan p = T > 1024 ? MatPlan{256, 256, 1} : MatPlan{128, 128, 1};
+  return p;
+}
+
+int64_t matmul_i8_ws(const sjd_i8_weights& w, int T) {
+  const MatPlan p = matmul_plan(w, T);
+  return p.splits > 1 ? (int64_t)p.splits * T * i8_shape(w.N, w.K).nb * 128 : 0;
+}
 
 hipError_t launch_matmul_i8(const sjd_i8_weights& w, const sjd_matmul_io& io, void* ws, hipStream_t s) {
   const I8Shape sh = i8_shape(w.N, w.K);
+  const MatPlan p = matmul_plan(w, io.T);
+  const uintptr_t es = io.dtype == SJD_F32 ? 4 : 2;
+  auto fine = [&](const void* q, int64_t row) { return ((uintptr_t)q & (4 * es - 1)) == 0 && row % 4 == 0; };
   const MatArgs a{(const char*)w.d_w, w.d_scale, io.d_code, io.d_code_scale, io.d_out, io.d_add, io.code_row, io.out_row,
                   io.add_row, io.T, w.N, (w.K + 15) & ~15, sh.nb, sh.ks, io.dtype == SJD_F32,
-                  ((uintptr_t)io.d_out & 3) == 0 && io.out_row % 2 == 0 && w.N % 2 == 0};
-  if (io.T <= 128) {
+                  fine(io.d_out, io.out_row) && (!io.d_add || fine(io.d_add, io.add_row)), p.splits, (int32_t*)ws};
+  if (!p.bt) {
     auto few = [&](auto ch, auto tt, auto depth, auto stage) {
       constexpr int CH = decltype(ch)::value, TT = decltype(tt)::value;
       hipLaunchKernelGGL((k_matmul_few<CH, TT, decltype(depth)::value, decltype(stage)::value>),
@@ -393,22 +491,25 @@ hipError_t launch_matmul_i8(const sjd_i8_weights& w, const sjd_matmul_io& io, vo
     if (narrow && io.T <= 8) few(Int<16>{}, Int<1>{}, Int<8>{}, direct);
     else if (narrow && io.T <= 16) few(Int<16>{}, Int<1>{}, Int<8>{}, stage);
     else if (narrow && io.T <= 32) few(Int<16>{}, Int<2>{}, Int<6>{}, stage);
-    else if (narrow && io.T <= 64) few(Int<16>{}, Int<4>{}, Int<4>{}, stage);
+    else if (narrow) few(Int<16>{}, Int<4>{}, Int<4>{}, stage);
     else if (io.T <= 8) few(Int<32>{}, Int<1>{}, Int<4>{}, direct);
     else if (io.T <= 32) few(Int<32>{}, Int<1>{}, Int<4>{}, stage);
-    else if (io.T <= 64) few(Int<32>{}, Int<2>{}, Int<3>{}, stage);
-    else few(Int<32>{}, Int<4>{}, Int<2>{}, stage);
+    else few(Int<32>{}, Int<2>{}, Int<3>{}, stage);
     return hipGetLastError();
   }
   auto many = [&](auto bt, auto bn, auto vt, auto vn) {
     constexpr int BT = decltype(bt)::value, BN = decltype(bn)::value, VT = decltype(vt)::value, VN = decltype(vn)::value;
+    if (p.bt != BT || p.bn != BN) return;
     const int nt = (io.T + BT - 1) / BT, nn = (w.N + BN - 1) / BN;
-    hipLaunchKernelGGL((k_matmul_many<BT, BN, VT, VN>), dim3(nt * nn), dim3(64 * VT * VN), 0, s, a, nt, nn);
+    hipLaunchKernelGGL((k_matmul_many<BT, BN, VT, VN>), dim3(nt * nn, p.splits), dim3(64 * VT * VN), 0, s, a, nt, nn);
   };
-  if (io.T > 1024) many(Int<256>{}, Int<256>{}, Int<2>{}, Int<4>{});
-  else many(Int<128>{}, Int<128>{}, Int<2>{}, Int<2>{});
-  return hipGetLastError();
-  hipLaunchKernelGGL(k_matmul_i8, dim3((io.T + 31) / 32, (sh.nb + 3) / 4), dim3(256), 0, s, a);
+  many(Int<256>{}, Int<256>{}, Int<2>{}, Int<2>{});
+  many(Int<128>{}, Int<256>{}, Int<2>{}, Int<4>{});
+  many(Int<128>{}, Int<128>{}, Int<2>{}, Int<2>{});
+  many(Int<128>{}, Int<64>{}, Int<2>{}, Int<2>{});
+  many(Int<64>{}, Int<128>{}, Int<2>{}, Int<2>{});
+  many(Int<64>{}, Int<64>{}, Int<2>{}, Int<2>{});
+  if (p.splits > 1) hipLaunchKernelGGL(k_matmul_join, dim3((w.N + 1023) / 1024, io.T), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
