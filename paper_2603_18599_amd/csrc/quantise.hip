@@ -1,6 +1,7 @@
 // Rows as 8-bit integers with a scale each (definition: sjd.h), the input of the
 // products in matmul_i8.hip, with what stands in front of a projection: an RMSNorm or
 // the gate of a gated layer.
+#include <algorithm>
 #include <type_traits>
 
 #include "device.h"
@@ -52,8 +53,8 @@ template <class E, int NT, int P, bool NORM, bool GATE>
 __global__ __launch_bounds__(NT < 256 ? 256 : NT) void k_quantise(QuantArgs a) {
   __shared__ float red[NT / kWave];
   __shared__ uint32_t redu[NT / kWave];
-  const int64_t t = NT == kWave ? blockIdx.x * 4LL + (threadIdx.x >> 6) : blockIdx.x;
-  if (NT == kWave && t >= a.T) return;
+  const int64_t g = (int64_t)blockIdx.y * gridDim.x + blockIdx.x, t = NT == kWave ? g * 4 + (threadIdx.x >> 6) : g;
+  if (t >= a.T) return;
   const int tid = threadIdx.x % NT, cols = (a.K + 15) & ~15;
   const E* x = (const E*)a.x + t * a.x_row;
   float y[P][8];
@@ -122,7 +123,9 @@ hipError_t launch_quantise_rows(const sjd_quantise_params& p, const sjd_quantise
   auto go = [&](auto e, auto nt, auto pieces) {
     using E = decltype(e);
     constexpr int NT = decltype(nt)::value, P = decltype(pieces)::value;
-    const dim3 grid(NT == kWave ? (p.T + 3) / 4 : p.T), block(NT < 256 ? 256 : NT);
+    // (two dimensions: one has less than 2^32 threads)
+    const int wgs = NT == kWave ? (p.T + 3) / 4 : p.T, gx = std::min(wgs, 1 << 20);
+    const dim3 grid(gx, (wgs + gx - 1) / gx), block(NT < 256 ? 256 : NT);
     if (io.d_norm) hipLaunchKernelGGL((k_quantise<E, NT, P, true, false>), grid, block, 0, s, a);
     else if (io.d_gate) hipLaunchKernelGGL((k_quantise<E, NT, P, false, true>), grid, block, 0, s, a);
     else hipLaunchKernelGGL((k_quantise<E, NT, P, false, false>), grid, block, 0, s, a);
