@@ -101,13 +101,13 @@ SJD_DEV int piece_pos(int u) {
 }
 
 // Writes the rows of one tile (32 positions from `in` of a page, head h) that a workgroup of
-// 256 holds: thread 8 i + c has dims c * N .. of position i, `ok` where that is one of the
+// 256 (or each 256 threads of one) holds: thread 8 i + c has dims c * N .. of position i, `ok` where that is one of the
 // positions [lo, hi) that the window holds. vs: the values' tile in LDS.
 template <int HD, bool FP8>
 SJD_DEV void store_tile(const PoolView& pv, char* page, int h, int in, int lo, int hi, bool ok, const float (&kf)[HD / 8],
                         const float (&vf)[HD / 8], char* vs) {
   constexpr int ES = FP8 ? 1 : 2, N = HD / 8;
-  const int i = threadIdx.x >> 3, c = threadIdx.x & 7;
+  const int tid = threadIdx.x & 255, i = tid >> 3, c = tid & 7;
   // (of the row's first 8 dims; a second chunk, 128-dim heads: 8 bytes on in e4m3, 1024 in bf16)
   char* kt = page + tile_off<HD, ES>(pv, h, in, 0) + key_byte<HD, FP8>(i, c * N);
   char* vt = page + tile_off<HD, ES>(pv, h, in, 1);
@@ -136,7 +136,7 @@ SJD_DEV void store_tile(const PoolView& pv, char* page, int h, int in, int lo, i
     for (int e = 0; e < N; ++e) *(uint16_t*)(vs + pad(val_byte<false>(i, c * N + e))) = f32_to_bf16(vf[e]);
   }
   __syncthreads();
-  for (int u = threadIdx.x; u < 2 * HD * ES; u += 256) {
+  for (int u = tid; u < 2 * HD * ES; u += 256) {
     const uint4 x = *(const uint4*)(vs + pad(16 * u));
     const int p = piece_pos<FP8>(u);
     char* d = vt + 16 * u;
