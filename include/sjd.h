@@ -106,6 +106,15 @@ typedef enum {
  * their precision are the default's unless SJD_KV_E4M3 is set too. Needs row_len >= 1,
  * and not SJD_TUNE (SJD_EINVAL otherwise). */
 #define SJD_ROPE_GRID 256u
+/* decoder contexts only, with SJD_KV_E4M3 (SJD_EINVAL without it): the layers'
+ * projections in 8-bit integers, their weights with a scale per output channel
+ * (half the default's memory), their input rows with a scale each
+ * (sjd_quantise_rows, sjd_matmul_i8), q, k and v placed and appended in one call
+ * (sjd_kv_append_rope). The residual rows stay fp32, and the LM head is the
+ * default's. The GEMM plan (sjd_get_plan) plays no part in the layers. SJD_ENOTSUP
+ * for d_model, n_heads * head_dim or ffn_dim above 65536, or more than 2^20 outputs
+ * of a projection. */
+#define SJD_W8A8 1024u
 /* sjd_verify_given only: the row behind a window's last draft holds the
  * target's probabilities too, and a window whose drafts are all accepted
  * commits one more token, drawn from it */
@@ -509,7 +518,7 @@ typedef struct {
   int32_t L, K, D;       /* window slots (1..64), candidates per depth (1..8), depth   */
   uint32_t flags;        /* SJD_AC | SJD_PD (0 = vanilla SJD; Sec. 5.3's ablation),
                             optionally | SJD_EAGER | SJD_NO_TUNE | SJD_TUNE |
-                            SJD_CHECK_FINITE | SJD_KV_E4M3 | SJD_ROPE_GRID                */
+                            SJD_CHECK_FINITE | SJD_KV_E4M3 | SJD_ROPE_GRID | SJD_W8A8     */
   float rms_eps, rope_theta;
   int32_t eol_id, row_len;
   int32_t weights_f32;   /* 1: weights are fp32, 0: bf16                                */

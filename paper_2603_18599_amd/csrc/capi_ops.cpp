@@ -5,7 +5,6 @@
 #include <cmath>
 
 #include "ops.h"
-#include "rows_i8.h"
 #include "sjd.h"
 
 namespace {
@@ -134,7 +133,7 @@ int check_quantise(const sjd_quantise_params* p, const sjd_quantise_io* io) {
   return !io->d_norm || aligned(io->d_norm, p->norm_dtype == SJD_F32 ? 4 : 2) ? SJD_OK : SJD_EINVAL;
 }
 
-bool i8_sizes(int32_t N, int32_t K) { return N >= 1 && N <= (1 << 20) && K >= 1 && K <= sjd::kMaxK; }
+bool i8_sizes(int32_t N, int32_t K) { return N >= 1 && N <= sjd::kMaxN && K >= 1 && K <= sjd::kMaxK; }
 
 int check_i8_weights(const sjd_i8_weights* w) {
   if (!w || !i8_sizes(w->N, w->K) || !w->d_w || !aligned(w->d_w, 256) || !w->d_scale || !aligned(w->d_scale, 4))
@@ -212,9 +211,7 @@ extern "C" int sjd_quantise_rows(const sjd_quantise_params* p, const sjd_quantis
 }
 
 extern "C" int64_t sjd_i8_weight_bytes(int32_t N, int32_t K) {
-  if (!i8_sizes(N, K)) return 0;
-  const sjd::I8Shape s = sjd::i8_shape(N, K);
-  return (int64_t)s.nb * s.ks * 1024;
+  return !i8_sizes(N, K) ? 0 : sjd::i8_weight_bytes(N, K);
 }
 
 extern "C" int sjd_pack_i8(const sjd_i8_weights* w, const void* src, int32_t dtype, int64_t row, void* stream) {

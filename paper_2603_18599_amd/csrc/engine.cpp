@@ -5,6 +5,7 @@
 // blocking).
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <array>
 #include <cmath>
 #include <cstdio>
@@ -76,6 +77,15 @@ struct Ctx {
   int32_t *pseq = nullptr, *ppos = nullptr;  // [kMaxStreams][4], [Mpad][axes]
   uint16_t *qkv_rows = nullptr, *att_rows = nullptr;  // [Mpad][q, k, v], [Mpad][q]
   void* attn_ws = nullptr;
+  // projections in 8-bit integers (SJD_W8A8), around the pages
+  struct I8Layer {
+    sjd_i8_weights qkv, o, gu, down;
+  };
+  bool w8 = false;
+  std::vector<I8Layer> l8;
+  int8_t* code = nullptr;  // a projection's input rows
+  float* code_scale = nullptr;
+  void* mm_ws = nullptr;
   sjd_rope_params rp{};
   double rope_freq[64];
   uint8_t rope_axis[64];
@@ -162,10 +172,18 @@ int check_config(const sjd_config* c) {
   if (c->L < 1 || c->L > 64 || c->K < 1 || c->K > 8 || c->D < 0 || (long)c->K * c->D > c->L) return SJD_EINVAL;
   if (c->V > 65536) return SJD_ENOTSUP;
   if (c->max_seq < c->L + 2) return SJD_EINVAL;
-  if (c->flags & ~(SJD_AC | SJD_PD | SJD_EAGER | SJD_NO_TUNE | SJD_TUNE | SJD_CHECK_FINITE | SJD_KV_E4M3 | SJD_ROPE_GRID))
+  if (c->flags & ~(SJD_AC | SJD_PD | SJD_EAGER | SJD_NO_TUNE | SJD_TUNE | SJD_CHECK_FINITE | SJD_KV_E4M3 | SJD_ROPE_GRID |
+                   SJD_W8A8))
     return SJD_EINVAL;
+  if ((c->flags & SJD_W8A8) && !(c->flags & SJD_KV_E4M3)) return SJD_EINVAL;
   if ((c->flags & (SJD_KV_E4M3 | SJD_ROPE_GRID)) && (c->flags & SJD_TUNE)) return SJD_EINVAL;
   if ((c->flags & SJD_ROPE_GRID) && c->row_len < 1) return SJD_EINVAL;
+  if (c->flags & SJD_W8A8) {  // sizes of the 8-bit products
+    const int64_t Nq = (int64_t)c->n_heads * c->head_dim, N = Nq + 2LL * c->n_kv_heads * c->head_dim;
+    if (c->d_model > sjd::kMaxK || Nq > sjd::kMaxK || c->ffn_dim > sjd::kMaxK || N > sjd::kMaxN || 2LL * c->ffn_dim > sjd::kMaxN)
+      return SJD_ENOTSUP;
+    if (!std::isnormal(c->rms_eps)) return SJD_EINVAL;
+  }
   if (!(c->rms_eps > 0.0f) || !(c->rope_theta > 0.0f)) return SJD_EINVAL;
   if (!std::isfinite(c->cfg_w)) return SJD_EINVAL;
   if (c->batch < 0) return SJD_EINVAL;
@@ -262,6 +280,45 @@ int paged_layer(Ctx& x, int l, int S, size_t plane, int M, int mt, bool prompt, 
   return SJD_OK;
 }
 
+// A layer with projections in 8-bit integers: residual rows in fp32 in, and out in place. Each
+// projection's input is quantised from what it is computed in (the norms and the gate inside
+// the quantiser); q, k and v stay fp32 until they are placed, so that q is rounded once (to bf16,
+// the attention's) and k and v once (to the pages' type).
+int i8_layer(Ctx& x, int l, int M, bool prompt, int cache, hipStream_t s) {
+  const sjd_config& c = x.c;
+  const int d = c.d_model, hd = c.head_dim, Nq = c.n_heads * hd, Nkv = c.n_kv_heads * hd, N = Nq + 2 * Nkv, F = c.ffn_dim;
+  const Ctx::I8Layer& w = x.l8[l];
+  auto quantise = [&](const void* rows, int dtype, int K, int64_t row, const void* norm, const void* gate) {
+    const sjd_quantise_params p{M, K, dtype, SJD_BF16, c.rms_eps, row, row, K};
+    const sjd_quantise_io io{rows, norm, gate, x.code, x.code_scale};
+    return sjd::launch_quantise_rows(p, io, s);
+  };
+  auto product = [&](const sjd_i8_weights& m, int dtype, void* out, const void* add) {
+    const sjd_matmul_io io{M, dtype, x.code, x.code_scale, out, add, m.K, m.N, m.N};
+    return sjd::launch_matmul_i8(m, io, x.mm_ws, s);
+  };
+  HIPTRY(quantise(x.x, SJD_F32, d, d, x.lw[l][0], nullptr));
+  HIPTRY(product(w.qkv, SJD_F32, x.qkv, nullptr));
+  sjd_pages p = x.pages;
+  p.d_pool = (char*)x.pages.d_pool + l * x.pool_bytes;
+  const sjd_windows win = page_windows(x, M, prompt, cache);
+  const sjd_kv_rows kv{x.qkv + Nq, x.qkv + Nq + Nkv, N, N, SJD_F32};
+  const sjd_append_rope rope{c.n_heads, x.rp.pairs, x.rp.axes, SJD_BF16, x.rp.h_freq, x.rp.h_axis, x.ppos, x.qkv,
+                             x.qkv_rows, N, Nq};
+  HIPTRY(sjd::launch_kv_append_rope(p, win, kv, rope, s));
+  const sjd_attention_io io{c.n_heads, (float)(1.0 / std::sqrt((double)hd)), x.qkv_rows, x.att_rows, Nq, Nq,
+                            prompt ? nullptr : x.win->anc};
+  HIPTRY(sjd::launch_paged_attention(p, win, io, x.attn_ws, s));
+  HIPTRY(quantise(x.att_rows, SJD_BF16, Nq, Nq, nullptr, nullptr));
+  HIPTRY(product(w.o, SJD_F32, x.x, x.x));
+  uint16_t* const gu = (uint16_t*)x.gup;
+  HIPTRY(quantise(x.x, SJD_F32, d, d, x.lw[l][5], nullptr));
+  HIPTRY(product(w.gu, SJD_BF16, gu, nullptr));
+  HIPTRY(quantise(gu + F, SJD_BF16, F, 2 * F, nullptr, gu));
+  HIPTRY(product(w.down, SJD_F32, x.x, x.x));
+  return SJD_OK;
+}
+
 enum { kProjQkv = 0, kProjO = 1, kProjGu = 2, kProjDown = 3 };
 
 // Window forward of M rows: two streams (sm.mode != kStreamsOne, see
@@ -297,6 +354,10 @@ int forward(Ctx& x, int M, const int32_t* prompt, const int32_t* n_dev, int n_ho
   normed.inv_d = 1.0f / (float)d;
   normed.eps = c.rms_eps;
   for (int l = 0; l < c.n_layers; ++l) {
+    if (x.w8) {
+      TRY(i8_layer(x, l, M, prompt != nullptr, cache, s));
+      continue;
+    }
     const auto& w = x.lw[l];
     const size_t lofs = (size_t)l * Hkv * x.cap_pad * hd + (size_t)cache * x.kv_elems;
     sjd::KvPlanes kv{x.q, x.q_lo, x.kc + lofs, x.kc_lo + lofs, x.vt + lofs, x.vt_lo + lofs, x.kv_elems};
@@ -566,6 +627,56 @@ int cache_check(Ctx& x) {
   return SJD_OK;
 }
 
+// A layer's matrices in 8-bit integers, those with the same input as one.
+int pack_layer(Ctx& x, const void* const* lp, hipStream_t s) {
+  const sjd_config& c = x.c;
+  const int d = c.d_model, Nq = c.n_heads * c.head_dim, Nkv = c.n_kv_heads * c.head_dim, F = c.ffn_dim;
+  const int dtype = c.weights_f32 ? SJD_F32 : SJD_BF16;
+  auto make = [&](int N, int K, sjd_i8_weights* w) {
+    char* data = nullptr;
+    *w = sjd_i8_weights{N, K, nullptr, nullptr};
+    TRY(dalloc(x, &data, (size_t)sjd::i8_weight_bytes(N, K)));
+    w->d_w = data;
+    return dalloc(x, &w->d_scale, (size_t)N);
+  };
+  // channels [row0, row0 + N) of w (whole blocks of 32)
+  auto pack = [&](const sjd_i8_weights& w, const void* src, int row0, int N) {
+    const sjd_i8_weights part{N, w.K, (char*)w.d_w + sjd::i8_weight_bytes(row0, w.K), w.d_scale + row0};
+    return sjd::launch_pack_i8(part, src, dtype, w.K, s) == hipSuccess ? SJD_OK : SJD_EHIP;
+  };
+  Ctx::I8Layer w{};
+  TRY(make(Nq + 2 * Nkv, d, &w.qkv));
+  TRY(make(d, Nq, &w.o));
+  TRY(make(2 * F, d, &w.gu));
+  TRY(make(d, F, &w.down));
+  TRY(pack(w.qkv, lp[1], 0, Nq));
+  TRY(pack(w.qkv, lp[2], Nq, Nkv));
+  TRY(pack(w.qkv, lp[3], Nq + Nkv, Nkv));
+  TRY(pack(w.o, lp[4], 0, d));
+  TRY(pack(w.gu, lp[6], 0, F));
+  TRY(pack(w.gu, lp[7], F, F));
+  TRY(pack(w.down, lp[8], 0, d));
+  x.l8.push_back(w);
+  return SJD_OK;
+}
+
+// What the 8-bit projections work in: a window's codes, and scratch of the largest product of
+// a window of any length.
+int i8_buffers(Ctx& x) {
+  const sjd_config& c = x.c;
+  const int Nq = c.n_heads * c.head_dim, K = std::max(c.d_model, std::max(Nq, c.ffn_dim));
+  int64_t ws = 0;
+  for (int M = 1; M <= x.Mpad; ++M)
+    for (const sjd_i8_weights& w : {x.l8[0].qkv, x.l8[0].o, x.l8[0].gu, x.l8[0].down})
+      ws = std::max(ws, sjd::matmul_i8_ws(w, M));
+  char* p = nullptr;
+  TRY(dalloc(x, &x.code, (size_t)x.Mpad * K));
+  TRY(dalloc(x, &x.code_scale, (size_t)x.Mpad));
+  TRY(dalloc(x, &p, (size_t)ws));
+  x.mm_ws = p;
+  return SJD_OK;
+}
+
 // Pools, tables and row buffers of a context with e4m3 pages.
 int page_buffers(Ctx& x, hipStream_t s) {
   const sjd_config& c = x.c;
@@ -646,6 +757,7 @@ extern "C" int sjd_init(const sjd_config* cfg, const sjd_weights* w, void* strea
   const int f32 = c.weights_f32 ? 1 : 0;
   x.paged = (c.flags & SJD_KV_E4M3) != 0;
   x.grid = (c.flags & SJD_ROPE_GRID) != 0;
+  x.w8 = (c.flags & SJD_W8A8) != 0;
   x.fused = fused_shape(c) && !(c.flags & SJD_TUNE) && !x.paged && !x.grid;
   auto copy_rows = [&](const void* p, size_t count, const uint16_t** dst) -> int {
     uint16_t* b = nullptr;
@@ -681,6 +793,10 @@ extern "C" int sjd_init(const sjd_config* cfg, const sjd_weights* w, void* strea
     auto& o = x.lw[l];
     rc = copy_rows(lp[0], d, &o[0]);
     if (rc == SJD_OK) rc = copy_rows(lp[5], d, &o[5]);
+    if (x.w8) {
+      if (rc == SJD_OK) rc = pack_layer(x, lp, s);
+      continue;
+    }
     uint16_t *qkv = nullptr, *wo = nullptr, *wgu = nullptr, *wd = nullptr;
     const size_t tq = (size_t)Nq * d, tkv = (size_t)Nkv * d;
     if (rc == SJD_OK) rc = dalloc(x, &qkv, tq + 2 * tkv);
@@ -727,6 +843,7 @@ extern "C" int sjd_init(const sjd_config* cfg, const sjd_weights* w, void* strea
     if (hipMemsetAsync(x.ppos, 0, 12 * (size_t)Mp, s) != hipSuccess) return fail(SJD_EHIP);
   }
   if (x.paged && (rc = page_buffers(x, s))) return fail(rc);
+  if (x.w8 && (rc = i8_buffers(x))) return fail(rc);
   x.att = x.xn + xnsz;
   x.hbuf = x.att + attsz;
   x.zeros = x.hbuf + hsz;
@@ -818,6 +935,7 @@ extern "C" int sjd_init(const sjd_config* cfg, const sjd_weights* w, void* strea
       for (const Ctx::Plan& q : p.cand) smax[p.kind] = q.S > smax[p.kind] ? q.S : smax[p.kind];
     }
   }
+  if (x.w8) smax[0] = smax[1] = smax[2] = smax[3] = 1;  // (the plan is that of the bf16 projections)
   const int sr = smax[1] > smax[3] ? smax[1] : smax[3];
   const size_t nfours = (size_t)Mp * sjd::norm_chunks(d) * 64;
   if (x.fused) {

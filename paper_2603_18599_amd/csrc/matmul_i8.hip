@@ -489,6 +489,11 @@ static MatPlan matmul_plan(const sjd_i8_weights& w, int T) {
   return best;
 }
 
+int64_t i8_weight_bytes(int N, int K) {
+  const I8Shape s = i8_shape(N, K);
+  return (int64_t)s.nb * s.ks * 1024;
+}
+
 int64_t matmul_i8_ws(const sjd_i8_weights& w, int T) {
   const MatPlan p = matmul_plan(w, T);
   return p.splits > 1 ? (int64_t)p.splits * T * i8_shape(w.N, w.K).nb * 128 : 0;

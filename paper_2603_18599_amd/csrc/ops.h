@@ -133,6 +133,9 @@ hipError_t launch_page_commit(const DevState* st, const Window* win, const sjd_p
 hipError_t launch_rope_axes(const sjd_rope_params& p, const sjd_rope_io& io, hipStream_t s);
 
 // ---- projections in 8-bit integers
+constexpr int kMaxK = 65536;    // inputs: 128 * 128 * kMaxK fits an int32
+constexpr int kMaxN = 1 << 20;  // channels
+int64_t i8_weight_bytes(int N, int K);
 hipError_t launch_quantise_rows(const sjd_quantise_params& p, const sjd_quantise_io& io, hipStream_t s);
 hipError_t launch_pack_i8(const sjd_i8_weights& w, const void* src, int dtype, int64_t row, hipStream_t s);
 int64_t matmul_i8_ws(const sjd_i8_weights& w, int T);

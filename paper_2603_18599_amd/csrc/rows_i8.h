@@ -5,7 +5,6 @@
 
 namespace sjd {
 
-constexpr int kMaxK = 65536;      // 128 * 128 * kMaxK fits an int32
 constexpr float kLeastRow = 0x1p-100f;  // rows below it count as zeros (127 / max stays finite)
 
 SJD_DEV float elem_f32(uint16_t v) { return bf16_to_f32(v); }

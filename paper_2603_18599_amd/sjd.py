@@ -22,6 +22,7 @@ SJD_FULL_SELECT = 64
 SJD_KV_E4M3 = 128
 SJD_ROPE_GRID = 256
 SJD_BONUS = 512
+SJD_W8A8 = 1024
 SJD_VERIFY_NOALLOC_MAX_ROWS = 131072
 
 _STATUS = {0: "SJD_OK", -1: "SJD_EINVAL", -2: "SJD_ENOMEM", -3: "SJD_EHIP", -4: "SJD_ESTATE", -5: "SJD_ENOTSUP",
