@@ -116,7 +116,7 @@ constexpr int kFewWaves = 8;
 // STAGE: codes are loaded eight lanes to a row's 128 bytes and pass through the wave's own
 // part of LDS; else each lane loads its operand, which touches a line per row.
 template <int CH, int TT, int DEPTH, bool STAGE>
-__global__ __launch_bounds__(64 * kFewWaves, 2) void k_matmul_few(MatArgs a) {
+__global__ __launch_bounds__(64 * kFewWaves) void k_matmul_few(MatArgs a) {
   using M = FewMfma<CH>;
   constexpr int S = M::kSteps, ROW = CH + 4;  // (ints of a row of sums: 16 bytes more spread them over the banks)
   constexpr int kSums = kFewWaves * CH * ROW, kStage = STAGE ? kFewWaves * TT * CH * 32 : 0;
@@ -475,7 +475,7 @@ static MatPlan matmul_plan(const sjd_i8_weights& w, int T) {
                                     {256, 256, 1, 11.5, 0.875, 1.0}};
   const int64_t bytes = (int64_t)w.N * w.K;
   MatPlan best{0, 0, 1};
-  double least = T <= 128 ? 3.6 + bytes * 0.37e-6 * ((T + 63) / 64) : 1e30;
+  double least = T <= 128 ? 3.6 + bytes * (w.N > 8192 ? 0.29e-6 : 0.37e-6) * ((T + 63) / 64) : 1e30;
   for (const Tile& t : kTiles)
     for (int s = 1; s <= 8; s *= 2) {
       const int64_t wgs = (int64_t)((w.N + t.bn - 1) / t.bn) * ((T + t.bt - 1) / t.bt) * s;
@@ -515,14 +515,16 @@ hipError_t launch_matmul_i8(const sjd_i8_weights& w, const sjd_matmul_io& io, vo
     };
     const std::false_type direct;
     const std::true_type stage;
-    const bool narrow = w.N <= 8192;
-    if (narrow && io.T <= 8) few(Int<16>{}, Int<1>{}, Int<8>{}, direct);
-    else if (narrow && io.T <= 16) few(Int<16>{}, Int<1>{}, Int<8>{}, stage);
-    else if (narrow && io.T <= 32) few(Int<16>{}, Int<2>{}, Int<6>{}, stage);
-    else if (narrow) few(Int<16>{}, Int<4>{}, Int<4>{}, stage);
-    else if (io.T <= 8) few(Int<32>{}, Int<1>{}, Int<4>{}, direct);
-    else if (io.T <= 32) few(Int<32>{}, Int<1>{}, Int<4>{}, stage);
-    else few(Int<32>{}, Int<2>{}, Int<3>{}, stage);
+    // (16 channels to a workgroup where 32 leave compute units without one, or each with so few that
+    // their ends show: us, 16 and 32 channels, of 16 rows 4096 x 4096 5.5 and 6.0, 12288 12.3 and
+    // 13.5, 22016 22.6 and 21.1; of 32 rows 4096 x 11008 15.1 and 17.9, 12288 x 4096 15.5 and 14.8. More
+    // loads in flight cost workgroups: depths 2, 3 and 4 of 32 rows, 22016 x 4096: 22.6, 24.5, 25.8)
+    if (io.T <= 8) few(Int<16>{}, Int<1>{}, Int<4>{}, direct);
+    else if (io.T <= 16 && w.N <= 16384) few(Int<16>{}, Int<1>{}, Int<3>{}, stage);
+    else if (io.T <= 32 && w.N > 8192) few(Int<32>{}, Int<1>{}, Int<2>{}, stage);
+    else if (io.T <= 32) few(Int<16>{}, Int<2>{}, Int<2>{}, stage);
+    else if (w.N > 8192) few(Int<32>{}, Int<2>{}, Int<1>{}, stage);
+    else few(Int<16>{}, Int<4>{}, Int<4>{}, stage);
     return hipGetLastError();
   }
   auto many = [&](auto bt, auto bn, auto vt, auto vn) {
