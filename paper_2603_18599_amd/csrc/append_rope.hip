@@ -257,7 +257,7 @@ hipError_t launch_kv_append_rope(const sjd_pages& p, const sjd_windows& w, const
   for (int i = 0; i < o.pairs; ++i) {
     // (of the size: a fraction of a negative number would round)
     const double v = std::fabs(o.h_freq[i] / 6.283185307179586476925286766559);
-    const uint64_t u = (uint64_t)std::ldexp(v - std::floor(v), 64);
+    const uint64_t u = (uint64_t)((v - std::floor(v)) * 0x1p64);
     a.rev[i] = o.h_freq[i] < 0 ? 0 - u : u;
     a.axis[i] = o.h_axis[i];
   }

@@ -445,10 +445,10 @@ __global__ __launch_bounds__(256) void k_pack_i8(PackArgs a) {
         const int k = k0 + e;
         if (k >= a.K) continue;
         const E s = ((const E*)a.src)[n * a.row + k];
-        int8_t c = 0;
-        if constexpr (kCodes) c = s;
+        uint32_t c = 0;
+        if constexpr (kCodes) c = (uint8_t)s;
         else if (inv[i] > 0.0f) c = code_of(elem_f32(s), inv[i]);
-        v[e / 4] |= (uint32_t)(uint8_t)c << (8 * (e & 3));
+        v[e / 4] |= c << (8 * (e & 3));
       }
     *(uint4*)(a.w + ((int64_t)blockIdx.x * a.ks * 64 + p) * 16) = make_uint4(v[0], v[1], v[2], v[3]);
   }

@@ -106,7 +106,7 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void k_quantise(QuantArgs a) {
     uint32_t w[2] = {};
     if (rs.inv > 0.0f)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) w[e / 4] |= (uint32_t)(uint8_t)code_of(y[i][e], rs.inv) << (8 * (e & 3));
+      for (int e = 0; e < 8; ++e) w[e / 4] |= code_of(y[i][e], rs.inv) << (8 * (e & 3));
     *(uint2*)(code + k) = make_uint2(w[0], w[1]);
   }
 }

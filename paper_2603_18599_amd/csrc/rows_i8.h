@@ -9,8 +9,13 @@ constexpr float kLeastRow = 0x1p-100f;  // rows below it count as zeros (127 / m
 
 SJD_DEV float elem_f32(uint16_t v) { return bf16_to_f32(v); }
 SJD_DEV float elem_f32(float v) { return v; }
-// (e^-x overflows to infinity below -88: the quotient is then -0, the limit)
-SJD_DEV float silu(float x) { return x / (1.0f + expf(-x)); }
+// x / (1 + e^-x) by the hardware's power of two and reciprocal, a step each: a third of the
+// instructions of the library's exponential and a rounded quotient. (The power's argument rounds by
+// 2^-24 of |x| log2 e, which moves the result by x^2 e^-|x| 2^-24 where the power is large: less than
+// a step of a result at 1. Beyond 2^128 the power is infinite, and its reciprocal 0, the limit.)
+SJD_DEV float silu(float x) {
+  return x * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * -1.44269504088896341f));
+}
 
 struct RowScale {
   float scale, inv;  // inv 0: the codes are zeros
@@ -22,7 +27,9 @@ SJD_DEV RowScale row_scale(uint32_t bits, bool bad) {
   if (m < kLeastRow) return {0.0f, 0.0f};
   return {m / 127.0f, 127.0f / m};
 }
-SJD_DEV int8_t code_of(float y, float inv) { return (int8_t)(int)fminf(fmaxf(rintf(y * inv), -127.0f), 127.0f); }
+// The code of y (|y| * inv <= 127 + 2^-16): the sum with 1.5 * 2^23 rounds once, to the nearest
+// whole number, ties to even, and holds it in its low bits
+SJD_DEV uint32_t code_of(float y, float inv) { return __float_as_uint(__builtin_fmaf(y, inv, 12582912.0f)) & 0xFFu; }
 
 // over a workgroup of N threads (scratch: a word per wave)
 template <int N>
