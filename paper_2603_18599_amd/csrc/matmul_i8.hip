@@ -244,8 +244,7 @@ SJD_DEV void put_rows(const MatArgs& a, const int* sums, const float* scales, in
 // Half-way through a step its operands are all in registers: its buffer is filled again, with
 // the step four on.
 template <int BT, int BN, int VT, int VN>
-__global__ __launch_bounds__(64 * VT * VN, BT * BN / (VT * VN) > 64 * 128 ? 1 : 2) void k_matmul_many(MatArgs a, int nt,
-                                                                                                   int nn) {
+__global__ __launch_bounds__(64 * VT * VN, 2) void k_matmul_many(MatArgs a, int nt, int nn) {
   constexpr int WT = BT / VT, WN = BN / VN, FT = WT / 32, FN = WN / 32, WAVES = VT * VN;
   constexpr int kBuf = (BT + BN) * 64;
   __shared__ __align__(256) float scales[BT];
@@ -457,9 +456,9 @@ __global__ __launch_bounds__(256) void k_pack_i8(PackArgs a) {
 }  // namespace
 
 // Which kernel, tile and split of the inputs a product takes: the cheapest by an estimate in
-// us, fitted to 1900 timings of it all (24 to 4096 rows, 512 to 22016 channels, 1024 to 14336
-// inputs; its choice costs 0.4% more than the best of them on average, 7% at most). The
-// results do not depend on it.
+// us, fitted to some 2000 timings of them all (24 to 8190 rows, 512 to 32768 channels, 1024 to
+// 14336 inputs). Over 88 sizes of 256 rows and more its choice took 0.9% more than the best of
+// them on average, 13% at most. The results do not depend on it.
 struct MatPlan {
   int bt, bn;  // rows and channels of a workgroup; bt 0: few rows
   int splits;
@@ -472,7 +471,7 @@ static MatPlan matmul_plan(const sjd_i8_weights& w, int T) {
   };
   static constexpr Tile kTiles[] = {{64, 64, 4, 2.4, 0.195, 0.20},     {64, 128, 2, 4.8, 0.26, 0.225},
                                     {128, 128, 2, 7.1, 0.32, 0.315},   {128, 256, 1, 5.8, 0.475, 0.55},
-                                    {256, 256, 1, 11.5, 0.875, 1.0}};
+                                    {256, 256, 1, 10.0, 0.86, 0.91}};
   const int64_t bytes = (int64_t)w.N * w.K;
   MatPlan best{0, 0, 1};
   double least = T <= 128 ? 3.6 + bytes * (w.N > 8192 ? 0.29e-6 : 0.37e-6) * ((T + 63) / 64) : 1e30;
@@ -533,7 +532,7 @@ hipError_t launch_matmul_i8(const sjd_i8_weights& w, const sjd_matmul_io& io, vo
     const int nt = (io.T + BT - 1) / BT, nn = (w.N + BN - 1) / BN;
     hipLaunchKernelGGL((k_matmul_many<BT, BN, VT, VN>), dim3(nt * nn, p.splits), dim3(64 * VT * VN), 0, s, a, nt, nn);
   };
-  many(Int<256>{}, Int<256>{}, Int<2>{}, Int<2>{});
+  many(Int<256>{}, Int<256>{}, Int<2>{}, Int<4>{});
   many(Int<128>{}, Int<256>{}, Int<2>{}, Int<4>{});
   many(Int<128>{}, Int<128>{}, Int<2>{}, Int<2>{});
   many(Int<64>{}, Int<128>{}, Int<2>{}, Int<2>{});
