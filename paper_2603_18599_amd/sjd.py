@@ -7,7 +7,7 @@ fallback path.
 """
 import ctypes as C
 import os
-from array import array
+import struct
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_NAME = "libsjd.so"
@@ -78,7 +78,7 @@ class RopeParams(C.Structure):
     _fields_ = [("T", C.c_int32), ("H", C.c_int32), ("Hkv", C.c_int32), ("head_dim", C.c_int32),
                 ("pairs", C.c_int32), ("axes", C.c_int32), ("dtype", C.c_int32), ("inverse", C.c_int32),
                 ("q_row", C.c_int64), ("k_row", C.c_int64), ("out_q_row", C.c_int64), ("out_k_row", C.c_int64),
-                ("h_freq", C.c_void_p), ("h_axis", C.c_char_p)]
+                ("h_freq", C.c_char_p), ("h_axis", C.c_char_p)]
 
 
 class RopeIO(C.Structure):
@@ -108,7 +108,7 @@ class AttentionIO(C.Structure):
 
 class AppendRope(C.Structure):
     _fields_ = [("H", C.c_int32), ("pairs", C.c_int32), ("axes", C.c_int32), ("out_dtype", C.c_int32),
-                ("h_freq", C.c_void_p), ("h_axis", C.c_char_p), ("d_pos", C.c_void_p), ("d_q", C.c_void_p),
+                ("h_freq", C.c_char_p), ("h_axis", C.c_char_p), ("d_pos", C.c_void_p), ("d_q", C.c_void_p),
                 ("d_out_q", C.c_void_p), ("q_row", C.c_int64), ("out_q_row", C.c_int64)]
 
 
@@ -344,6 +344,16 @@ def sjd_verify_given(p, q, draft, n, u, r, meta, tok, next=None, *, flags=0, vis
     _launch(fn, stream, dev, C.byref(par), C.byref(io))
 
 
+def _pairs(fn, freq, axis):
+    """Frequencies (double) and axes (bytes) of the pairs of dims, as the library reads them."""
+    n = len(freq)
+    _expect(fn, len(axis) == n)
+    try:
+        return n, struct.pack("%dd" % n, *freq), bytes([*axis])  # (a list: the values, also of an array of words)
+    except (struct.error, TypeError, ValueError):
+        raise SjdError(fn, -1) from None
+
+
 def sjd_rope_axes(q, k, pos, freq, axis, *, out_q=None, out_k=None, inverse=False, stream=None):
     """Rotary positions with several axes (sjd_rope_axes in include/sjd.h) on
     rows q [T, H, hd] and k [T, Hkv, hd] (either may be None; bfloat16 or
@@ -352,9 +362,9 @@ def sjd_rope_axes(q, k, pos, freq, axis, *, out_q=None, out_k=None, inverse=Fals
     fn = "sjd_rope_axes"
     torch, types = _types()
     x = q if q is not None else k
-    _expect(fn, x is not None and x.dim() == 3 and pos.dim() == 2 and len(axis) == len(freq))
+    _expect(fn, x is not None and x.dim() == 3 and pos.dim() == 2)
     (T, _, hd), dt, dev, axes = x.shape, x.dtype, x.get_device(), pos.shape[1]
-    f, ax = array("d", freq), bytes(axis)
+    n, f, ax = _pairs(fn, freq, axis)
 
     def rows(t, out):  # heads, strides and addresses of a tensor and of what it becomes
         if t is None:
@@ -371,8 +381,8 @@ def sjd_rope_axes(q, k, pos, freq, axis, *, out_q=None, out_k=None, inverse=Fals
 
     H, q_row, out_q_row, qp, out_qp = rows(q, out_q)
     Hkv, k_row, out_k_row, kp, out_kp = rows(k, out_k)
-    par = RopeParams(T, H, Hkv, hd, len(f), axes, types.get(dt, -1), 1 if inverse else 0, q_row, k_row, out_q_row,
-                     out_k_row, f.buffer_info()[0], ax)
+    par = RopeParams(T, H, Hkv, hd, n, axes, types.get(dt, -1), 1 if inverse else 0, q_row, k_row, out_q_row, out_k_row, f,
+                     ax)
     io = RopeIO(qp, kp, _dense(fn, pos, (T, axes), torch.int32, dev), out_qp, out_kp)
     _launch(fn, stream, dev, C.byref(par), C.byref(io))
 
@@ -437,16 +447,19 @@ def sjd_kv_append_rope(pages, win, k, v, pos, freq, axis, *, q=None, out_q=None,
     torch, types = _types()
     T, hd, dev, dt = win.T, pages.head_dim, pages.device, k.dtype
     _expect(fn, dt is v.dtype and win.device == dev and k.get_device() == dev and v.get_device() == dev and
-            pos.dim() == 2 and len(axis) == len(freq) and (q is not None or out_q is None))
-    axes, f, ax = pos.shape[1], array("d", freq), bytes(axis)
-    rows = KvRows(k.data_ptr(), v.data_ptr(), _row_stride(fn, k, T, pages.n_kv_heads, hd),
-                  _row_stride(fn, v, T, pages.n_kv_heads, hd), types.get(dt, -1))
-    par = AppendRope(0, len(f), axes, 1, f.buffer_info()[0], ax, _dense(fn, pos, (T, axes), torch.int32, dev))
-    if q is not None:
+            pos.dim() == 2 and (q is not None or out_q is None))
+    axes, Hkv, (n, f, ax) = pos.shape[1], pages.n_kv_heads, _pairs(fn, freq, axis)
+    rows = KvRows(k.data_ptr(), v.data_ptr(), _row_stride(fn, k, T, Hkv, hd), _row_stride(fn, v, T, Hkv, hd),
+                  types.get(dt, -1))
+    at = _dense(fn, pos, (T, axes), torch.int32, dev)
+    if q is None:
+        par = AppendRope(0, n, axes, 1, f, ax, at)
+    else:
         out = q if out_q is None else out_q
         _expect(fn, q.dim() == 3 and q.dtype is dt and q.get_device() == dev and out.get_device() == dev)
-        par.H, par.out_dtype, par.d_q, par.d_out_q = q.shape[1], types.get(out.dtype, -1), q.data_ptr(), out.data_ptr()
-        par.q_row, par.out_q_row = _row_stride(fn, q, T, par.H, hd), _row_stride(fn, out, T, par.H, hd)
+        H = q.shape[1]
+        par = AppendRope(H, n, axes, types.get(out.dtype, -1), f, ax, at, q.data_ptr(), out.data_ptr(),
+                         _row_stride(fn, q, T, H, hd), _row_stride(fn, out, T, H, hd))
     _launch(fn, stream, dev, C.byref(pages.desc), C.byref(win.desc), C.byref(rows), C.byref(par))
 
 

@@ -133,3 +133,38 @@ def test_python_side_refuses_tensors_that_do_not_fit():
             sjd.sjd_matmul_i8(w, *a, **kw)
     with pytest.raises(sjd.SjdError):
         sjd.sjd_pack_i8(w, torch.zeros(40, 49))
+
+
+def test_workspace_of_products():
+    """Split inputs need 32-bit sums: a call without room for them is refused."""
+    lib = sjd.load_library()
+    w = dict(N=4096, K=11008)
+    io = dict(T=128, code_row=11008, out_row=4096, add_row=4096)
+    need = lib.sjd_matmul_i8_workspace(C.byref(sjd.I8WeightsDesc(**{**WEIGHTS, **w})), 128)
+    assert need >= 2 * 128 * 4096 * 4 and need % (128 * 4096 * 4) == 0
+    for ws, size in ((None, need), (None, 0), (P, 0), (P, need - 1), (P + 8, need), (P, -1)):
+        assert matmul(w, io, ws, size) == -1, (ws, size)
+    for b in BAD_WEIGHTS:
+        assert lib.sjd_matmul_i8_workspace(C.byref(sjd.I8WeightsDesc(**{**WEIGHTS, **b})), 128) <= 0, b
+    small = sjd.I8WeightsDesc(**WEIGHTS)
+    assert lib.sjd_matmul_i8_workspace(C.byref(small), 0) == 0 == lib.sjd_matmul_i8_workspace(C.byref(small), 1)
+    assert lib.sjd_matmul_i8_workspace(C.byref(small), -1) <= 0 and lib.sjd_matmul_i8_workspace(None, 1) <= 0
+
+
+@pytest.mark.parametrize("freq, axis", [([1.0] * 4, [0] * 3), ([1.0] * 4, [0, 0, 0, 256]), ([1.0] * 4, [0, -1, 0, 0]),
+                                        ([1.0, 1.0, 1.0, "1"], [0] * 4), ([1.0] * 4, [0, 0, 0.5, 0])])
+def test_pairs_of_other_kinds_are_refused(freq, axis):
+    with pytest.raises(sjd.SjdError):
+        sjd._pairs("sjd_kv_append_rope", freq, axis)
+
+
+def test_pairs_take_any_sequence_of_numbers():
+    import struct
+
+    import numpy as np
+    import torch
+    want = (3, struct.pack("3d", 1.0, 0.5, -0.25), bytes([2, 0, 1]))
+    f, a = [1.0, 0.5, -0.25], [2, 0, 1]
+    for freq, axis in ((f, a), (tuple(f), bytes(a)), (np.float32(f), np.int64(a)), (torch.tensor(f), torch.tensor(a))):
+        assert sjd._pairs("sjd_kv_append_rope", freq, axis) == want
+    assert sjd._pairs("sjd_kv_append_rope", [1.0], torch.tensor([1])) == (1, struct.pack("d", 1.0), b"\1")
