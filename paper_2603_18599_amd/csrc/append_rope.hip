@@ -7,8 +7,9 @@
 // costs 30 instructions and every head of a row shares it, so a workgroup keeps its rows' (cos,
 // sin) in LDS. Keys and values go by tiles of 32 positions as sjd_kv_append's do, queries by
 // themselves beside them: one after the other in a workgroup they took 7.3 us for four tokens,
-// side by side 4.9 (two calls: 3.7 + 4.2). 10400 rows of 32 and 8 heads of 128 into e4m3 pages
-// (232 MB): 42 to 46 us, 5.0 to 5.5 TB/s (two calls 49); of 32 and 32 heads into bf16 pages 114 (120).
+// side by side 4.9 (two calls: 3.7 + 4.2). 10432 rows of 32 and 8 heads of 128 into e4m3 pages
+// (234 MB): 55 us from memory, 4.3 TB/s; 43 where calls follow each other on rows that the last
+// cache still holds in part (two calls 49); of 32 and 32 heads into bf16 pages 107 (120).
 #include "paged_rows.h"
 
 namespace sjd {
@@ -209,36 +210,61 @@ __global__ __launch_bounds__(kThreads) void k_append_rope(PlaceArgs a) {
   lo = max(lo, a.R * part);
   hi = min(hi, a.R * part + a.R);
   if (lo >= hi) return;
-  angles(a, t0, lo, hi, cs);
-  __syncthreads();
   const int np = a.pairs / W, rest = a.out == a.q ? 0 : (HD - 2 * a.pairs) / W, per = np + rest;
   const int step = kThreads / per, g0 = threadIdx.x / per, place = threadIdx.x - g0 * per;
-  if (g0 >= step) return;
-  for (int g = g0; g < (hi - lo) * a.H; g += step) {
-    const int r = lo + g / a.H, h = g % a.H;
-    const int64_t src = (t0 + r) * a.q_row + h * HD, dst = (t0 + r) * a.out_row + h * HD;
-    const float2* const turns = cs + r * turn_row(a.pairs) + place * W;
-    const int j = place < np ? place * W : 2 * a.pairs + (place - np) * W;
-    if constexpr (WIDE) {
-      float x[8], y[8];
-      load_row<F32, 8>(a.q, src + j, x);
-      if (place < np) {
-        load_row<F32, 8>(a.q, src + a.pairs + j, y);
+  const int total = g0 < step ? (hi - lo) * a.H : 0;
+  const int j = place < np ? place * W : 2 * a.pairs + (place - np) * W;
+  if constexpr (WIDE) {
+    // two pieces at a time, ahead of their use, the first ones before the angles (one, loaded when
+    // it is needed: 62 us for the rows above; four: 58)
+    constexpr int U = 2;
+    Raw<F32, 8> x[U], y[U];
+    int r[U], h[U];
+    const int other = place < np ? a.pairs : 0;
+    // (no branches: a wait would be for all that is under way. Items past the last read it again)
+    auto load = [&](int g) __attribute__((always_inline)) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          float u, v;
-          rotate_pair(x[e], y[e], turns[e], u, v);
-          x[e] = u;
-          y[e] = v;
-        }
-        store_row<OUT32, 8>(a.out, dst + a.pairs + j, y);
+      for (int u = 0; u < U; ++u) {
+        const int at = min(g + u * step, (hi - lo) * a.H - 1);
+        r[u] = at / a.H;
+        h[u] = at - r[u] * a.H;
+        r[u] += lo;
+        const int64_t src = (t0 + r[u]) * a.q_row + h[u] * HD + j;
+        x[u].load(a.q, src);
+        y[u].load(a.q, src + other);
       }
-      store_row<OUT32, 8>(a.out, dst + j, x);
-    } else {
+    };
+    load(g0);
+    angles(a, t0, lo, hi, cs);
+    __syncthreads();
+    for (int g = g0; g < total; g += U * step) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (g + u * step >= total) break;
+        const int64_t dst = (t0 + r[u]) * a.out_row + h[u] * HD + j;
+        const float2* const turns = cs + r[u] * turn_row(a.pairs) + place * W;
+        float p[8], q[8];
+        x[u].get(p);
+        if (place < np) {
+          y[u].get(q);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) rotate_pair(p[e], q[e], turns[e], p[e], q[e]);
+          store_row<OUT32, 8>(a.out, dst + a.pairs, q);
+        }
+        store_row<OUT32, 8>(a.out, dst, p);
+      }
+      if (g + U * step < total) load(g + U * step);
+    }
+  } else {
+    angles(a, t0, lo, hi, cs);
+    __syncthreads();
+    for (int g = g0; g < total; g += step) {
+      const int r = lo + g / a.H, h = g % a.H;
+      const int64_t src = (t0 + r) * a.q_row + h * HD, dst = (t0 + r) * a.out_row + h * HD;
       const E* q = (const E*)a.q + src;
       float u = elem(q[j]), v;
       if (place < np) {
-        rotate_pair(u, elem(q[a.pairs + j]), *turns, u, v);
+        rotate_pair(u, elem(q[a.pairs + j]), cs[r * turn_row(a.pairs) + place * W], u, v);
         put<O>(a.out, dst + a.pairs + j, v);
       }
       put<O>(a.out, dst + j, u);
@@ -261,14 +287,15 @@ hipError_t launch_kv_append_rope(const sjd_pages& p, const sjd_windows& w, const
     a.rev[i] = o.h_freq[i] < 0 ? 0 - u : u;
     a.axis[i] = o.h_axis[i];
   }
-  // Up to four heads share a tile's angles, and eight positions' queries theirs, where that leaves
-  // two workgroups of either kind to a compute unit (10400 rows of 32 and 8 heads, us: one head 55,
-  // two 50, four 42; of 32 and 32 heads: four 114, sixteen, which follow each other, 126)
+  // Up to four heads share a tile's angles, and four positions' queries theirs, where that leaves
+  // two workgroups of either kind to a compute unit (10432 rows of 32 and 8 heads, us: one head 63,
+  // two 58, four 55, and with queries of eight positions 58, of sixteen 61; of 32 and 32 heads:
+  // four 107, sixteen, which follow each other, 126)
   const int64_t tiles = (w.max_rows + 62) / 32;
   a.HP = 1;
   while (a.HP < 4 && a.HP < p.n_kv_heads && tiles * w.B * ((p.n_kv_heads + 2 * a.HP - 1) / (2 * a.HP)) >= 512) a.HP *= 2;
   a.YK = (p.n_kv_heads + a.HP - 1) / a.HP;
-  for (a.R = 8; a.R > 1 && tiles * w.B * (32 / a.R) < 512;) a.R /= 2;
+  for (a.R = 4; a.R > 1 && tiles * w.B * (32 / a.R) < 512;) a.R /= 2;
   const dim3 grid(tiles, a.YK + (o.H ? 32 / a.R : 0), w.B), block(kThreads);
   auto go = [&](auto hd, auto fp8, auto f32, auto out32, auto wide) {
     hipLaunchKernelGGL((k_append_rope<decltype(hd)::value, decltype(fp8)::value, decltype(f32)::value,
