@@ -40,37 +40,42 @@ SJD_DEV uint32_t pk_bf16(float a, float b) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
 }
 
+// A sum with its scales, plus an addend: alike in every kernel, so that a row's bits do not
+// depend on which one it meets
+SJD_DEV float scaled(int sum, float ws, float cs) { return (float)sum * ws * cs; }
+SJD_DEV float scaled(int sum, float ws, float cs, float add) { return __builtin_fmaf((float)sum * ws, cs, add); }
+
 // Channels n .. n + 3 of row t, from their sums
-SJD_DEV void put(const MatArgs& a, int t, int n, const i32x4& sum, const float4& ws, float cs) {
-  float v[4] = {(float)sum[0] * ws.x * cs, (float)sum[1] * ws.y * cs, (float)sum[2] * ws.z * cs, (float)sum[3] * ws.w * cs};
+SJD_DEV void put(const MatArgs& a, int t, int n, const i32x4& sum, const float4& scales, float cs) {
+  const float ws[4] = {scales.x, scales.y, scales.z, scales.w};
+  float v[4];
   const int64_t at = t * a.out_row + n, from = t * a.add_row + n;
   if (a.wide && n + 4 <= a.N) {
-    if (a.f32) {
-      if (a.add) {
-        const float4 x = *(const float4*)((const float*)a.add + from);
-        v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
-      }
-      *(float4*)((float*)a.out + at) = make_float4(v[0], v[1], v[2], v[3]);
-    } else {
-      if (a.add) {
-        const uint2 x = *(const uint2*)((const uint16_t*)a.add + from);
-        v[0] += __uint_as_float(x.x << 16); v[1] += __uint_as_float(x.x & 0xFFFF0000u);
-        v[2] += __uint_as_float(x.y << 16); v[3] += __uint_as_float(x.y & 0xFFFF0000u);
-      }
-      *(uint2*)((uint16_t*)a.out + at) = make_uint2(pk_bf16(v[0], v[1]), pk_bf16(v[2], v[3]));
+    float add[4];
+    if (a.add && a.f32) {
+      const float4 x = *(const float4*)((const float*)a.add + from);
+      add[0] = x.x; add[1] = x.y; add[2] = x.z; add[3] = x.w;
+    } else if (a.add) {
+      const uint2 x = *(const uint2*)((const uint16_t*)a.add + from);
+      add[0] = __uint_as_float(x.x << 16); add[1] = __uint_as_float(x.x & 0xFFFF0000u);
+      add[2] = __uint_as_float(x.y << 16); add[3] = __uint_as_float(x.y & 0xFFFF0000u);
     }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = a.add ? scaled(sum[e], ws[e], cs, add[e]) : scaled(sum[e], ws[e], cs);
+    if (a.f32) *(float4*)((float*)a.out + at) = make_float4(v[0], v[1], v[2], v[3]);
+    else *(uint2*)((uint16_t*)a.out + at) = make_uint2(pk_bf16(v[0], v[1]), pk_bf16(v[2], v[3]));
     return;
   }
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     if (n + e >= a.N) break;
-    if (a.f32) {
-      if (a.add) v[e] += ((const float*)a.add)[from + e];
-      ((float*)a.out)[at + e] = v[e];
-    } else {
-      if (a.add) v[e] += bf16_to_f32(((const uint16_t*)a.add)[from + e]);
-      ((uint16_t*)a.out)[at + e] = f32_to_bf16(v[e]);
+    float x = scaled(sum[e], ws[e], cs);
+    if (a.add) {
+      const float add = a.f32 ? ((const float*)a.add)[from + e] : bf16_to_f32(((const uint16_t*)a.add)[from + e]);
+      x = scaled(sum[e], ws[e], cs, add);
     }
+    if (a.f32) ((float*)a.out)[at + e] = x;
+    else ((uint16_t*)a.out)[at + e] = f32_to_bf16(x);
   }
 }
 SJD_DEV float4 channel_scales(const MatArgs& a, int n) {
@@ -223,17 +228,20 @@ SJD_DEV void put_rows(const MatArgs& a, const int* sums, const float* scales, in
 #pragma unroll
   for (int i = 0; i < U; ++i) {
     const int t = t0 + q0 + i * STEP;
-    float v[4] = {(float)c[i][0] * ws.x * cs[i], (float)c[i][1] * ws.y * cs[i], (float)c[i][2] * ws.z * cs[i],
-                  (float)c[i][3] * ws.w * cs[i]};
+    float v[4], x[4] = {};
+    if constexpr (ADD && F32) {
+      x[0] = add[i].x, x[1] = add[i].y, x[2] = add[i].z, x[3] = add[i].w;
+    } else if constexpr (ADD) {
+      x[0] = __uint_as_float(add[i].x << 16), x[1] = __uint_as_float(add[i].x & 0xFFFF0000u);
+      x[2] = __uint_as_float(add[i].y << 16), x[3] = __uint_as_float(add[i].y & 0xFFFF0000u);
+    }
+    const float w[4] = {ws.x, ws.y, ws.z, ws.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = ADD ? scaled(c[i][e], w[e], cs[i], x[e]) : scaled(c[i][e], w[e], cs[i]);
     P* const out = (P*)((char*)a.out + (t * a.out_row + n) * ES);
     if constexpr (F32) {
-      if constexpr (ADD) v[0] += add[i].x, v[1] += add[i].y, v[2] += add[i].z, v[3] += add[i].w;
       if (t < a.T) *out = make_float4(v[0], v[1], v[2], v[3]);
     } else {
-      if constexpr (ADD) {
-        v[0] += __uint_as_float(add[i].x << 16), v[1] += __uint_as_float(add[i].x & 0xFFFF0000u);
-        v[2] += __uint_as_float(add[i].y << 16), v[3] += __uint_as_float(add[i].y & 0xFFFF0000u);
-      }
       if (t < a.T) *out = make_uint2(pk_bf16(v[0], v[1]), pk_bf16(v[2], v[3]));
     }
   }

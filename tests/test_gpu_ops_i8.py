@@ -204,6 +204,21 @@ def test_rows_do_not_depend_on_their_company():
         assert torch.equal(run(h, a[lo:lo + n].contiguous(), s[lo:lo + n].contiguous(), "fp32"), whole[lo:lo + n])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("N,K", [(1100, 1536), (1101, 1537), (512, 8192)])
+def test_rows_with_addends_do_not_depend_on_their_company(N, K, dtype):
+    """The addend joins by the same steps in the kernels of few and of many rows, where
+    the inputs are split and where channels do not come by fours."""
+    h, w = weights(N, K, 1)
+    a, s = codes(1500, K, 2)
+    add = torch.randn(1500, N, device="cuda").to(DT[dtype])
+    whole = run(h, a, s, dtype, add)
+    assert len({sjd.matmul_workspace(h, n).numel() > 0 for n in (1, 100, 300, 700, 1500)}) == (2 if K == 8192 else 1)
+    for lo, n in ((0, 1), (699, 1), (5, 16), (100, 33), (30, 100), (7, 300), (200, 700)):
+        assert torch.equal(run(h, a[lo:lo + n].contiguous(), s[lo:lo + n].contiguous(), dtype, add[lo:lo + n].contiguous()),
+                           whole[lo:lo + n]), (lo, n)
+
+
 def test_nan_scales_and_addends_stay_in_their_rows():
     N, K, T = 150, 256, 70
     h, w = weights(N, K, 3)
