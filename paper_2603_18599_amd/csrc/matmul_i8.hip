@@ -1,6 +1,7 @@
 // Products in 8-bit integers (definition: sjd.h): rows of codes with packed weights,
 // exact in 32-bit integers, then the scales of row and channel.
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "device.h"
@@ -28,7 +29,6 @@ struct MatArgs {
   int T, N, cols;  // cols: codes of a row that are there
   int nb, ks;
   int f32;
-  int wide;  // four channels of a row are aligned for one access
   int splits;      // of the inputs; with more than one
   int32_t* sums;   // .. sums of their parts, [splits][T][32 nb]
 };
@@ -45,38 +45,56 @@ SJD_DEV uint32_t pk_bf16(float a, float b) {
 SJD_DEV float scaled(int sum, float ws, float cs) { return (float)sum * ws * cs; }
 SJD_DEV float scaled(int sum, float ws, float cs, float add) { return __builtin_fmaf((float)sum * ws, cs, add); }
 
+// Four channels of an output row, which may start at any element: one access of the size of
+// four elements at the alignment of one. (Where a row is aligned for no more, such an access
+// passes lane by lane: 2748 rows of 779 channels in large tiles take 27 us, of 780 15. Elements
+// of a row one behind the other take 24, but in small tiles 18% longer than these.)
+template <bool F32>
+struct Four {
+  using E = std::conditional_t<F32, float, uint16_t>;
+  E v[4];
+  SJD_DEV void load(const void* base, int64_t at) { __builtin_memcpy(v, (const E*)base + at, sizeof v); }
+  SJD_DEV float get(int e) const {
+    if constexpr (F32) return v[e];
+    else return bf16_to_f32(v[e]);
+  }
+};
+template <bool F32>
+SJD_DEV void store_four(void* base, int64_t at, const float (&v)[4]) {
+  if constexpr (F32) {
+    __builtin_memcpy((float*)base + at, v, sizeof v);
+  } else {
+    const uint32_t u[2] = {pk_bf16(v[0], v[1]), pk_bf16(v[2], v[3])};
+    __builtin_memcpy((uint16_t*)base + at, u, sizeof u);
+  }
+}
+
 // Channels n .. n + 3 of row t, from their sums
+template <bool F32>
 SJD_DEV void put(const MatArgs& a, int t, int n, const i32x4& sum, const float4& scales, float cs) {
+  using E = typename Four<F32>::E;
   const float ws[4] = {scales.x, scales.y, scales.z, scales.w};
-  float v[4];
   const int64_t at = t * a.out_row + n, from = t * a.add_row + n;
-  if (a.wide && n + 4 <= a.N) {
-    float add[4];
-    if (a.add && a.f32) {
-      const float4 x = *(const float4*)((const float*)a.add + from);
-      add[0] = x.x; add[1] = x.y; add[2] = x.z; add[3] = x.w;
-    } else if (a.add) {
-      const uint2 x = *(const uint2*)((const uint16_t*)a.add + from);
-      add[0] = __uint_as_float(x.x << 16); add[1] = __uint_as_float(x.x & 0xFFFF0000u);
-      add[2] = __uint_as_float(x.y << 16); add[3] = __uint_as_float(x.y & 0xFFFF0000u);
-    }
+  Four<F32> x = {};
+  float v[4];
+  if (n + 4 <= a.N) {
+    if (a.add) x.load(a.add, from);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = a.add ? scaled(sum[e], ws[e], cs, add[e]) : scaled(sum[e], ws[e], cs);
-    if (a.f32) *(float4*)((float*)a.out + at) = make_float4(v[0], v[1], v[2], v[3]);
-    else *(uint2*)((uint16_t*)a.out + at) = make_uint2(pk_bf16(v[0], v[1]), pk_bf16(v[2], v[3]));
+    for (int e = 0; e < 4; ++e) v[e] = a.add ? scaled(sum[e], ws[e], cs, x.get(e)) : scaled(sum[e], ws[e], cs);
+    store_four<F32>(a.out, at, v);
     return;
   }
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     if (n + e >= a.N) break;
-    float x = scaled(sum[e], ws[e], cs);
-    if (a.add) {
-      const float add = a.f32 ? ((const float*)a.add)[from + e] : bf16_to_f32(((const uint16_t*)a.add)[from + e]);
-      x = scaled(sum[e], ws[e], cs, add);
-    }
-    if (a.f32) ((float*)a.out)[at + e] = x;
-    else ((uint16_t*)a.out)[at + e] = f32_to_bf16(x);
+    if (a.add) x.v[e] = ((const E*)a.add)[from + e];
+    v[e] = a.add ? scaled(sum[e], ws[e], cs, x.get(e)) : scaled(sum[e], ws[e], cs);
+    if constexpr (F32) ((E*)a.out)[at + e] = v[e];
+    else ((E*)a.out)[at + e] = f32_to_bf16(v[e]);
   }
+}
+SJD_DEV void put(const MatArgs& a, int t, int n, const i32x4& sum, const float4& scales, float cs) {
+  a.f32 ? put<true>(a, t, n, sum, scales, cs) : put<false>(a, t, n, sum, scales, cs);
 }
 SJD_DEV float4 channel_scales(const MatArgs& a, int n) {
   return make_float4(a.wscale[min(n, a.N - 1)], a.wscale[min(n + 1, a.N - 1)], a.wscale[min(n + 2, a.N - 1)],
@@ -209,40 +227,41 @@ SJD_DEV void wait_barrier() {
   asm volatile("" ::: "memory");
 }
 
-// Rows q0 + i * STEP (i < U) of a wave's block of sums in LDS, scaled and stored: four
+// A wave's block of sums in LDS, 32 rows of WN channels (n0 ..), scaled and stored, four
 // channels a lane
-template <bool F32, bool ADD, int U, int STEP, int OUT>
-SJD_DEV void put_rows(const MatArgs& a, const int* sums, const float* scales, int t0, int q0, int n, const float4& ws) {
-  using P = std::conditional_t<F32, float4, uint2>;
-  constexpr int ES = F32 ? 4 : 2;
-  i32x4 c[U];
-  P add[U];
-  float cs[U];
-#pragma unroll
-  for (int i = 0; i < U; ++i) {
-    const int q = q0 + i * STEP;
-    c[i] = *(const i32x4*)(sums + q * OUT);
-    cs[i] = scales[q];
-    if constexpr (ADD) add[i] = *(const P*)((const char*)a.add + (min(t0 + q, a.T - 1) * a.add_row + n) * ES);
+template <bool F32, bool ADD, int WN, int OUT>
+SJD_DEV void put_block(const MatArgs& a, const int* sums, const float* scales, int t0, int n0, const float4& ws) {
+  constexpr int LPR = WN / 4, STEP = 64 / LPR, U = 32 / STEP < 8 ? 32 / STEP : 8;
+  const int lane = threadIdx.x & 63, q0 = lane / LPR, col = lane % LPR * 4, n = n0 + col;
+  if (n >= a.N) return;
+  sums += col;
+  if (n + 4 > a.N) {
+    for (int q = q0; q < 32; q += STEP)
+      if (t0 + q < a.T) put<F32>(a, t0 + q, n, *(const i32x4*)(sums + q * OUT), ws, scales[q]);
+    return;
   }
+  const float w[4] = {ws.x, ws.y, ws.z, ws.w};
+  for (int qu = q0; qu < 32; qu += U * STEP) {
+    i32x4 c[U];
+    Four<F32> add[U];
+    float cs[U];
 #pragma unroll
-  for (int i = 0; i < U; ++i) {
-    const int t = t0 + q0 + i * STEP;
-    float v[4], x[4] = {};
-    if constexpr (ADD && F32) {
-      x[0] = add[i].x, x[1] = add[i].y, x[2] = add[i].z, x[3] = add[i].w;
-    } else if constexpr (ADD) {
-      x[0] = __uint_as_float(add[i].x << 16), x[1] = __uint_as_float(add[i].x & 0xFFFF0000u);
-      x[2] = __uint_as_float(add[i].y << 16), x[3] = __uint_as_float(add[i].y & 0xFFFF0000u);
+    for (int i = 0; i < U; ++i) {
+      const int q = qu + i * STEP;
+      c[i] = *(const i32x4*)(sums + q * OUT);
+      cs[i] = scales[q];
+      if constexpr (ADD) add[i].load(a.add, min(t0 + q, a.T - 1) * a.add_row + n);
     }
-    const float w[4] = {ws.x, ws.y, ws.z, ws.w};
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = ADD ? scaled(c[i][e], w[e], cs[i], x[e]) : scaled(c[i][e], w[e], cs[i]);
-    P* const out = (P*)((char*)a.out + (t * a.out_row + n) * ES);
-    if constexpr (F32) {
-      if (t < a.T) *out = make_float4(v[0], v[1], v[2], v[3]);
-    } else {
-      if (t < a.T) *out = make_uint2(pk_bf16(v[0], v[1]), pk_bf16(v[2], v[3]));
+    for (int i = 0; i < U; ++i) {
+      const int t = t0 + qu + i * STEP;
+      float v[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if constexpr (ADD) v[e] = scaled(c[i][e], w[e], cs[i], add[i].get(e));
+        else v[e] = scaled(c[i][e], w[e], cs[i]);
+      }
+      if (t < a.T) store_four<F32>(a.out, t * a.out_row + n, v);
     }
   }
 }
@@ -279,24 +298,19 @@ __global__ __launch_bounds__(64 * VT * VN, 2) void k_matmul_many(MatArgs a, int 
   const char* w[LN];
   const int kl = 16 * swizzle<4>(lane >> 2, lane & 3);
 #pragma unroll
-  for (int i = 0; i < LT; ++i)
-    code[i] = a.code + min(t0 + 16 * (wave * LT + i) + (lane >> 2), a.T - 1) * a.code_row + (int64_t)u0 * 64 + kl;
+  for (int i = 0; i < LT; ++i) code[i] = a.code + min(t0 + 16 * (wave * LT + i) + (lane >> 2), a.T - 1) * a.code_row;
 #pragma unroll
   for (int i = 0; i < LN; ++i) {
     const int q = wave * LN + i;  // row block q / 2, tile q % 2 of the step
-    w[i] = a.w + ((int64_t)min(b0 + q / 2, a.nb - 1) * a.ks + 2 * u0 + q % 2) * 1024;
+    w[i] = a.w + ((int64_t)min(b0 + q / 2, a.nb - 1) * a.ks + q % 2) * 1024;
   }
-  // load p of step u (its pointer then is at the next step's). FULL: no code lies behind its row;
-  // else such a piece reads the row's first, against weights of zero
-  auto fill = [&](auto full, char* lds, int u, int p) __attribute__((always_inline)) {
-    if (p < LT) {
-      const int k = u * 64 + kl;
-      load_lds(decltype(full)::value || k < a.cols ? code[p] : code[p] - k, lds + (wave * LT + p) * 1024);
-      code[p] += 64;
-    } else {
-      load_lds(w[p - LT] + (uint32_t)(lane * 16), lds + BT * 64 + (wave * LN + p - LT) * 1024);
-      w[p - LT] += 2048;
-    }
+  // Load p of step u. Steps behind the last read it once more, and codes behind a row its last 16,
+  // against weights of zero: without a branch the compiler knows which loads are under way (with
+  // one for each it waited for all of them in a call's last 8 to 11 steps, 2 us at a time).
+  auto fill = [&](char* lds, int u, int p) __attribute__((always_inline)) {
+    const int at = min(u, u1 - 1);
+    if (p < LT) load_lds(code[p] + min(at * 64 + kl, a.cols - 16), lds + (wave * LT + p) * 1024);
+    else load_lds(w[p - LT] + at * 2048 + (uint32_t)(lane * 16), lds + BT * 64 + (wave * LN + p - LT) * 1024);
   };
   i32x16 c[FT][FN] = {};
   i32x4 x[2][FT], y[2][FN];
@@ -309,96 +323,93 @@ __global__ __launch_bounds__(64 * VT * VN, 2) void k_matmul_many(MatArgs a, int 
 #pragma unroll
     for (int j = 0; j < FN; ++j) y[s][j] = *(const i32x4*)(lds + BT * 64 + ((wn + j) * 2 + s) * 1024 + lane * 16);
   };
-  // Products of half a step, `more`: with loads P0 .. P1 - 1 of step u between them. They go out one
+  // Products of half a step, with loads P0 .. P1 - 1 of step u between them. They go out one
   // at a time, over a whole step: the waves' loads of half of it would wait for each other.
-  auto multiply = [&](auto full, int s, bool more, char* lds, int u, auto p0, auto p1) __attribute__((always_inline)) {
+  auto multiply = [&](int s, char* lds, int u, auto p0, auto p1) __attribute__((always_inline)) {
     constexpr int P0 = decltype(p0)::value, N = decltype(p1)::value - P0;
 #pragma unroll
     for (int i = 0; i < FT; ++i) {
-      if (more) {
 #pragma unroll
-        for (int p = 0; p < N; ++p)
-          if (p * FT / N == i) fill(full, lds, u, P0 + p);
-      }
+      for (int p = 0; p < N; ++p)
+        if (p * FT / N == i) fill(lds, u, P0 + p);
 #pragma unroll
       for (int j = 0; j < FN; ++j) c[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(y[s][j], x[s][i], c[i][j], 0, 0, 0);
     }
   };
-  // FULL: there are eight steps behind it
-  auto step = [&](auto full, char* now, const char* next, char* last, int u) __attribute__((always_inline)) {
-    constexpr bool FULL = decltype(full)::value;
-    if (!FULL && u >= u1) return;
+  auto step = [&](char* now, const char* next, char* last, int u) __attribute__((always_inline)) {
     frags(now, 1);
-    multiply(full, 0, FULL || u + 3 < u1, last, u + 3, Int<L0>{}, Int<L>{});
+    multiply(0, last, u + 3, Int<L0>{}, Int<L>{});
     // the next step is there, and no wave reads this one's buffer any more
-    if (FULL || u + 3 < u1) wait_barrier<2 * L>();
-    else if (u + 2 < u1) wait_barrier<L>();
-    else wait_barrier<0>();
-    if (FULL || u + 1 < u1) frags(next, 0);
-    multiply(full, 1, FULL || u + 4 < u1, now, u + 4, Int<0>{}, Int<L0>{});
+    wait_barrier<2 * L>();
+    frags(next, 0);
+    multiply(1, now, u + 4, Int<0>{}, Int<L0>{});
   };
   const float cs = threadIdx.x < BT ? a.cscale[min(t0 + (int)threadIdx.x, a.T - 1)] : 0.0f;
-  const std::false_type checked;
 #pragma unroll
   for (int p = 0; p < 3 * L + L0; ++p) {
     const int i = p / L;
-    if (i == 0 || u0 + i < u1) fill(checked, i == 0 ? lds0 : i == 1 ? lds1 : i == 2 ? lds2 : lds3, u0 + i, p % L);
+    fill(i == 0 ? lds0 : i == 1 ? lds1 : i == 2 ? lds2 : lds3, u0 + i, p % L);
   }
-  if (u0 + 3 < u1) wait_barrier<2 * L + L0>();
-  else wait_barrier<0>();
+  wait_barrier<2 * L + L0>();
   frags(lds0, 0);
   int u = u0;
-  auto four = [&](auto full) __attribute__((always_inline)) {
-    step(full, lds0, lds1, lds3, u);
-    step(full, lds1, lds2, lds0, u + 1);
-    step(full, lds2, lds3, lds1, u + 2);
-    step(full, lds3, lds0, lds2, u + 3);
-  };
-  for (; u + 12 <= u1; u += 4) four(std::true_type{});
-  for (; u < u1; u += 4) four(checked);
+  for (; u + 4 <= u1; u += 4) {
+    step(lds0, lds1, lds3, u);
+    step(lds1, lds2, lds0, u + 1);
+    step(lds2, lds3, lds1, u + 2);
+    step(lds3, lds0, lds2, u + 3);
+  }
+  if (u < u1) {
+    step(lds0, lds1, lds3, u);
+    if (u + 1 < u1) step(lds1, lds2, lds0, u + 1);
+    if (u + 2 < u1) step(lds2, lds3, lds1, u + 2);
+  }
+  wait_barrier<0>();  // (loads of steps behind the last)
 
   // Blocks of 32 rows pass through a part of LDS of the wave's own, to leave in whole rows
   // (register r of a block: channel 8 (r / 4) + 4 (lane / 32) + r % 4, row lane % 32)
-  constexpr int OUT = WN + 4, kParts = kBuf / (32 * OUT * 4), LPR = WN / 4, RPI = 64 / LPR, U = 32 / RPI < 8 ? 32 / RPI : 8;
+  constexpr int OUT = WN + 4, kParts = kBuf / (32 * OUT * 4), LPR = WN / 4;
   static_assert(kParts * 4 >= WAVES && BT <= 64 * WAVES, "a part for each wave, a scale for each thread");
   if (threadIdx.x < BT) scales[threadIdx.x] = cs;
   __syncthreads();
   const int part = wave / kParts;
   int* const mine = (int*)(part == 0 ? lds0 : part == 1 ? lds1 : part == 2 ? lds2 : lds3) + wave % kParts * (32 * OUT);
-  const int col = lane % LPR * 4, n = (b0 + wn) * 32 + col, q0 = lane / LPR;
-  const float4 ws = channel_scales(a, n);
-  const int64_t row = a.nb * 32LL;
-  int32_t* const sums = a.sums + (int64_t)blockIdx.y * a.T * row + n;
+  const int n0 = (b0 + wn) * 32;
+  const float4 ws = channel_scales(a, n0 + lane % LPR * 4);
+  auto blocks = [&](auto leave) __attribute__((always_inline)) {
 #pragma unroll
-  for (int i = 0; i < FT; ++i) {
+    for (int i = 0; i < FT; ++i) {
 #pragma unroll
-    for (int j = 0; j < FN; ++j)
+      for (int j = 0; j < FN; ++j)
 #pragma unroll
-      for (int r = 0; r < 16; r += 4)
-        *(i32x4*)(mine + (lane & 31) * OUT + 32 * j + 2 * r + 4 * (lane >> 5)) =
-            i32x4{c[i][j][r], c[i][j][r + 1], c[i][j][r + 2], c[i][j][r + 3]};
-    const int tb = t0 + wt + 32 * i;
-    const float* const sc = scales + wt + 32 * i;
-    if (a.splits > 1) {
-#pragma unroll
-      for (int q = 0; q < 32; q += RPI) {
-        const i32x4 v = *(const i32x4*)(mine + (q0 + q) * OUT + col);
-        if (tb + q0 + q < a.T && n < row) *(i32x4*)(sums + (tb + q0 + q) * row) = v;
-      }
-    } else if (a.wide && n + 4 <= a.N) {
-      for (int q = q0; q < 32; q += U * RPI) {
-        if (a.f32) {
-          if (a.add) put_rows<true, true, U, RPI, OUT>(a, mine + col, sc, tb, q, n, ws);
-          else put_rows<true, false, U, RPI, OUT>(a, mine + col, sc, tb, q, n, ws);
-        } else {
-          if (a.add) put_rows<false, true, U, RPI, OUT>(a, mine + col, sc, tb, q, n, ws);
-          else put_rows<false, false, U, RPI, OUT>(a, mine + col, sc, tb, q, n, ws);
-        }
-      }
-    } else if (n < a.N) {
-      for (int q = q0; q < 32; q += RPI)
-        if (tb + q < a.T) put(a, tb + q, n, *(const i32x4*)(mine + q * OUT + col), ws, sc[q]);
+        for (int r = 0; r < 16; r += 4)
+          *(i32x4*)(mine + (lane & 31) * OUT + 32 * j + 2 * r + 4 * (lane >> 5)) =
+              i32x4{c[i][j][r], c[i][j][r + 1], c[i][j][r + 2], c[i][j][r + 3]};
+      leave(wt + 32 * i);
     }
+  };
+  auto rows = [&](auto f32, auto add) __attribute__((always_inline)) {
+    blocks([&](int t) __attribute__((always_inline)) {
+      put_block<decltype(f32)::value, decltype(add)::value, WN, OUT>(a, mine, scales + t, t0 + t, n0, ws);
+    });
+  };
+  const std::true_type yes;
+  const std::false_type no;
+  if (a.splits > 1) {
+    const int64_t row = a.nb * 32LL;
+    const int col = lane % LPR * 4, n = n0 + col;
+    int32_t* const sums = a.sums + (int64_t)blockIdx.y * a.T * row + n;
+    blocks([&](int t) __attribute__((always_inline)) {
+#pragma unroll
+      for (int q = 0; q < 32; q += 64 / LPR) {
+        const int r = q + lane / LPR;
+        const i32x4 v = *(const i32x4*)(mine + r * OUT + col);
+        if (t0 + t + r < a.T && n < row) *(i32x4*)(sums + (t0 + t + r) * row) = v;
+      }
+    });
+  } else {
+    if (a.f32) a.add ? rows(yes, yes) : rows(yes, no);
+    else a.add ? rows(no, yes) : rows(no, no);
   }
 }
 
@@ -464,36 +475,84 @@ __global__ __launch_bounds__(256) void k_pack_i8(PackArgs a) {
 }  // namespace
 
 // Which kernel, tile and split of the inputs a product takes: the cheapest by an estimate in
-// us, fitted to some 2000 timings of them all (24 to 8190 rows, 512 to 32768 channels, 1024 to
-// 14336 inputs). Over 88 sizes of 256 rows and more its choice took 0.9% more than the best of
-// them on average, 13% at most. The results do not depend on it.
+// us, fitted to 5170 timings of them all (33 to 5569 rows, 272 to 30197 channels, 289 to 14336
+// inputs; 10% off, root mean square). Over their 480 sizes its choice took 1.5% more than the
+// best of them on average, 43% at most. The results do not depend on it.
 struct MatPlan {
   int bt, bn;  // rows and channels of a workgroup; bt 0: few rows
   int splits;
+  double us;
 };
-static MatPlan matmul_plan(const sjd_i8_weights& w, int T) {
-  if (T <= 32) return {0, 0, 1};
+static MatPlan plan_of(int N, int K, int T) {
+  // a step of 64 inputs takes `half` where half of the compute units have a workgroup, `whole`
+  // where all have, `shared` for each of several; one more round of workgroups takes `gap`, the
+  // outputs of a workgroup whose rows are not aligned `odd`
   struct Tile {
-    int bt, bn, fit;             // .. workgroups on a compute unit
-    double fixed, alone, shared;  // start and end; a step of 64 inputs, of one and of each of several on a unit
+    int bt, bn, fit;  // .. workgroups that share a unit
+    double fixed, half, whole, shared, gap, odd;
   };
-  static constexpr Tile kTiles[] = {{64, 64, 4, 2.4, 0.195, 0.20},     {64, 128, 2, 4.8, 0.26, 0.225},
-                                    {128, 128, 2, 7.1, 0.32, 0.315},   {128, 256, 1, 5.8, 0.475, 0.55},
-                                    {256, 256, 1, 10.0, 0.86, 0.91}};
-  const int64_t bytes = (int64_t)w.N * w.K;
-  MatPlan best{0, 0, 1};
-  double least = T <= 128 ? 3.6 + bytes * (w.N > 8192 ? 0.29e-6 : 0.37e-6) * ((T + 63) / 64) : 1e30;
+  static constexpr Tile kTiles[] = {{64, 64, 4, 3.1, 0.138, 0.150, 0.102, 0.1, 0.7},
+                                    {64, 128, 2, 3.5, 0.161, 0.099, 0.127, 0.3, 1.7},
+                                    {128, 128, 2, 4.3, 0.238, 0.227, 0.247, 2.8, 3.2},
+                                    {128, 256, 1, 4.9, 0.347, 0.372, 0.371, 4.5, 3.4},
+                                    {256, 256, 1, 7.0, 0.597, 0.740, 0.814, 4.2, 7.7}};
+  const double bytes = (double)N * K;
+  MatPlan best{0, 0, 1, 1e30};
+  if (T <= 128) {
+    const int more = (T + 63) / 64 - 1;
+    best.us = 4.1 + std::hypot(bytes * (N > 8192 ? 0.28e-6 + 0.155e-6 * more : 0.352e-6 + 0.338e-6 * more), K * 0.58e-3);
+  }
+  if (T <= 32) return best;
   for (const Tile& t : kTiles)
     for (int s = 1; s <= 8; s *= 2) {
-      const int64_t wgs = (int64_t)((w.N + t.bn - 1) / t.bn) * ((T + t.bt - 1) / t.bt) * s;
-      if (s > 1 && (wgs > 640 || w.K < 512 * s)) break;
-      const int64_t per = (wgs + 255) / 256, rounds = (per + t.fit - 1) / t.fit;
-      double us = t.fixed + (rounds - 1) * 1.2 + (w.K + 127) / 128 * 2.0 / s * (per == 1 ? t.alone : per * t.shared);
-      us = std::max(us, 4 + bytes * 0.25e-6);                           // the weights from memory
-      if (s > 1) us += 3.3 + (double)s * T * w.N * 2.5e-6;              // the parts' sums, and a launch
-      if (us < least) least = us, best = MatPlan{t.bt, t.bn, s};
+      const int64_t nt = (T + t.bt - 1) / t.bt, wgs = (N + t.bn - 1) / t.bn * nt * s;
+      if (s > 1 && (wgs > 640 || K < 512 * s)) break;
+      const int64_t per = (wgs + 255) / 256, last = t.fit > 1 ? wgs : wgs - (per - 1) * 256;
+      const double steps = (K + 127) / 128 * 2.0 / s;
+      double work;
+      if (per == 1 || t.fit == 1)
+        work = steps * (t.half + (t.whole - t.half) * std::clamp(last / 128.0 - 1, 0.0, 1.0)) +
+               (per - 1) * (t.gap + steps * t.shared);
+      else
+        work = steps * per * t.shared + ((per + t.fit - 1) / t.fit - 1) * t.gap;
+      if (N % 4 && s == 1) work += per * t.odd;
+      // (the weights pass from memory, and once more for every row of tiles, beside the work)
+      double us = t.fixed + std::hypot(work, bytes * (0.235e-6 + 0.073e-6 * (nt - 1)));
+      if (s > 1) us += 2.0 + 1.43e-6 * s * T * N;  // the parts' sums, and a launch
+      if (us < best.us) best = MatPlan{t.bt, t.bn, s, us};
     }
   return best;
+}
+
+// Rows [t0, t0 + T) and channels [n0, n0 + N) of a product, one launch
+struct MatPart {
+  int t0, T, n0, N;
+  MatPlan plan;
+};
+// The last round of large tiles may leave most compute units without one: where the estimate
+// gains by it, whole rounds are one launch, and the rows or channels that are left another, of
+// tiles that suit them. Returns the number of parts.
+static int matmul_parts(int N, int K, int T, MatPart (&part)[2]) {
+  part[0] = {0, T, 0, N, plan_of(N, K, T)};
+  if (T <= 128 || part[0].plan.splits > 1) return 1;
+  double least = part[0].plan.us * 0.98;
+  int parts = 1;
+  auto consider = [&](int T1, int N1) {
+    if (T1 <= 0 || N1 <= 0 || (T1 >= T && N1 >= N)) return;
+    const MatPart a{0, std::min(T1, T), 0, std::min(N1, N), plan_of(std::min(N1, N), K, std::min(T1, T))};
+    const MatPart b = a.T < T ? MatPart{a.T, T - a.T, 0, N, plan_of(N, K, T - a.T)}
+                              : MatPart{0, T, a.N, N - a.N, plan_of(N - a.N, K, T)};
+    const double us = a.plan.us + b.plan.us + 1;
+    if (us < least) least = us, part[0] = a, part[1] = b, parts = 2;
+  };
+  for (int bt : {128, 256}) {
+    const int64_t nt = (T + bt - 1) / bt, nn = (N + 255) / 256, full = nt * nn / 256 * 256;
+    if (full) {
+      consider(T, (int)std::min<int64_t>(full / nt, nn - 1) * 256);
+      consider((int)std::min<int64_t>(full / nn, nt - 1) * bt, N);
+    }
+  }
+  return parts;
 }
 
 int64_t i8_weight_bytes(int N, int K) {
@@ -501,24 +560,29 @@ int64_t i8_weight_bytes(int N, int K) {
   return (int64_t)s.nb * s.ks * 1024;
 }
 
+static int64_t sums_bytes(const MatPart& p) {
+  return p.plan.splits > 1 ? (int64_t)p.plan.splits * p.T * ((p.N + 31) / 32) * 128 : 0;
+}
 int64_t matmul_i8_ws(const sjd_i8_weights& w, int T) {
-  const MatPlan p = matmul_plan(w, T);
-  return p.splits > 1 ? (int64_t)p.splits * T * i8_shape(w.N, w.K).nb * 128 : 0;
+  MatPart p[2];
+  return matmul_parts(w.N, w.K, T, p) == 1 ? sums_bytes(p[0]) : std::max(sums_bytes(p[0]), sums_bytes(p[1]));
 }
 
-hipError_t launch_matmul_i8(const sjd_i8_weights& w, const sjd_matmul_io& io, void* ws, hipStream_t s) {
-  const I8Shape sh = i8_shape(w.N, w.K);
-  const MatPlan p = matmul_plan(w, io.T);
+static void launch_part(const sjd_i8_weights& w, const sjd_matmul_io& io, const MatPart& part, void* ws, hipStream_t s) {
+  const MatPlan& p = part.plan;
+  const int T = part.T, N = part.N;
+  const I8Shape sh = i8_shape(N, w.K);
   const uintptr_t es = io.dtype == SJD_F32 ? 4 : 2;
-  auto fine = [&](const void* q, int64_t row) { return ((uintptr_t)q & (4 * es - 1)) == 0 && row % 4 == 0; };
-  const MatArgs a{(const char*)w.d_w, w.d_scale, io.d_code, io.d_code_scale, io.d_out, io.d_add, io.code_row, io.out_row,
-                  io.add_row, io.T, w.N, (w.K + 15) & ~15, sh.nb, sh.ks, io.dtype == SJD_F32,
-                  fine(io.d_out, io.out_row) && (!io.d_add || fine(io.d_add, io.add_row)), p.splits, (int32_t*)ws};
+  auto from = [&](const void* q, int64_t row) { return (char*)q + (part.t0 * row + part.n0) * es; };
+  const MatArgs a{(const char*)w.d_w + i8_weight_bytes(part.n0, w.K), w.d_scale + part.n0,
+                  io.d_code + part.t0 * io.code_row, io.d_code_scale + part.t0, from(io.d_out, io.out_row),
+                  io.d_add ? from(io.d_add, io.add_row) : nullptr, io.code_row, io.out_row, io.add_row, T, N,
+                  (w.K + 15) & ~15, sh.nb, sh.ks, io.dtype == SJD_F32, p.splits, (int32_t*)ws};
   if (!p.bt) {
     auto few = [&](auto ch, auto tt, auto depth, auto stage) {
       constexpr int CH = decltype(ch)::value, TT = decltype(tt)::value;
       hipLaunchKernelGGL((k_matmul_few<CH, TT, decltype(depth)::value, decltype(stage)::value>),
-                         dim3((w.N + CH - 1) / CH, (io.T + CH * TT - 1) / (CH * TT)), dim3(64 * kFewWaves), 0, s, a);
+                         dim3((N + CH - 1) / CH, (T + CH * TT - 1) / (CH * TT)), dim3(64 * kFewWaves), 0, s, a);
     };
     const std::false_type direct;
     const std::true_type stage;
@@ -526,18 +590,18 @@ hipError_t launch_matmul_i8(const sjd_i8_weights& w, const sjd_matmul_io& io, vo
     // their ends show: us, 16 and 32 channels, of 16 rows 4096 x 4096 5.5 and 6.0, 12288 12.3 and
     // 13.5, 22016 22.6 and 21.1; of 32 rows 4096 x 11008 15.1 and 17.9, 12288 x 4096 15.5 and 14.8. More
     // loads in flight cost workgroups: depths 2, 3 and 4 of 32 rows, 22016 x 4096: 22.6, 24.5, 25.8)
-    if (io.T <= 8) few(Int<16>{}, Int<1>{}, Int<4>{}, direct);
-    else if (io.T <= 16 && w.N <= 16384) few(Int<16>{}, Int<1>{}, Int<3>{}, stage);
-    else if (io.T <= 32 && w.N > 8192) few(Int<32>{}, Int<1>{}, Int<2>{}, stage);
-    else if (io.T <= 32) few(Int<16>{}, Int<2>{}, Int<2>{}, stage);
-    else if (w.N > 8192) few(Int<32>{}, Int<2>{}, Int<1>{}, stage);
+    if (T <= 8) few(Int<16>{}, Int<1>{}, Int<4>{}, direct);
+    else if (T <= 16 && N <= 16384) few(Int<16>{}, Int<1>{}, Int<3>{}, stage);
+    else if (T <= 32 && N > 8192) few(Int<32>{}, Int<1>{}, Int<2>{}, stage);
+    else if (T <= 32) few(Int<16>{}, Int<2>{}, Int<2>{}, stage);
+    else if (N > 8192) few(Int<32>{}, Int<2>{}, Int<1>{}, stage);
     else few(Int<16>{}, Int<4>{}, Int<4>{}, stage);
-    return hipGetLastError();
+    return;
   }
   auto many = [&](auto bt, auto bn, auto vt, auto vn) {
     constexpr int BT = decltype(bt)::value, BN = decltype(bn)::value, VT = decltype(vt)::value, VN = decltype(vn)::value;
     if (p.bt != BT || p.bn != BN) return;
-    const int nt = (io.T + BT - 1) / BT, nn = (w.N + BN - 1) / BN;
+    const int nt = (T + BT - 1) / BT, nn = (N + BN - 1) / BN;
     hipLaunchKernelGGL((k_matmul_many<BT, BN, VT, VN>), dim3(nt * nn, p.splits), dim3(64 * VT * VN), 0, s, a, nt, nn);
   };
   many(Int<256>{}, Int<256>{}, Int<2>{}, Int<4>{});
@@ -545,7 +609,13 @@ hipError_t launch_matmul_i8(const sjd_i8_weights& w, const sjd_matmul_io& io, vo
   many(Int<128>{}, Int<128>{}, Int<2>{}, Int<2>{});
   many(Int<64>{}, Int<128>{}, Int<2>{}, Int<2>{});
   many(Int<64>{}, Int<64>{}, Int<2>{}, Int<2>{});
-  if (p.splits > 1) hipLaunchKernelGGL(k_matmul_join, dim3(io.T, (w.N + 1023) / 1024), dim3(256), 0, s, a);
+  if (p.splits > 1) hipLaunchKernelGGL(k_matmul_join, dim3(T, (N + 1023) / 1024), dim3(256), 0, s, a);
+}
+
+hipError_t launch_matmul_i8(const sjd_i8_weights& w, const sjd_matmul_io& io, void* ws, hipStream_t s) {
+  MatPart part[2];
+  const int parts = matmul_parts(w.N, w.K, io.T, part);
+  for (int i = 0; i < parts; ++i) launch_part(w, io, part[i], ws, s);
   return hipGetLastError();
 }
 

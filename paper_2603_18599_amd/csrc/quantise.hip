@@ -21,26 +21,19 @@ struct QuantArgs {
   float* scale;
   int64_t x_row, gate_row, code_row;
   int T, K;
-  int x_wide, gate_wide, norm_wide;  // 16-byte loads are aligned
   int norm_f32;
   float inv_k, eps;
 };
 
-// Elements k .. k + 7 of a row, zeros behind K
+// Elements k .. k + 7 of a row, zeros behind K. Rows may start at any element: a piece is
+// loaded at the alignment of one.
 template <class E>
-SJD_DEV void load8(const E* row, int k, int K, bool wide, float (&v)[8]) {
-  if (wide && k + 8 <= K) {
-    constexpr int N = sizeof(E) / 2;  // 16-byte pieces
-    uint4 p[N];
+SJD_DEV void load8(const E* row, int k, int K, float (&v)[8]) {
+  if (k + 8 <= K) {
+    E x[8];
+    __builtin_memcpy(x, row + k, sizeof x);
 #pragma unroll
-    for (int i = 0; i < N; ++i) p[i] = ((const uint4*)(row + k))[i];
-    if constexpr (N == 2) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(((const uint32_t*)p)[e]);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = bf16_to_f32((uint16_t)(((const uint32_t*)p)[e / 2] >> (16 * (e & 1))));
-    }
+    for (int e = 0; e < 8; ++e) v[e] = elem_f32(x[e]);
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = k + e < K ? elem_f32(row[k + e]) : 0.0f;
@@ -59,7 +52,7 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void k_quantise(QuantArgs a) {
   const E* x = (const E*)a.x + t * a.x_row;
   float y[P][8];
 #pragma unroll
-  for (int i = 0; i < P; ++i) load8(x, (tid + i * NT) * 8, a.K, a.x_wide, y[i]);
+  for (int i = 0; i < P; ++i) load8(x, (tid + i * NT) * 8, a.K, y[i]);
   bool bad = false;
   if constexpr (NORM) {
     float ss = 0.0f;
@@ -74,8 +67,8 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void k_quantise(QuantArgs a) {
     for (int i = 0; i < P; ++i) {
       const int k = (tid + i * NT) * 8;
       float g[8];
-      if (a.norm_f32) load8((const float*)a.norm, k, a.K, a.norm_wide, g);
-      else load8((const uint16_t*)a.norm, k, a.K, a.norm_wide, g);
+      if (a.norm_f32) load8((const float*)a.norm, k, a.K, g);
+      else load8((const uint16_t*)a.norm, k, a.K, g);
 #pragma unroll
       for (int e = 0; e < 8; ++e) y[i][e] = y[i][e] * rinv * g[e];
     }
@@ -85,7 +78,7 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void k_quantise(QuantArgs a) {
 #pragma unroll
     for (int i = 0; i < P; ++i) {
       float g[8];
-      load8(gate, (tid + i * NT) * 8, a.K, a.gate_wide, g);
+      load8(gate, (tid + i * NT) * 8, a.K, g);
 #pragma unroll
       for (int e = 0; e < 8; ++e) y[i][e] *= silu(g[e]);
     }
@@ -114,11 +107,7 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void k_quantise(QuantArgs a) {
 }  // namespace
 
 hipError_t launch_quantise_rows(const sjd_quantise_params& p, const sjd_quantise_io& io, hipStream_t s) {
-  auto wide = [](const void* q, int64_t row, int dtype) {
-    return ((uintptr_t)q & 15) == 0 && row % (dtype == SJD_F32 ? 4 : 8) == 0;
-  };
   const QuantArgs a{io.d_x, io.d_norm, io.d_gate, io.d_code, io.d_scale, p.x_row, p.gate_row, p.code_row, p.T, p.K,
-                    wide(io.d_x, p.x_row, p.dtype), wide(io.d_gate, p.gate_row, p.dtype), wide(io.d_norm, 0, p.norm_dtype),
                     p.norm_dtype == SJD_F32, (float)(1.0 / p.K), p.eps};
   auto go = [&](auto e, auto nt, auto pieces) {
     using E = decltype(e);

@@ -219,6 +219,23 @@ def test_rows_with_addends_do_not_depend_on_their_company(N, K, dtype):
                            whole[lo:lo + n]), (lo, n)
 
 
+@pytest.mark.parametrize("T,N,K,dtype", [(4171, 4096, 4096, "bf16"), (4171, 4096, 11008, "fp32"), (1500, 12288, 4096, "bf16"),
+                                         (4096, 5001, 4096, "bf16"), (1500, 22016, 1000, "fp32")])
+def test_products_in_two_parts(T, N, K, dtype):
+    """Sizes whose last rows or channels are a launch of their own, with outputs and
+    addends in wider tensors whose other elements stay as they were."""
+    h, w = weights(N, K, 5)
+    a, s = codes(T, K, 6)
+    out = torch.full((T, N + 3), 7.0, device="cuda", dtype=DT[dtype])
+    add = torch.randn(T, N + 1, device="cuda").to(DT[dtype])[:, :N]
+    run(h, a, s, dtype, add, out[:, 1:1 + N])
+    check_product(out[:, 1:1 + N], *product(a, s, w, h.scale, add))
+    assert (out[:, 0] == 7).all() and (out[:, 1 + N:] == 7).all()
+    for lo, n in ((T - 1, 1), (T - 80, 80), (0, 200)):
+        assert torch.equal(run(h, a[lo:lo + n].contiguous(), s[lo:lo + n].contiguous(), dtype, add[lo:lo + n]),
+                           out[lo:lo + n, 1:1 + N]), (lo, n)
+
+
 def test_nan_scales_and_addends_stay_in_their_rows():
     N, K, T = 150, 256, 70
     h, w = weights(N, K, 3)
