@@ -487,8 +487,9 @@ SJD_API int sjd_pack_i8(const sjd_i8_weights* weights, const void* d_src, int32_
 
 /* out[t][n] = code_scale[t] * scale[n] * sum over k of code[t][k] * w[n][k] (+ add[t][n]),
  * rounded once to out's type behind 32-bit arithmetic. d_ws:
- * sjd_matmul_i8_workspace() bytes of scratch, 256-byte aligned (NULL when that is 0); it
- * holds nothing between calls, and calls that overlap in time need one each. */
+ * sjd_matmul_i8_workspace() bytes of scratch, 256-byte aligned (NULL when that is 0; fewer
+ * rows may need more of it); it holds nothing between calls, and calls that overlap in
+ * time need one each. */
 typedef struct {
   int32_t T;                 /* rows, 0 .. 2^24                                        */
   int32_t dtype;             /* of d_out and d_add: SJD_F32 or SJD_BF16                 */

@@ -516,16 +516,18 @@ static MatPlan plan_of(int N, int K, int T) {
                                     {128, 256, 1, 4.9, 0.347, 0.372, 0.371, 4.5, 3.4},
                                     {256, 256, 1, 7.0, 0.597, 0.740, 0.814, 4.2, 7.7}};
   const double bytes = (double)N * K;
+  auto both = [](double a, double b) { return std::sqrt(a * a + b * b); };  // (two that overlap in part)
   MatPlan best{0, 0, 1, 1e30};
   if (T <= 128) {
     const int more = (T + 63) / 64 - 1;
-    best.us = 4.1 + std::hypot(bytes * (N > 8192 ? 0.28e-6 + 0.155e-6 * more : 0.352e-6 + 0.338e-6 * more), K * 0.58e-3);
+    best.us = 4.1 + both(bytes * (N > 8192 ? 0.28e-6 + 0.155e-6 * more : 0.352e-6 + 0.338e-6 * more), K * 0.58e-3);
   }
   if (T <= 32) return best;
   for (const Tile& t : kTiles)
     for (int s = 1; s <= 8; s *= 2) {
       const int64_t nt = (T + t.bt - 1) / t.bt, wgs = (N + t.bn - 1) / t.bn * nt * s;
       if (s > 1 && (wgs > 640 || K < 512 * s)) break;
+      if (wgs >= 1 << 23) continue;  // (a launch has less than 2^32 threads)
       const int64_t per = (wgs + 255) / 256, last = t.fit > 1 ? wgs : wgs - (per - 1) * 256;
       const double steps = (K + 127) / 128 * 2.0 / s;
       double work;
@@ -536,7 +538,7 @@ static MatPlan plan_of(int N, int K, int T) {
         work = steps * per * t.shared + ((per + t.fit - 1) / t.fit - 1) * t.gap;
       if (N % 4 && s == 1) work += per * t.odd;
       // (the weights pass from memory, and once more for every row of tiles, beside the work)
-      double us = t.fixed + std::hypot(work, bytes * (0.235e-6 + 0.073e-6 * (nt - 1)));
+      double us = t.fixed + both(work, bytes * (0.235e-6 + 0.073e-6 * (nt - 1)));
       if (s > 1) us += 2.0 + 1.43e-6 * s * T * N;  // the parts' sums, and a launch
       if (us < best.us) best = MatPlan{t.bt, t.bn, s, us};
     }

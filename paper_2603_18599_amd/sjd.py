@@ -552,8 +552,8 @@ def sjd_pack_i8(weights, src, stream=None):
 
 
 def matmul_workspace(weights, T):
-    """Scratch for sjd_matmul_i8 of T rows with these weights (calls that overlap in
-    time need one each)."""
+    """Scratch for sjd_matmul_i8 of T rows with these weights (fewer rows may need more;
+    calls that overlap in time need one each)."""
     n = load_library().sjd_matmul_i8_workspace(C.byref(weights.desc), T)
     return _types()[0].empty(n, dtype=_types()[0].uint8, device=weights.w.device)
 

@@ -219,7 +219,8 @@ def test_rows_with_addends_do_not_depend_on_their_company(N, K, dtype):
                            whole[lo:lo + n]), (lo, n)
 
 
-@pytest.mark.parametrize("T,N,K,dtype", [(4171, 4096, 4096, "bf16"), (4171, 4096, 11008, "fp32"), (1500, 12288, 4096, "bf16"),
+@pytest.mark.parametrize("T,N,K,dtype", [(4171, 4096, 4096, "bf16"), (4116, 4096, 4096, "fp32"),
+                                         (4171, 4096, 11008, "fp32"), (1500, 12288, 4096, "bf16"),
                                          (4096, 5001, 4096, "bf16"), (1500, 22016, 1000, "fp32")])
 def test_products_in_two_parts(T, N, K, dtype):
     """Sizes whose last rows or channels are a launch of their own, with outputs and
