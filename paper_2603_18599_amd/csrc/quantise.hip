@@ -5,7 +5,8 @@
 // Bound by memory: a row is read once, stays in registers while its norm and its largest value
 // are found, and leaves as codes. A wave has a row of up to 2048 inputs, which needs no barrier, a
 // workgroup a longer one; many rows fill the card by themselves, few are bound by the launch and
-// the chain load - sum - largest - store (a row of 4096: 2.5 us, 128 gated rows of 11008: 4.5). 4096
+// the chain load - sum - largest - store (a row of 4096: 2.5 us, 128 gated rows of 11008: 4.5; 2000
+// rows of 20000 behind a norm 43, more than 32768 inputs pass through scratch in part). 4096
 // gated rows of 11008 37 us, 6.1 TB/s (in part from the last cache), 4096 x 4096 behind a norm 12.9.
 #include <algorithm>
 #include <type_traits>
@@ -131,6 +132,7 @@ hipError_t launch_quantise_rows(const sjd_quantise_params& p, const sjd_quantise
     else if (p.K <= 2048) go(e, Int<64>{}, Int<4>{});
     else if (p.K <= 4096) go(e, Int<256>{}, Int<2>{});
     else if (p.K <= 16384) go(e, Int<1024>{}, Int<2>{});
+    else if (p.K <= 32768) go(e, Int<1024>{}, Int<4>{});
     else go(e, Int<1024>{}, Int<8>{});
   };
   if (p.dtype == SJD_F32) pick(float{});
