@@ -4,7 +4,7 @@
 //
 // Bound by memory: a row is read once, stays in registers while its norm and its largest value
 // are found, and leaves as codes. A wave has a row of up to 2048 inputs, which needs no barrier, a
-// workgroup a longer one; many rows fill the card by themselves, few are bound by the launch and
+// workgroup a longer one or one of few; many rows fill the card by themselves, few are bound by the launch and
 // the chain load - sum - largest - store (a row of 4096: 2.5 us, 128 gated rows of 11008: 4.5; 2000
 // rows of 20000 behind a norm 43, more than 32768 inputs pass through scratch in part). 4096
 // gated rows of 11008 37 us, 6.1 TB/s (in part from the last cache), 4096 x 4096 behind a norm 12.9.
@@ -63,11 +63,21 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void k_quantise(QuantArgs a) {
   bool bad = false;
   if constexpr (NORM) {
     float ss = 0.0f;
+    if constexpr (NT == kWave) {  // (in the order of a workgroup with a piece a thread)
 #pragma unroll
-    for (int i = 0; i < P; ++i)
+      for (int i = 0; i < P; ++i) {
+        float part = 0.0f;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) ss = __builtin_fmaf(y[i][e], y[i][e], ss);
-    ss = NT == kWave ? wave_sum(ss) : block_sum<NT>(ss, red);
+        for (int e = 0; e < 8; ++e) part = __builtin_fmaf(y[i][e], y[i][e], part);
+        ss += wave_sum(part);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < P; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) ss = __builtin_fmaf(y[i][e], y[i][e], ss);
+      ss = block_sum<NT>(ss, red);
+    }
     bad = !(ss < INFINITY);
     const float rinv = 1.0f / sqrtf(ss * a.inv_k + a.eps);
 #pragma unroll
@@ -126,9 +136,12 @@ hipError_t launch_quantise_rows(const sjd_quantise_params& p, const sjd_quantise
     else if (io.d_gate) hipLaunchKernelGGL((k_quantise<E, NT, P, false, true>), grid, block, 0, s, a);
     else hipLaunchKernelGGL((k_quantise<E, NT, P, false, false>), grid, block, 0, s, a);
   };
-  // (by K alone: the order of a row's sum does not depend on the rows beside it)
+  // (The order of a row's sum is by K alone: it does not depend on the rows beside it. Of 512 to 2048
+  // inputs a workgroup to a row takes 3.1 us for 32 rows of 1024 behind a norm, a wave 3.8; for 4096
+  // rows 7.1 and 5.5)
   auto pick = [&](auto e) {
     if (p.K <= 512) go(e, Int<64>{}, Int<1>{});
+    else if (p.K <= 2048 && p.T <= 1024) go(e, Int<256>{}, Int<1>{});
     else if (p.K <= 2048) go(e, Int<64>{}, Int<4>{});
     else if (p.K <= 4096) go(e, Int<256>{}, Int<2>{});
     else if (p.K <= 16384) go(e, Int<1024>{}, Int<2>{});

@@ -73,6 +73,25 @@ def test_quantise_strides_types_and_neighbours(K, form):
         assert (buf[:, :16] == 55).all() and (buf[:, 16 + cols:] == 55).all()
 
 
+@pytest.mark.parametrize("K", [300, 700, 1024, 2047, 4096])
+@pytest.mark.parametrize("form", ["rows", "norm", "gate"])
+def test_quantised_rows_do_not_depend_on_their_company(form, K):
+    """A row's codes and scale have the same bits alone, among a few and among many."""
+    T = 1500
+    x, g = torch.randn(T, K, device="cuda"), torch.randn(T, K, device="cuda")
+
+    def rows(lo, n):
+        code, scale = torch.empty(n, sjd.code_columns(K), dtype=torch.int8, device="cuda"), torch.empty(n, device="cuda")
+        kw = dict(norm=g[0]) if form == "norm" else dict(gate=g[lo:lo + n]) if form == "gate" else {}
+        sjd.sjd_quantise_rows(x[lo:lo + n], code, scale, **kw)
+        return code, scale
+
+    code, scale = rows(0, T)
+    for lo, n in ((0, 1), (700, 64), (3, 1024), (4, 1025)):
+        c, s = rows(lo, n)
+        assert torch.equal(c, code[lo:lo + n]) and torch.equal(s, scale[lo:lo + n]), (lo, n)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("K", [70, 4096, 30000])
 def test_quantise_rows_of_special_values(K, dtype):
