@@ -287,8 +287,9 @@ def _expect(fn, ok):
 
 
 def _launch(fn, stream, device, *args):
-    """The call on `stream`, or the device's current one. Its tensors lie on
-    `device`, which must be the current GPU (the library launches there)."""
+    """The call on `stream`, or the device's current one; structs among the
+    arguments go by address. Its tensors lie on `device`, which must be the
+    current GPU (the library launches there)."""
     torch = _types()[0]
     _expect(fn, device >= 0 and device == torch._C._cuda_getDevice())
     raw = stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(device)
@@ -341,7 +342,7 @@ def sjd_verify_given(p, q, draft, n, u, r, meta, tok, next=None, *, flags=0, vis
                  _dense(fn, meta, (B, 4), i32, dev), _dense(fn, tok, (B, L + 1), i32, dev),
                  None if next is None else _dense(fn, next, (B, L), i32, dev))
     par = GivenParams(B, L, V, flags, vis_lo, p_row, p_win, q_row, q_win)
-    _launch(fn, stream, dev, C.byref(par), C.byref(io))
+    _launch(fn, stream, dev, par, io)
 
 
 def _pairs(fn, freq, axis):
@@ -384,7 +385,7 @@ def sjd_rope_axes(q, k, pos, freq, axis, *, out_q=None, out_k=None, inverse=Fals
     par = RopeParams(T, H, Hkv, hd, n, axes, types.get(dt, -1), 1 if inverse else 0, q_row, k_row, out_q_row, out_k_row, f,
                      ax)
     io = RopeIO(qp, kp, _dense(fn, pos, (T, axes), torch.int32, dev), out_qp, out_kp)
-    _launch(fn, stream, dev, C.byref(par), C.byref(io))
+    _launch(fn, stream, dev, par, io)
 
 
 def page_bytes(page_len, n_kv_heads, head_dim, dtype):
@@ -422,7 +423,7 @@ def _kv_call(fn, pages, win, k, v, stream):
     _expect(fn, k.dtype is v.dtype and win.device == dev and k.get_device() == dev and v.get_device() == dev)
     rows = KvRows(k.data_ptr(), v.data_ptr(), _row_stride(fn, k, T, H, hd), _row_stride(fn, v, T, H, hd),
                   _types()[1].get(k.dtype, -1))
-    _launch(fn, stream, dev, C.byref(pages.desc), C.byref(win.desc), C.byref(rows))
+    _launch(fn, stream, dev, pages.desc, win.desc, rows)
 
 
 def sjd_kv_append(pages, win, k, v, stream=None):
@@ -460,7 +461,7 @@ def sjd_kv_append_rope(pages, win, k, v, pos, freq, axis, *, q=None, out_q=None,
         H = q.shape[1]
         par = AppendRope(H, n, axes, types.get(out.dtype, -1), f, ax, at, q.data_ptr(), out.data_ptr(),
                          _row_stride(fn, q, T, H, hd), _row_stride(fn, out, T, H, hd))
-    _launch(fn, stream, dev, C.byref(pages.desc), C.byref(win.desc), C.byref(rows), C.byref(par))
+    _launch(fn, stream, dev, pages.desc, win.desc, rows, par)
 
 
 def attention_workspace(pages, win, H):
@@ -483,7 +484,7 @@ def sjd_paged_attention(pages, win, q, out, ws, *, scale, anc=None, stream=None)
     _expect(fn, ws.dtype is torch.uint8 and ws.is_contiguous() and (size == 0 or ws.get_device() == dev))
     io = AttentionIO(H, scale, q.data_ptr(), out.data_ptr(), _row_stride(fn, q, T, H, hd), _row_stride(fn, out, T, H, hd),
                      None if anc is None else _dense(fn, anc, (T,), torch.int64, dev))
-    _launch(fn, stream, dev, C.byref(pages.desc), C.byref(win.desc), C.byref(io), ws.data_ptr(), size)
+    _launch(fn, stream, dev, pages.desc, win.desc, io, ws.data_ptr(), size)
 
 
 def _rows2(fn, t, T, cols, device):
@@ -520,7 +521,7 @@ def sjd_quantise_rows(x, code, scale, *, norm=None, gate=None, eps=1e-5, stream=
         gp, gate_row = _rows2(fn, gate, T, K, dev)
     par = QuantiseParams(T, K, types.get(dt, -1), norm_type, eps, x_row, gate_row, code_row)
     io = QuantiseIO(xp, npt, gp, cp, _dense(fn, scale, (T,), torch.float32, dev))
-    _launch(fn, stream, dev, C.byref(par), C.byref(io))
+    _launch(fn, stream, dev, par, io)
 
 
 class I8Weights:
@@ -547,7 +548,7 @@ def sjd_pack_i8(weights, src, stream=None):
     fn = "sjd_pack_i8"
     torch, types = _types()
     p, row = _rows2(fn, src, weights.N, weights.K, weights.device)
-    _launch(fn, stream, weights.device, C.byref(weights.desc), p, 3 if src.dtype is torch.int8 else types.get(src.dtype, -1),
+    _launch(fn, stream, weights.device, weights.desc, p, 3 if src.dtype is torch.int8 else types.get(src.dtype, -1),
             row)
 
 
@@ -575,7 +576,7 @@ def sjd_matmul_i8(weights, code, code_scale, out, ws, *, add=None, stream=None):
     _expect(fn, size == 0 or ws.get_device() == dev)
     io = MatmulIO(T, types.get(dt, -1), cp, _dense(fn, code_scale, (T,), torch.float32, dev), op, ap, code_row, out_row,
                   add_row)
-    _launch(fn, stream, dev, C.byref(weights.desc), C.byref(io), ws.data_ptr(), size)
+    _launch(fn, stream, dev, weights.desc, io, ws.data_ptr(), size)
 
 
 class Engine:
