@@ -368,3 +368,33 @@ def test_two_streams_and_graphs():
         for d, v in zip(sets, got):
             go(d)
             assert torch.equal(d["out"], v)
+
+
+def test_captured_products_that_share_a_workspace():
+    """Split inputs and a product in two parts, captured with one workspace and replayed
+    in turn on one stream: nothing in it outlives a call."""
+    calls = []
+    for T, N, K in ((128, 4096, 11008), (1500, 12288, 4096), (4171, 4096, 4096)):
+        h, _ = weights(N, K, T)
+        a, s = codes(T, K, T + 1)
+        calls.append((h, a, s, torch.empty(T, N, device="cuda", dtype=torch.bfloat16)))
+    ws = max((sjd.matmul_workspace(h, a.shape[0]) for h, a, _, _ in calls), key=torch.Tensor.numel)
+    assert ws.numel() > 0
+    graphs = []
+    for h, a, s, out in calls:
+        sjd.sjd_matmul_i8(h, a, s, out, ws)
+        torch.cuda.synchronize()
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            sjd.sjd_matmul_i8(h, a, s, out, ws)
+    for i in range(4):
+        for h, a, s, out in calls:
+            a.random_(-127, 128)
+            out.zero_()
+        for g in graphs:
+            g.replay()
+        ws.fill_(0xFF)
+        graphs[i % 3].replay()
+        torch.cuda.synchronize()
+        for h, a, s, out in calls:
+            assert torch.equal(out, run(h, a, s, "bf16"))
