@@ -105,6 +105,39 @@ def test_append_rope(hd, Hkv, H, P, axes, dtype, out, plen, seqs, cache):
         assert torch.equal(q[:used], oq[:used]) and torch.equal(pool.t, first)
 
 
+@pytest.mark.parametrize("inplace", [False, True])
+@pytest.mark.parametrize("hd,Hkv,H,P,dtype,cache", [(128, 16, 32, 64, "bf16", "e4m3"), (128, 16, 16, 16, "fp32", "bf16"),
+                                                    (64, 24, 48, 5, "bf16", "bf16"), (64, 16, 33, 32, "bf16", "e4m3")])
+def test_large_calls_give_the_bits_of_small_ones(hd, Hkv, H, P, dtype, cache, inplace):
+    """Calls large enough that a workgroup has several heads and positions, against a call
+    for each sequence, and the queries against the formula."""
+    seqs = [(600, 70), (511, 0), (577, 33), (1, 5), (640, 64)]
+    pool, table, seq, T, win = setup(seqs, 64, Hkv, hd, cache, extra=2)
+    q, k, v = (torch.randn(T, n, hd, device="cuda").to(DT[dtype]) for n in (H, Hkv, Hkv))
+    pos = torch.randint(0, 100000, (T, 2), dtype=torch.int32, device="cuda")
+    freq, axis = [10000.0 ** (-i / P) for i in range(P)], [i % 2 for i in range(P)]
+    before = pool.t.clone()
+
+    def place(w, x):
+        out = None if inplace else torch.full_like(x, 7.0)
+        sjd.sjd_kv_append_rope(pool.pages, w, k, v, pos, freq, axis, q=x, out_q=out)
+        return x if inplace else out
+
+    got, pages = place(win, q.clone()), pool.t.clone()
+    pool.t.copy_(before)
+    one, x = q.clone(), q.clone()
+    for z, (first, r, c, _) in enumerate(seq):
+        w = sjd.Windows(torch.tensor([seq[z]], dtype=torch.int32).cuda(), torch.from_numpy(table[z:z + 1]).cuda(), T, r, c)
+        one[first:first + r] = place(w, x)[first:first + r]
+    used = T - 2
+    assert torch.equal(got[:used], one[:used]) and torch.equal(pages, pool.t)
+    assert torch.equal(got[used:], q[used:] if inplace else torch.full_like(q[used:], 7.0))
+    want, err = rope_reference(q, pos.cpu().numpy(), freq, axis, False), turn_error(q, P)
+    err = err + 1e5 * 2.0 ** -50 * np.abs(q.double().cpu().numpy()).max()
+    tol = err + ((np.abs(want) + err) * 2.0 ** -8 if dtype == "bf16" else 2.0 ** -24 * np.abs(want))
+    assert (np.abs(got.double().cpu().numpy() - want)[:used] <= tol[:used]).all()
+
+
 @pytest.mark.parametrize("cache", ["e4m3", "bf16"])
 def test_rows_of_a_joint_projection(cache):
     """q, k and v inside the rows of one product, queries turned in place."""
