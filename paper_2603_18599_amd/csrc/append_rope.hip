@@ -191,7 +191,7 @@ __global__ __launch_bounds__(kThreads) void k_append_rope(PlaceArgs a) {
 #pragma unroll
           for (int e = 0; e < N; ++e) {
             const int j = c * N + e;
-            o[e] = elem(k[j < a.pairs ? j + a.pairs : j < 2 * a.pairs ? j - a.pairs : j]);
+            o[e] = j < 2 * a.pairs ? elem(k[j < a.pairs ? j + a.pairs : j - a.pairs]) : 0.0f;
           }
         }
         turn<N>(turns, kf, o);
@@ -204,16 +204,18 @@ __global__ __launch_bounds__(kThreads) void k_append_rope(PlaceArgs a) {
     }
   }
 
-  // Queries of R positions: a piece is W pairs, or W dims that pass through (rows turned in place
-  // keep them); a thread keeps to one place of the heads
+  // Queries of R positions: a piece is W pairs, or dims that pass through (rows turned in place keep
+  // them): eight, or one up to the first aligned eight; a thread keeps to one place of the heads
   const int part = (int)blockIdx.y - a.YK;
   lo = max(lo, a.R * part);
   hi = min(hi, a.R * part + a.R);
   if (lo >= hi) return;
-  const int np = a.pairs / W, rest = a.out == a.q ? 0 : (HD - 2 * a.pairs) / W, per = np + rest;
+  const int np = a.pairs / W, ones = -2 * a.pairs & 7, rest = a.out == a.q ? 0 : ones + (HD - 2 * a.pairs) / 8;
+  const int per = np + rest;
   const int step = kThreads / per, g0 = threadIdx.x / per, place = threadIdx.x - g0 * per;
   const int total = g0 < step ? (hi - lo) * a.H : 0;
-  const int j = place < np ? place * W : 2 * a.pairs + (place - np) * W;
+  const bool eight = place >= np + ones;  // (WIDE: ones is 0)
+  const int j = place < np ? place * W : 2 * a.pairs + (eight ? ones + (place - np - ones) * 8 : place - np);
   if constexpr (WIDE) {
     // two pieces at a time, ahead of their use, the first ones before the angles (one, loaded when
     // it is needed: 62 us for the rows above; four: 58)
@@ -261,6 +263,12 @@ __global__ __launch_bounds__(kThreads) void k_append_rope(PlaceArgs a) {
     for (int g = g0; g < total; g += step) {
       const int r = lo + g / a.H, h = g % a.H;
       const int64_t src = (t0 + r) * a.q_row + h * HD, dst = (t0 + r) * a.out_row + h * HD;
+      if (eight) {
+        float x[8];
+        load_row<F32, 8>(a.q, src + j, x);
+        store_row<OUT32, 8>(a.out, dst + j, x);
+        continue;
+      }
       const E* q = (const E*)a.q + src;
       float u = elem(q[j]), v;
       if (place < np) {
