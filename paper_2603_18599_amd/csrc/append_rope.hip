@@ -87,8 +87,8 @@ struct Raw {
   }
 };
 // The turns of dims j .. j + N - 1 from those of their row's pairs: x, with the other of its pair o,
-// becomes x * cos + o * sin, the sine's sign being the first's or the second's of a pair
-// (dims that pass through: 1, 0). WIDE: pairs is a multiple of 8
+// becomes x * cos + o * sin, the sine's sign being the first's or the second's of a pair.
+// WIDE: pairs is a multiple of 8
 template <bool WIDE, int N>
 SJD_DEV void turns_of(const float2* cs, int j, int pairs, float2 (&t)[N]) {
 #pragma unroll
@@ -96,16 +96,17 @@ SJD_DEV void turns_of(const float2* cs, int j, int pairs, float2 (&t)[N]) {
     const int d = WIDE ? j + (e & ~7) : j + e;  // (of a piece of 8, or each by itself)
     const bool low = d < pairs;
     t[e] = make_float2(1.0f, 0.0f);
-    if (d >= 2 * pairs) continue;
+    if (d >= 2 * pairs) continue;  // (passes through)
     t[e] = cs[j + e - (low ? 0 : pairs)];
     if (low) t[e].y = -t[e].y;
   }
 }
-// (the roundings are rotate_pair's)
+// (the roundings are rotate_pair's). The first `turned` dims; those behind them pass through as they
+// are: a product with 0 would make NaN of infinities, and a sum with it +0 of -0
 template <int N>
-SJD_DEV void turn(const float2 (&t)[N], float (&x)[N], const float (&o)[N]) {
+SJD_DEV void turn(const float2 (&t)[N], int turned, float (&x)[N], const float (&o)[N]) {
 #pragma unroll
-  for (int e = 0; e < N; ++e) x[e] = __builtin_fmaf(x[e], t[e].x, o[e] * t[e].y);
+  for (int e = 0; e < N; ++e) x[e] = e < turned ? __builtin_fmaf(x[e], t[e].x, o[e] * t[e].y) : x[e];
 }
 
 template <class E>
@@ -194,7 +195,7 @@ __global__ __launch_bounds__(kThreads) void k_append_rope(PlaceArgs a) {
             o[e] = j < 2 * a.pairs ? elem(k[j < a.pairs ? j + a.pairs : j - a.pairs]) : 0.0f;
           }
         }
-        turn<N>(turns, kf, o);
+        turn<N>(turns, 2 * a.pairs - c * N, kf, o);
       }
       const int now = h;
       if (++h < end) load();

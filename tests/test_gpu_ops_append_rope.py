@@ -203,6 +203,46 @@ def test_special_values_keep_to_their_rows():
         assert torch.isnan(outs[1][1][33, 0, 2]) and torch.isnan(outs[1][0][33, 0, 3])
 
 
+@pytest.mark.parametrize("cache", ["e4m3", "bf16"])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("hd,Hkv,P", [(64, 1, 5), (64, 3, 16), (64, 2, 24), (128, 1, 5), (128, 2, 16), (128, 9, 40), (64, 2, 31)])
+def test_dims_that_pass_through_keep_their_values(hd, Hkv, P, dtype, cache):
+    """Infinities, NaN and zeros of either sign in key and query dims behind the pairs: the bytes
+    of sjd_rope_axes and then sjd_kv_append. (At position 0, whose angles are exactly 0 in both, whole
+    pages; elsewhere, in bf16 pages, the dims that pass through.)"""
+    H = 3
+    q, k, v = (torch.randn(45, n, hd, device="cuda") for n in (H, Hkv, Hkv))
+    values = torch.tensor([float("inf"), -float("inf"), float("nan"), -0.0, 0.0, 3e38, -1e-40])
+    for i, x in enumerate(values):
+        for t in (q, k, v):
+            t[3 * i + 1, i % t.shape[1], 2 * P + (5 * i + 1) % (hd - 2 * P)] = x
+    k[40, 0, 2 * P:], k[41, 0, 2 * P:], q[41, 0, 2 * P:] = float("inf"), -0.0, -0.0
+    q, k, v = (t.to(DT[dtype]) for t in (q, k, v))
+    freq, axis = [10000.0 ** (-i / P) for i in range(P)], [i % 2 for i in range(P)]
+    bits = lambda t: t.view(torch.int16 if t.dtype is torch.bfloat16 else torch.int32)  # noqa: E731
+    for at in (0, 1):
+        one, table, seq, T, win = setup([(45, 20)], 64, Hkv, hd, cache)
+        two, pos = Pool(one.n_pages, 64, Hkv, hd, cache), torch.arange(T, dtype=torch.int32, device="cuda")
+        pos = (at * pos[:, None] + torch.zeros(1, 2, dtype=torch.int32, device="cuda")).contiguous()
+        oq, q2, k2 = (torch.empty_like(t) for t in (q, q, k))
+        sjd.sjd_kv_append_rope(one.pages, win, k, v, pos, freq, axis, q=q, out_q=oq)
+        sjd.sjd_rope_axes(q, k, pos, freq, axis, out_q=q2, out_k=k2)
+        sjd.sjd_kv_append(two.pages, win, k2, v)
+        assert torch.equal(bits(oq[..., 2 * P:]), bits(q[..., 2 * P:]))
+        if at == 0:
+            assert torch.equal(bits(oq), bits(q2)) and torch.equal(one.t, two.t)
+            continue
+        got = []
+        for pool in (one, two):
+            out = [torch.empty(T, Hkv, hd, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+            sjd.sjd_kv_read(pool.pages, win, *out)
+            got.append(out)
+        assert torch.equal(bits(got[0][1]), bits(got[1][1]))
+        if cache == "bf16":
+            assert torch.equal(bits(got[0][0][..., 2 * P:]), bits(got[1][0][..., 2 * P:]))
+            assert torch.equal(bits(got[0][0][..., 2 * P:]), bits(k[..., 2 * P:].to(torch.bfloat16)))
+
+
 def layer(d, T, seed):
     """A decoder layer's tensors: 8-bit weights of q, k, v; output; gate and up; down."""
     g = torch.Generator(device="cuda").manual_seed(seed)
