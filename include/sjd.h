@@ -442,7 +442,7 @@ SJD_API int sjd_paged_attention(const sjd_pages* pages, const sjd_windows* win, 
 
 /* Row t as codes and a scale: y = x, or with d_norm x * norm / sqrt(mean of x^2 + eps)
  * (RMSNorm), or with d_gate gate / (1 + e^-gate) * x (the input of a gated layer's last
- * projection); scale[t] = max |y| / 127, code = y * (127 / max |y|) to the nearest, ties
+ * projection; 0 where e^-gate is above the largest float); scale[t] = max |y| / 127, code = y * (127 / max |y|) to the nearest, ties
  * to even. A row with max |y| below 2^-100 counts as zeros (scale 0). A row for which a
  * y is not finite, or the sum of the x^2 is not, has zeros for codes and NaN for its
  * scale, so that the products of that row, and of no other, are NaN. Computed in 32

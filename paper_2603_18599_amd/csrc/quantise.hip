@@ -7,7 +7,7 @@
 // workgroup a longer one or one of few; many rows fill the card by themselves, few are bound by the launch and
 // the chain load - sum - largest - store (a row of 4096: 2.5 us, 128 gated rows of 11008: 4.5; 2000
 // rows of 20000 behind a norm 43, more than 32768 inputs pass through scratch in part). 4096
-// gated rows of 11008 37 us, 6.1 TB/s (in part from the last cache), 4096 x 4096 behind a norm 12.9.
+// gated rows of 11008 42 us, 5.4 TB/s (in part from the last cache), 4096 x 4096 behind a norm 12.9.
 #include <algorithm>
 #include <type_traits>
 

@@ -126,6 +126,26 @@ def test_quantise_rows_of_special_values(K, dtype):
     check_rows(y, off, code[8:], scale[8:], code.shape[1])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("lo,hi,size", [(-5, -1, 1.0), (-12, -6, 1.0), (-30, -20, 1e3), (-60, -10, 1e6), (-62, -58, 1e10),
+                                        (-87, -80, 1e25), (-88.6, -87.5, 1e27), (20, 30, 1.0), (80, 200, 1.0),
+                                        (1e-20, 1e-10, 1.0), (-1e-3, 1e-3, 1.0), (3e37, 3e38, 1e-20)])
+def test_gates_of_one_size(lo, hi, size, dtype):
+    """Rows whose gates are all far below zero, or far above, or near it: no moderate gate covers for
+    what they lose. In steps of 2^-24: the power is within 2 and its correction, their product, the
+    sum with 1 and the gate's product round by one each, the reciprocal is within 2, and the last
+    product rounds by one: 9. ln 2 as a float moves e^-gate by another 0.047 |gate|."""
+    T, K = 6, 3000
+    g = torch.Generator(device="cuda").manual_seed(int(min(lo, 1000)) + 100)
+    x = (torch.randn(T, K, generator=g, device="cuda") * size).to(DT[dtype])
+    gate = (lo + (hi - lo) * torch.rand(T, K, generator=g, device="cuda")).to(DT[dtype])
+    code = torch.empty(T, sjd.code_columns(K), dtype=torch.int8, device="cuda")
+    scale = torch.empty(T, device="cuda")
+    sjd.sjd_quantise_rows(x, code, scale, gate=gate)
+    z = gate.double()
+    check_rows(x.double() * z / (1 + torch.exp(-z)), (9 + 0.047 * max(-lo, 0)) * ULP, code, scale, code.shape[1])
+
+
 def weights(N, K, seed, low=-127):
     g = torch.Generator(device="cuda").manual_seed(seed)
     w = torch.randint(low, 128, (N, K), generator=g, device="cuda", dtype=torch.int8)
