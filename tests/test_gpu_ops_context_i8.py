@@ -191,6 +191,104 @@ def test_two_contexts_at_once():
         eng.close()
 
 
+def of_operators(cfg, w, toks, n_prompt):
+    """The residual rows (fp32) of a window behind the last layer, from the operators themselves: the prompt's
+    cached rows as one window, then the rows from its last token on, a causal chain."""
+    H, Hkv, hd, F, L = (cfg[k] for k in ("n_heads", "n_kv_heads", "head_dim", "ffn_dim", "L"))
+    Nq, N, P, theta = H * hd, (H + 2 * Hkv) * hd, hd // 2, cfg["rope_theta"]
+    grid = bool(cfg["flags"] & sjd.SJD_ROPE_GRID)
+    freq = [float(theta) ** (-2.0 * i / hd) for i in range(P)]
+    axis = [0 if not grid or i < P // 4 else 1 + i % 2 for i in range(P)]
+    at = places(cfg, n_prompt, range(len(toks))).to(torch.int32)[:, :3 if grid else 1].contiguous().cuda()
+    n_pages = -(-cfg["max_seq"] // 64) + 1
+    table = torch.randperm(n_pages, generator=torch.Generator().manual_seed(1)).to(torch.int32).cuda()[None].contiguous()
+
+    def pack(*parts):
+        m = torch.cat(parts).cuda()
+        h = sjd.I8Weights(*m.shape)
+        sjd.sjd_pack_i8(h, m)
+        return h
+
+    layers = [dict(qkv=pack(l["wq"], l["wk"], l["wv"]), o=pack(l["wo"]), gu=pack(l["wg"], l["wu"]), down=pack(l["wd"]),
+                   norm=[l[n].to(torch.bfloat16).cuda() for n in ("attn_norm", "ffn_norm")],
+                   pool=torch.zeros(n_pages * sjd.page_bytes(64, Hkv, hd, "e4m3"), dtype=torch.uint8, device="cuda"))
+              for l in w["layers"]]
+    for first, T in ((0, n_prompt - 1), (n_prompt - 1, L)):
+        if T == 0:
+            continue
+        seq = torch.tensor([[0, T, first, 0]], dtype=torch.int32).cuda()
+        win = sjd.Windows(seq, table, T, T, cfg["max_seq"])
+        x = w["embed"].to(torch.bfloat16).float()[torch.tensor(toks[first:first + T]).long()].cuda()
+        qkv, q8 = torch.empty(T, N, device="cuda"), torch.empty(T, H, hd, dtype=torch.bfloat16, device="cuda")
+        q, k, v = (qkv[:, a:b].view(T, -1, hd) for a, b in ((0, Nq), (Nq, Nq + Hkv * hd), (Nq + Hkv * hd, N)))
+        att, gu = torch.empty_like(q8), torch.empty(T, 2 * F, dtype=torch.bfloat16, device="cuda")
+
+        def project(h, rows, out, add=None, **kw):
+            code, scale = torch.empty(T, h.K, dtype=torch.int8, device="cuda"), torch.empty(T, device="cuda")
+            sjd.sjd_quantise_rows(rows, code, scale, eps=cfg["rms_eps"], **kw)
+            sjd.sjd_matmul_i8(h, code, scale, out, sjd.matmul_workspace(h, T), add=add)
+
+        for l in layers:
+            pages = sjd.Pages(l["pool"], n_pages, 64, Hkv, hd, "e4m3")
+            project(l["qkv"], x, qkv, norm=l["norm"][0])
+            sjd.sjd_kv_append_rope(pages, win, k, v, at[first:first + T].contiguous(), freq, axis, q=q, out_q=q8)
+            sjd.sjd_paged_attention(pages, win, q8, att, sjd.attention_workspace(pages, win, H), scale=hd ** -0.5)
+            project(l["o"], att.view(T, Nq), x, x)
+            project(l["gu"], x, gu, norm=l["norm"][1])
+            project(l["down"], gu[:, F:], x, x, gate=gu[:, :F])
+    return x
+
+
+def head(cfg, w, x):
+    """Logits of residual rows in 64 bits, and how far the context's head may be off them: its inputs are
+    two bf16 parts (2^-18 of each left out), its sums and the squares' run over d_model terms in 32 bits
+    (2^-23 a term: the matrix unit need not round to nearest), with a few roundings beside."""
+    x, g = x.double().cpu(), w["final_norm"].double()
+    y = x / torch.sqrt((x * x).mean(-1, keepdim=True) + cfg["rms_eps"]) * g
+    m = w["lm_head"].to(torch.bfloat16).double()[cfg["vis_lo"]:cfg["vis_lo"] + cfg["V"]]
+    return y @ m.T, (2.0 ** -18 + (2 * cfg["d_model"] + 16) * 2.0 ** -23) * (y.abs() @ m.abs().T)
+
+
+CHAINS = [dict(L=16), dict(L=1, K=1, D=0, n_prompt=1), dict(L=33, n_prompt=60), dict(L=16, n_prompt=120, **GQA),
+          dict(L=16, weights_f32=True)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("flags", FLAGS)
+@pytest.mark.parametrize("over", CHAINS)
+def test_window_logits_are_those_of_the_operators(over, flags):
+    """A context's layers are the operators' calls, bit for bit: its logits are the head's of the rows that
+    the calls give. (What 8 bits round moves the logits by more than 20 times this bound:
+    test_projections_in_more_bits_are_told_apart.)"""
+    cfg = config(flags, **over)
+    w = model_weights(cfg, 3, std=STD)
+    prompt, drafts = tokens(cfg, cfg["n_prompt"], 4), tokens(cfg, cfg["L"], 5, vis=True)
+    eng = make_engine(cfg, weights_device(w))
+    eng.prefill(prompt.cuda(), 1)
+    eng.set_drafts(drafts.cuda())
+    out = torch.empty(cfg["L"], cfg["V"], device="cuda")
+    eng.forward_window(out)
+    want, tol = head(cfg, w, of_operators(cfg, w, prompt.tolist() + drafts.tolist()[:-1], cfg["n_prompt"]))
+    err = (out.cpu().double() - want).abs()
+    print("off by", err.max().item(), "of", tol.max().item())
+    assert (err <= tol).all()
+    eng.close()
+
+
+def test_projections_in_more_bits_are_told_apart():
+    """(CPU) The plain decoder without the projections' quantisation, as a context that ignored the flag
+    would be, is off by more than 20 times the bound of the comparison with the operators (one is enough)."""
+    for over in MODELS:
+        for flags in FLAGS:
+            cfg, run = config(flags, **over), case(over, flags)
+            same = lambda x: x  # noqa: E731
+            rms = off_by(run(inputs=same, weights=same), run())[1]
+            x = torch.randn(8, cfg["d_model"], generator=torch.Generator().manual_seed(1))
+            tol = head(cfg, model_weights(cfg, 3, std=STD), x)[1].max().item()  # (of normed rows: their size does not matter)
+            print("rms", rms, "bound", tol)
+            assert rms > 20 * tol
+
+
 def case(over, flags):
     cfg = config(flags, **over)
     w = model_weights(cfg, 3, std=STD)
