@@ -112,6 +112,13 @@ SJD_DEV float4 channel_scales(const MatArgs& a, int n) {
                      a.wscale[min(n + 3, a.N - 1)]);
 }
 
+// Between one lane's writes of LDS and another's reads in the same wave: no instruction (a wave's accesses
+// of LDS keep their order), the compiler's order alone
+SJD_DEV void wave_order() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+  __builtin_amdgcn_wave_barrier();
+}
+
 // Few rows: a workgroup has CH channels and TT tiles of CH rows. Its eight waves share the inputs,
 // units of 128 of them with DEPTH units' loads in flight, straight from memory into the registers
 // of the matrix operand, and add their sums up in LDS: 4096 channels would else be 128 waves. One
@@ -191,6 +198,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_matmul_few(MatArgs a) {
         for (int i = 0; i < TT; ++i)
 #pragma unroll
           for (int s = 0; s < S; ++s) *(i32x4*)(mine + (i * S + s) * 256 + lane * 4) = y[d][i][s];
+        wave_order();
       }
 #pragma unroll
       for (int s = 0; s < S; ++s)
@@ -205,6 +213,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_matmul_few(MatArgs a) {
           }
         }
       if (u + d + DEPTH < u1) load(d, u + d + DEPTH);
+      if constexpr (STAGE) wave_order();
     }
   int(*const sums)[CH * ROW] = (int(*)[CH * ROW])lds;
 #pragma unroll
@@ -401,7 +410,9 @@ __global__ __launch_bounds__(64 * VT * VN, 2) void k_matmul_many(MatArgs a, int 
         for (int r = 0; r < 16; r += 4)
           *(i32x4*)(mine + (lane & 31) * OUT + 32 * j + 2 * r + 4 * (lane >> 5)) =
               i32x4{c[i][j][r], c[i][j][r + 1], c[i][j][r + 2], c[i][j][r + 3]};
+      wave_order();
       leave(wt + 32 * i);
+      wave_order();
     }
   };
   auto rows = [&](auto f32, auto add) __attribute__((always_inline)) {
