@@ -353,7 +353,7 @@ SJD_API int64_t sjd_page_bytes(const sjd_pages* pages);
  * data cannot be reported as a status: a sequence whose numbers are negative,
  * exceed these bounds, its table or T is left out (nothing of it is read or written),
  * and so are positions whose page id lies outside [0, n_pages). Windows must not
- * share rows, nor (sjd_kv_append) positions of a page. */
+ * share rows, nor (sjd_kv_append, sjd_kv_append_rope) positions of a page. */
 typedef struct {
   int32_t B;          /* sequences, 0..65535                                          */
   int32_t T;          /* rows of the row tensors                                      */
@@ -382,8 +382,12 @@ SJD_API int sjd_kv_read(const sjd_pages* pages, const sjd_windows* win, const sj
 
 /* sjd_rope_axes and sjd_kv_append in one call: the windows' key rows are placed on
  * their axes and go into the pages with the value rows, rounded once (to the pages'
- * type), and their query rows are placed in d_out_q. The rows of sequences that are
- * left out keep their bytes; a window's queries are placed whatever its pages are. */
+ * type), and their query rows are placed in d_out_q. Dims from 2 * pairs on keep their
+ * values (infinities, NaN and the sign of zeros too). The rows of sequences that are
+ * left out keep their bytes; a window's queries are placed whatever its pages are. There is
+ * no `inverse`, and the bits need not be those of the two calls: angles are reduced by steps
+ * of their own (last bits of turned values), and keys are not rounded to the rows' type
+ * before the pages'. */
 typedef struct {
   int32_t H;         /* query heads, 0..1024; 0: no query rows                          */
   int32_t pairs;     /* 1 .. head_dim / 2                                            */
@@ -486,10 +490,12 @@ SJD_API int64_t sjd_i8_weight_bytes(int32_t N, int32_t K);
 SJD_API int sjd_pack_i8(const sjd_i8_weights* weights, const void* d_src, int32_t dtype, int64_t row, void* stream);
 
 /* out[t][n] = code_scale[t] * scale[n] * sum over k of code[t][k] * w[n][k] (+ add[t][n]),
- * rounded once to out's type behind 32-bit arithmetic. d_ws:
- * sjd_matmul_i8_workspace() bytes of scratch, 256-byte aligned (NULL when that is 0; fewer
- * rows may need more of it); it holds nothing between calls, and calls that overlap in
- * time need one each. */
+ * rounded once to out's type behind 32-bit arithmetic, in which the sum meets scale[n]
+ * first (their product must be a float too). d_ws:
+ * sjd_matmul_i8_workspace() bytes of scratch, 256-byte aligned (NULL when that is 0). Fewer
+ * rows may need more of it than many, whose tiles fill the card by themselves: a program whose
+ * row counts vary asks for each count that it will pass (a microsecond each). It
+ * holds nothing between calls, and calls that overlap in time need one each. */
 typedef struct {
   int32_t T;                 /* rows, 0 .. 2^24                                        */
   int32_t dtype;             /* of d_out and d_add: SJD_F32 or SJD_BF16                 */

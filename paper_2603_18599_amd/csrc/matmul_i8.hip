@@ -5,9 +5,11 @@
 //
 // Few rows: the weights pass once through memory, which bounds them (one row, 32768 x 4096: 20 us,
 // 6.8 TB/s where the last cache holds part of the 134 MB; 25 in a row of other work, 5.4). Many
-// rows: bound by the matrix units and by the clock that they leave (8190 rows of 4096 x 14336:
-// 402 us, 2390 TOP/s, the matrix units busy in 70% of the cycles at 1.63 GHz; 4096^3: 66 us, 2090
-// TOP/s, 51% at 1.95 GHz).
+// rows: bound by the matrix units and by the clock that they leave (bf16 outputs, no addend: 8190 rows
+// of 4096 x 14336 402 us, 2390 TOP/s, the matrix units busy in 70% of the cycles at 1.63 GHz; 4096^3 66 us,
+// 2090 TOP/s, 51% at 1.95 GHz). Between, loads on their way bound them (128 rows of 4096 x 11008, 64 x
+// 128 tiles in four parts: 13.4 us, 43 steps of 0.24 us in a workgroup to each unit, three steps of 12
+// KB under way, 136 MB from the dies' caches, the matrix units busy in 16%).
 //
 // The rows' codes are the second operand: a lane then owns one row and 16 channels of a 32 x 32
 // block, four of them one behind the other, so sums and outputs move 16 and 8 bytes at a time.
@@ -122,7 +124,8 @@ SJD_DEV void wave_order() {
 // Few rows: a workgroup has CH channels and TT tiles of CH rows. Its eight waves share the inputs,
 // units of 128 of them with DEPTH units' loads in flight, straight from memory into the registers
 // of the matrix operand, and add their sums up in LDS: 4096 channels would else be 128 waves. One
-// row of 4096 x 4096: 3.9 us; 32 rows of 12288 x 4096: 9.9 us, 5.1 TB/s.
+// row of 4096 x 4096: 3.8 us; 32 rows of 12288 x 4096: 9.8 us, 5.1 TB/s, launches in a row on the same
+// weights, which the last cache holds (5.6 and 14.3 us where they come from memory).
 template <int CH>
 struct FewMfma;
 template <>
@@ -441,8 +444,8 @@ __global__ __launch_bounds__(64 * VT * VN, 2) void k_matmul_many(MatArgs a, int 
 }
 
 // Sums of the parts of split inputs, scaled: a thread has four channels of a row. Bound by memory
-// that the parts' sums have just passed into (128 rows of 4096 channels, four parts: 2.9 us, near
-// the least a launch takes).
+// that the parts' sums have just passed into (128 rows of 4096 channels, four parts: 4.1 us, 3.8 at
+// the least).
 __global__ __launch_bounds__(256) void k_matmul_join(MatArgs a) {
   const int n0 = (blockIdx.y * 256 + threadIdx.x) * 4, t = blockIdx.x;
   if (n0 >= a.N) return;
@@ -461,8 +464,9 @@ struct PackArgs {
   int N, K, ks;
 };
 
-// A workgroup: a row block. Channels' scales, then its tiles in 16-byte pieces. (Runs once for a
-// program's weights: 22016 x 4096 codes 195 us.)
+// A workgroup: a row block. Channels' scales, then its tiles in 16-byte pieces. Bound by its loads, of an
+// element each (22016 x 4096 codes 174 us, from bf16 340, fp32 447; 4096 x 11008, 128 workgroups with 2.7
+// times the inputs each: 177, 619, 639): it runs once for a program's weights.
 template <class E>
 __global__ __launch_bounds__(256) void k_pack_i8(PackArgs a) {
   __shared__ float inv[32];
@@ -507,7 +511,8 @@ __global__ __launch_bounds__(256) void k_pack_i8(PackArgs a) {
 // Which kernel, tile and split of the inputs a product takes: the cheapest by an estimate in
 // us, fitted to 5170 timings of them all (33 to 5569 rows, 272 to 30197 channels, 289 to 14336
 // inputs; 10% off, root mean square). Over their 480 sizes its choice took 1.5% more than the
-// best of them on average, 43% at most. The results do not depend on it.
+// best of them on average, 43% at most (384 rows of 5572 x 8391; 64 rows of 5120 x 5120 37%, of 6144 x 4096
+// 31%, the others below 28%). The results do not depend on it.
 struct MatPlan {
   int bt, bn;  // rows and channels of a workgroup; bt 0: few rows
   int splits;
@@ -619,9 +624,10 @@ static void launch_part(const sjd_i8_weights& w, const sjd_matmul_io& io, const 
     const std::false_type direct;
     const std::true_type stage;
     // (16 channels to a workgroup where 32 leave compute units without one, or each with so few that
-    // their ends show: us, 16 and 32 channels, of 16 rows 4096 x 4096 5.5 and 6.0, 12288 12.3 and
-    // 13.5, 22016 22.6 and 21.1; of 32 rows 4096 x 11008 15.1 and 17.9, 12288 x 4096 15.5 and 14.8. More
-    // loads in flight cost workgroups: depths 2, 3 and 4 of 32 rows, 22016 x 4096: 22.6, 24.5, 25.8)
+    // their ends show: us with weights from memory, several in turn, 16 and 32 channels, of 16 rows 4096 x
+    // 4096 5.5 and 6.0, 12288 12.3 and 13.5, 22016 22.6 and 21.1; of 32 rows 4096 x 11008 15.1 and 17.9, 12288
+    // x 4096 15.5 and 14.8. More loads in flight cost workgroups: depths 2, 3 and 4 of 32 rows, 22016 x 4096:
+    // 22.6, 24.5, 25.8)
     if (T <= 8) few(Int<16>{}, Int<1>{}, Int<4>{}, direct);
     else if (T <= 16 && N <= 16384) few(Int<16>{}, Int<1>{}, Int<3>{}, stage);
     else if (T <= 32 && N > 8192) few(Int<32>{}, Int<1>{}, Int<2>{}, stage);

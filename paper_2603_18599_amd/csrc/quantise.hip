@@ -5,9 +5,10 @@
 // Bound by memory: a row is read once, stays in registers while its norm and its largest value
 // are found, and leaves as codes. A wave has a row of up to 2048 inputs, which needs no barrier, a
 // workgroup a longer one or one of few; many rows fill the card by themselves, few are bound by the launch and
-// the chain load - sum - largest - store (a row of 4096: 2.5 us, 128 gated rows of 11008: 4.5; 2000
-// rows of 20000 behind a norm 43, more than 32768 inputs pass through scratch in part). 4096
-// gated rows of 11008 42 us, 5.4 TB/s (in part from the last cache), 4096 x 4096 behind a norm 12.9.
+// the chain load - sum - largest - store (a row of 4096: 2.4 us, 128 gated rows of 11008: 5.4; 2000
+// rows of 20000 behind a norm 42, more than 32768 inputs pass through scratch in part). Calls in a row
+// on rows that the last cache holds in part: 4096 gated rows of 11008 42 us, 5.4 TB/s, 4096 x 4096 behind a
+// norm 12.5; between other work the latter takes 15.4 to 18.6.
 #include <algorithm>
 #include <type_traits>
 
