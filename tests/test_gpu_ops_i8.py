@@ -146,6 +146,24 @@ def test_gates_of_one_size(lo, hi, size, dtype):
     check_rows(x.double() * z / (1 + torch.exp(-z)), (9 + 0.047 * max(-lo, 0)) * ULP, code, scale, code.shape[1])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("K", [100, 4096, 20000])
+def test_gates_of_special_values(K, dtype):
+    """A gate that is no number or has no limit makes its row, and no other, NaN, at whatever x; the largest
+    finite ones are themselves above zero and 0 below it."""
+    inf, nan = float("inf"), float("nan")
+    x, gate = torch.ones(8, K, device="cuda"), torch.ones(8, K, device="cuda")
+    gate[0, K - 1], gate[1, 0], gate[2, K // 2], gate[3, 1], gate[4], gate[5, 3] = inf, -inf, nan, 3e38, -3e38, -3e38
+    x[1, 0], x[3] = 0.0, 1e-3
+    x, gate = x.to(DT[dtype]), gate.to(DT[dtype])
+    code, scale = torch.empty(8, sjd.code_columns(K), dtype=torch.int8, device="cuda"), torch.empty(8, device="cuda")
+    sjd.sjd_quantise_rows(x, code, scale, gate=gate)
+    assert torch.isnan(scale[:3]).all() and (code[:3] == 0).all() and scale[4] == 0 and (code[4] == 0).all()
+    assert (code[[5, 6, 7], :K] == torch.where(gate[[5, 6, 7]] < 0, 0, 127)).all() and torch.isfinite(scale[5:]).all()
+    y = (x[3].double() * gate[3].double()).max()
+    assert abs(scale[3].double() - y / 127) <= y / 127 * 11 * ULP and code[3, 1] == 127 and (code[3, 2:] == 0).all()
+
+
 def weights(N, K, seed, low=-127):
     g = torch.Generator(device="cuda").manual_seed(seed)
     w = torch.randint(low, 128, (N, K), generator=g, device="cuda", dtype=torch.int8)
